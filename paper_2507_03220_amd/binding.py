@@ -1,6 +1,6 @@
 """ctypes binding of libsymb.so: argument marshalling only.
 
-Every function here has the name of the C entry point it calls (include/symb.h) and
+Every function here has the name of the C entry point it calls (include/symb.h, include/symb_block.h) and
 does nothing but turn torch tensors into device pointers and host lists into C arrays.
 All arithmetic runs in the HIP kernels; there is no CPU or PyTorch fallback: if the
 library is missing, `lib()` raises.
@@ -25,6 +25,9 @@ SYMB_BWD_FULL, SYMB_BWD_BASE_ONLY, SYMB_BWD_REUSE_DH = 0, 1, 2
 SYMB_GRAD_OVERWRITE, SYMB_GRAD_ACCUMULATE, SYMB_GRAD_REUSE_DH, SYMB_GRAD_REUSE_HS = 0, 1, 2, 4
 SYMB_MAX_RANK = 128
 SYMB_WEIGHT_LINEAR, SYMB_WEIGHT_CONV1D = 0, 1
+SYMB_NORM_LAYER, SYMB_NORM_RMS = 0, 1
+SYMB_NORM_MAX_WIDTH = 16384
+SYMB_ROTATE_HALVES, SYMB_ROTATE_ADJACENT = 0, 1
 
 EXPORTS = ("symb_create", "symb_destroy", "symb_validate_batch", "symb_debug_row_segment_map",
            "symb_plan_row_tiles", "symb_workspace_bytes", "symb_base_linear_fwd",
@@ -35,7 +38,8 @@ EXPORTS = ("symb_create", "symb_destroy", "symb_validate_batch", "symb_debug_row
            "symb_batcher_create", "symb_batcher_destroy", "symb_batcher_submit", "symb_batcher_pending",
            "symb_batcher_next_due", "symb_batcher_take",
            "symb_debug_gemm_timing_enable", "symb_debug_gemm_timing_read", "symb_debug_descriptor_stats",
-           "symb_debug_set_option", "symb_debug_xcd_rule", "symb_base_linear_fwd_static")
+           "symb_debug_set_option", "symb_debug_xcd_rule", "symb_base_linear_fwd_static",
+           "symb_norm_workspace_bytes", "symb_norm_fwd", "symb_norm_bwd", "symb_kv_append", "symb_kv_workspace_bytes", "symb_kv_attention")
 
 
 class symb_adapter(C.Structure):
@@ -51,6 +55,29 @@ class symb_batch(C.Structure):
     _fields_ = [("d_in", C.c_int32), ("d_out", C.c_int32), ("num_segments", C.c_int32),
                 ("seg_offsets", C.POINTER(C.c_int32)), ("adapters", C.POINTER(symb_adapter)),
                 ("weight_layout", C.c_int32)]
+
+
+class symb_norm(C.Structure):
+    _fields_ = [("weight", C.c_void_p), ("bias", C.c_void_p), ("dweight", C.c_void_p), ("dbias", C.c_void_p)]
+
+
+class symb_norm_batch(C.Structure):
+    _fields_ = [("width", C.c_int32), ("num_segments", C.c_int32), ("seg_offsets", C.POINTER(C.c_int32)),
+                ("norms", C.POINTER(symb_norm)), ("kind", C.c_int32), ("eps", C.c_float), ("weight_base", C.c_float)]
+
+
+class symb_kv_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("num_pages", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_tokens", C.c_int32)]
+
+
+class symb_kv_batch(C.Structure):
+    _fields_ = [("num_segments", C.c_int32), ("seg_offsets", C.POINTER(C.c_int32)), ("past", C.POINTER(C.c_int32)),
+                ("page_table", C.c_void_p), ("table_stride", C.c_int32)]
+
+
+class symb_rotation(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("positions", C.c_int32), ("dim", C.c_int32), ("pairs", C.c_int32)]
 
 
 class SymbError(RuntimeError):
@@ -95,6 +122,14 @@ def lib() -> C.CDLL:
         l.symb_debug_set_option.argtypes = [vp, i32, i32]
         l.symb_debug_xcd_rule.argtypes = [vp, C.POINTER(i32), C.POINTER(i32)]
         l.symb_base_linear_fwd_static.argtypes = [vp, bp, vp, vp, vp, vp, vp, vp]
+        np_, kp, cp, rp = (C.POINTER(t) for t in (symb_norm_batch, symb_kv_batch, symb_kv_cache, symb_rotation))
+        i64 = C.c_int64
+        l.symb_norm_workspace_bytes.argtypes = [np_, C.POINTER(sz)]
+        l.symb_norm_fwd.argtypes = [vp, np_, vp, vp, vp]
+        l.symb_norm_bwd.argtypes = [vp, np_, vp, vp, vp, u32, vp, sz, vp]
+        l.symb_kv_append.argtypes = [vp, kp, cp, rp, vp, i64, i32, vp, i64, vp, i64, vp, i64, vp]
+        l.symb_kv_workspace_bytes.argtypes = [kp, cp, i32, i32, C.POINTER(sz)]
+        l.symb_kv_attention.argtypes = [vp, kp, cp, vp, i64, i32, vp, i64, C.c_float, i32, C.c_float, vp, sz, vp]
         l.symb_status_string.argtypes = [C.c_int]
         l.symb_status_string.restype = C.c_char_p
         l.symb_last_error.argtypes = [vp]
@@ -152,6 +187,114 @@ class Batch:
         self.c = symb_batch(int(d_in), int(d_out), S, self._off, self._ad, int(weight_layout))
         self.d_in, self.d_out, self.S = int(d_in), int(d_out), S
         self.T = int(seg_offsets[-1]) if S >= 0 and len(seg_offsets) else 0
+
+    def ref(self):
+        return C.byref(self.c)
+
+
+def _int32s(values):
+    v = [int(x) for x in values]
+    return (C.c_int32 * max(len(v), 1))(*v)
+
+
+def _shaped(t, what: str, dtype: str, dims: int):
+    """The tensor as the C ABI takes it, or ValueError: `dims` dimensions of that type."""
+    if t.dim() != dims or not str(t.dtype).endswith(dtype):
+        raise ValueError(f"{what}: {dims} dimensions of {dtype} expected, got {tuple(t.shape)} of {t.dtype}")
+    return t
+
+
+def _dense(t, what: str, dtype: str, dims: int):
+    if not _shaped(t, what, dtype, dims).is_contiguous():
+        raise ValueError(f"{what} must be dense")
+    return t
+
+
+def _head_rows(t, what: str, T: int, heads: int, dim: int) -> int:
+    """Row stride of a [T][heads][dim] bf16 tensor whose rows may lie apart."""
+    _shaped(t, what, "bfloat16", 3)
+    if tuple(t.shape) != (T, heads, dim) or t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+        raise ValueError(f"{what}: [{T}][{heads}][{dim}] with whole rows expected, got {tuple(t.shape)}, strides {t.stride()}")
+    return t.stride(0) if T > 1 else max(t.stride(0), heads * dim)
+
+
+@dataclass
+class Norm:
+    """One segment's norm: bf16 weight and bias, fp32 gradients (device tensors or raw addresses; None as in symb_norm)."""
+    weight: object = None
+    bias: object = None
+    dweight: object = None
+    dbias: object = None
+
+
+class NormBatch:
+    """Owns the C arrays of one symb_norm_batch."""
+
+    def __init__(self, width: int, seg_offsets: Sequence[int], norms: Sequence[Norm], kind: int = SYMB_NORM_LAYER, eps: float = 1e-5,
+                 weight_base: float = 0.0):
+        S = len(norms)
+        if len(seg_offsets) != S + 1:
+            raise ValueError("seg_offsets must have num_segments + 1 entries")
+        self.width, self.S, self.T = int(width), S, int(seg_offsets[-1])
+        for i, n in enumerate(norms):
+            for what, t, dtype in (("weight", n.weight, "bfloat16"), ("bias", n.bias, "bfloat16"), ("dweight", n.dweight, "float32"), ("dbias", n.dbias, "float32")):
+                if t is not None and not isinstance(t, int) and _dense(t, f"{what} of segment {i}", dtype, 1).numel() != self.width:
+                    raise ValueError(f"{what} of segment {i} has {t.numel()} elements, the width is {self.width}")
+        self._off, self._keep = _int32s(seg_offsets), list(norms)
+        self._norms = (symb_norm * max(S, 1))(*[(_ptr(n.weight), _ptr(n.bias), _ptr(n.dweight), _ptr(n.dbias)) for n in norms])
+        self.c = symb_norm_batch(self.width, S, self._off, self._norms, int(kind), float(eps), float(weight_base))
+
+    def ref(self):
+        return C.byref(self.c)
+
+
+class KvCache:
+    """A pool of cache pages: k [pages][kv_heads][page_tokens][head_dim] and v [pages][kv_heads][head_dim][page_tokens] of float8_e4m3fn (or
+    uint8), k_scale and v_scale [pages][kv_heads] of float8_e8m0fnu (or uint8), all dense device tensors.  `empty` makes one."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        if k.dim() != 4 or v.dim() != 4 or tuple(v.shape) != (k.shape[0], k.shape[1], k.shape[3], k.shape[2]):
+            raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} are no cache pages")
+        for what, t, dims in (("k", k, 4), ("v", v, 4), ("k_scale", k_scale, 2), ("v_scale", v_scale, 2)):
+            if t.element_size() != 1 or not t.is_contiguous() or t.dim() != dims or tuple(t.shape[:2]) != tuple(k.shape[:2]):
+                raise ValueError(f"{what}: dense 8-bit tensor of {tuple(k.shape[:2])} blocks expected, got {tuple(t.shape)} of {t.dtype}")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.num_pages, self.kv_heads, self.page_tokens, self.head_dim = k.shape
+        self.c = symb_kv_cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), self.num_pages, self.kv_heads, self.head_dim, self.page_tokens)
+
+    @classmethod
+    def empty(cls, num_pages: int, kv_heads: int, head_dim: int, page_tokens: int = 64, device="cuda"):
+        import torch
+        make = lambda *shape, dtype: torch.zeros(shape, device=device, dtype=torch.uint8).view(dtype)  # noqa: E731
+        return cls(make(num_pages, kv_heads, page_tokens, head_dim, dtype=torch.float8_e4m3fn), make(num_pages, kv_heads, head_dim, page_tokens, dtype=torch.float8_e4m3fn),
+                   make(num_pages, kv_heads, dtype=torch.float8_e8m0fnu), make(num_pages, kv_heads, dtype=torch.float8_e8m0fnu))
+
+    def ref(self):
+        return C.byref(self.c)
+
+
+class KvBatch:
+    """Owns the C arrays of one symb_kv_batch; page_table: int32 device tensor [num_segments][pages] (None for host-only calls: `table_stride` then)."""
+
+    def __init__(self, seg_offsets: Sequence[int], past: Sequence[int], page_table, table_stride: int = 0):
+        self.S, self.T = len(past), int(seg_offsets[-1])
+        if len(seg_offsets) != self.S + 1:
+            raise ValueError("seg_offsets must have num_segments + 1 entries")
+        if page_table is not None and _dense(page_table, "page_table", "int32", 2).shape[0] != self.S:
+            raise ValueError(f"page_table has {page_table.shape[0]} rows for {self.S} segments")
+        self._off, self._past, self.page_table = _int32s(seg_offsets), _int32s(past), page_table
+        self.c = symb_kv_batch(self.S, self._off, self._past, _ptr(page_table), page_table.shape[1] if page_table is not None else int(table_stride))
+
+    def ref(self):
+        return C.byref(self.c)
+
+
+class Rotation:
+    """Cosines and sines by position: fp32 device tensor [positions][dim], cosines first."""
+
+    def __init__(self, table, pairs: int = SYMB_ROTATE_HALVES):
+        self.table = _dense(table, "table", "float32", 2)
+        self.c = symb_rotation(table.data_ptr(), table.shape[0], table.shape[1], int(pairs))
 
     def ref(self):
         return C.byref(self.c)
@@ -324,3 +467,50 @@ def symb_debug_xcd_rule(handle):
     ids = (C.c_int32 * 8)()
     _check(lib().symb_debug_xcd_rule(handle, C.byref(ok), ids), handle)
     return bool(ok.value), list(ids)
+
+
+# ---- include/symb_block.h ----------------------------------------------------------------------
+def symb_norm_workspace_bytes(batch: NormBatch) -> int:
+    out = C.c_size_t(0)
+    _check(lib().symb_norm_workspace_bytes(batch.ref(), C.byref(out)))
+    return int(out.value)
+
+
+def _norm_rows(batch: NormBatch, **tensors) -> None:
+    for what, t in tensors.items():
+        if tuple(_dense(t, what, "bfloat16", 2).shape) != (batch.T, batch.width):
+            raise ValueError(f"{what}: [{batch.T}][{batch.width}] expected, got {tuple(t.shape)}")
+
+
+def symb_norm_fwd(handle, batch: NormBatch, X, Y, stream: int = 0) -> None:
+    _norm_rows(batch, X=X, Y=Y)
+    _check(lib().symb_norm_fwd(handle, batch.ref(), X.data_ptr(), Y.data_ptr(), stream or None), handle)
+
+
+def symb_norm_bwd(handle, batch: NormBatch, X, dY, dX, flags: int = SYMB_GRAD_OVERWRITE, ws=None, stream: int = 0) -> None:
+    _norm_rows(batch, X=X, dY=dY, dX=dX)
+    wp, wb = _ws_args(ws)
+    _check(lib().symb_norm_bwd(handle, batch.ref(), X.data_ptr(), dY.data_ptr(), dX.data_ptr(), int(flags), wp, wb, stream or None), handle)
+
+
+def symb_kv_append(handle, batch: KvBatch, cache: KvCache, rotation: Optional[Rotation], q, q_out, k, v, stream: int = 0) -> None:
+    """q, q_out [T][q_heads][head_dim] (both None: keys and values only), k, v [T][kv_heads][head_dim]; rows may lie apart."""
+    T, H, D = batch.T, cache.kv_heads, cache.head_dim
+    heads = 0 if q is None else q.shape[1]
+    _check(lib().symb_kv_append(handle, batch.ref(), cache.ref(), None if rotation is None else rotation.ref(), _ptr(q),
+                                _head_rows(q, "q", T, heads, D) if heads else 0, heads, _ptr(q_out), _head_rows(q_out, "q_out", T, heads, D) if heads else 0,
+                                k.data_ptr(), _head_rows(k, "k", T, H, D), v.data_ptr(), _head_rows(v, "v", T, H, D), stream or None), handle)
+
+
+def symb_kv_workspace_bytes(batch: KvBatch, cache: KvCache, q_heads: int, window: int = 0) -> int:
+    out = C.c_size_t(0)
+    _check(lib().symb_kv_workspace_bytes(batch.ref(), cache.ref(), int(q_heads), int(window), C.byref(out)))
+    return int(out.value)
+
+
+def symb_kv_attention(handle, batch: KvBatch, cache: KvCache, q, out, scale: float, window: int = 0, cap: float = 0.0, ws=None, stream: int = 0) -> None:
+    """q, out [T][q_heads][head_dim]; rows may lie apart."""
+    T, heads, D = batch.T, q.shape[1], cache.head_dim
+    wp, wb = _ws_args(ws)
+    _check(lib().symb_kv_attention(handle, batch.ref(), cache.ref(), q.data_ptr(), _head_rows(q, "q", T, heads, D), heads, out.data_ptr(),
+                                   _head_rows(out, "out", T, heads, D), float(scale), int(window), float(cap), wp, wb, stream or None), handle)

@@ -1,0 +1,468 @@
+// Host side of include/symb_block.h: argument checks, work lists and launches of the norms and of the calls on the key/value cache.
+#include "../../include/symb_block.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <utility>
+#include <vector>
+
+#include "kv_append_kernel.hpp"
+#include "kv_attention_kernels.hpp"
+#include "norm_kernels.hpp"
+#include "symb_context.hpp"
+
+using namespace symb;
+
+namespace {
+
+// Nothing throws across the C boundary: the work lists are the only allocations.
+template <class F>
+symb_status guarded(symb_handle h, F&& f) {
+    try {
+        return f();
+    } catch (const std::bad_alloc&) {
+        return fail(h, SYMB_ERR_UNSUPPORTED, "out of host memory for the batch's work lists");
+    }
+}
+
+symb_status check_segments(symb_handle h, int32_t S, const int32_t* off) {
+    if (S < 0) return fail(h, SYMB_ERR_INVALID_ARG, "num_segments is negative");
+    if (!off) return fail(h, SYMB_ERR_INVALID_ARG, "seg_offsets is null");
+    if (off[0] != 0) return fail(h, SYMB_ERR_BAD_SEGMENTS, "seg_offsets[0] must be 0");
+    for (int i = 0; i < S; ++i)
+        if (off[i + 1] < off[i]) return fail(h, SYMB_ERR_BAD_SEGMENTS, "seg_offsets decrease at segment %d", i);
+    return SYMB_OK;
+}
+
+// ---- norms -----------------------------------------------------------------------------------
+symb_status check_norm(symb_handle h, const symb_norm_batch* b) {
+    if (!b) return fail(h, SYMB_ERR_INVALID_ARG, "batch is null");
+    if (b->width <= 0 || b->width % 8) return fail(h, SYMB_ERR_INVALID_ARG, "width must be a positive multiple of 8");
+    if (b->width > SYMB_NORM_MAX_WIDTH) return fail(h, SYMB_ERR_UNSUPPORTED, "width %d exceeds SYMB_NORM_MAX_WIDTH", b->width);
+    if (b->kind != SYMB_NORM_LAYER && b->kind != SYMB_NORM_RMS) return fail(h, SYMB_ERR_INVALID_ARG, "unknown norm kind %d", b->kind);
+    if (!(b->eps >= 0.f) || !std::isfinite(b->eps)) return fail(h, SYMB_ERR_INVALID_ARG, "eps must be finite and not negative");
+    if (!std::isfinite(b->weight_base)) return fail(h, SYMB_ERR_INVALID_ARG, "weight_base must be finite");
+    const symb_status st = check_segments(h, b->num_segments, b->seg_offsets);
+    if (st != SYMB_OK) return st;
+    if (b->num_segments && !b->norms) return fail(h, SYMB_ERR_INVALID_ARG, "norms is null");
+    for (int i = 0; i < b->num_segments; ++i) {
+        const symb_norm& n = b->norms[i];
+        for (const void* ptr : {n.weight, n.bias, (const void*)n.dweight, (const void*)n.dbias})
+            if (misaligned16(ptr)) return fail(h, SYMB_ERR_INVALID_ARG, "segment %d: norm pointer is not 16-byte aligned", i);
+    }
+    return SYMB_OK;
+}
+
+// The backward pass in chunks of rows.  Chunks of one group (the segments that name the same gradients) have their partial sums side by side, in the order
+// of the batch, and are added in it.
+struct NormPlan {
+    std::vector<NormChunk> chunks;
+    std::vector<NormGroup> groups;
+    int parts = 0;
+};
+// Enough chunks to give every CU several workgroups, and no shorter than kNormRows rows while that holds: a chunk's partial sums cost as much traffic as a row and a third.
+constexpr int kNormChunks = 1024, kNormRows = 4;
+symb_status plan_norm(symb_handle h, const symb_norm_batch* b, NormPlan& plan) {
+    const int S = b->num_segments, T = b->seg_offsets[S];
+    std::vector<int> order(S);
+    for (int i = 0; i < S; ++i) order[i] = i;
+    const symb_norm* n = b->norms;
+    auto key = [&](int i) { return std::make_pair((uintptr_t)n[i].dweight, (uintptr_t)n[i].dbias); };
+    std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return key(x) < key(y); });
+    // a gradient named together with two different partners
+    std::vector<std::pair<uintptr_t, uintptr_t>> seen;
+    for (int i = 0; i < S; ++i) {
+        if (i && key(order[i]) == key(order[i - 1])) continue;
+        const auto k = key(order[i]);
+        if (k.first) seen.emplace_back(k.first, i);
+        if (k.second) seen.emplace_back(k.second, i);
+    }
+    std::sort(seen.begin(), seen.end());
+    for (size_t i = 1; i < seen.size(); ++i)
+        if (seen[i].first == seen[i - 1].first) return fail(h, SYMB_ERR_INVALID_ARG, "two segments share one of dweight and dbias, but not both");
+    const int rows = std::max(kNormRows, (T + kNormChunks - 1) / kNormChunks);
+    for (int at = 0; at < S;) {
+        int to = at + 1;
+        while (to < S && key(order[to]) == key(order[at])) ++to;
+        const bool wanted = n[order[at]].dweight || n[order[at]].dbias;
+        NormGroup g{(float*)n[order[at]].dweight, (float*)n[order[at]].dbias, plan.parts, 0};
+        for (int i = at; i < to; ++i) {
+            const int s = order[i];
+            for (int r = b->seg_offsets[s]; r < b->seg_offsets[s + 1]; r += rows)
+                plan.chunks.push_back(NormChunk{s, r, std::min(rows, b->seg_offsets[s + 1] - r), wanted ? plan.parts + g.parts++ : -1});
+        }
+        plan.parts += g.parts;
+        if (wanted) plan.groups.push_back(g);
+        at = to;
+    }
+    return SYMB_OK;
+}
+size_t norm_part_bytes(const NormPlan& plan, int width) { return align_up((size_t)plan.parts * width * sizeof(float), 256); }
+
+std::vector<NormDesc> norm_descs(const symb_norm_batch* b) {
+    std::vector<NormDesc> d(b->num_segments);
+    for (int i = 0; i < b->num_segments; ++i)
+        d[i] = NormDesc{(const bf16*)b->norms[i].weight, (const bf16*)b->norms[i].bias, (float*)b->norms[i].dweight, (float*)b->norms[i].dbias};
+    return d;
+}
+
+template <bool RMS, int WAVES, int NV>
+void launch_norm_fwd(const NormFwdParams& p, hipStream_t s) {
+    constexpr int rows = WAVES < 4 ? 4 / WAVES : 1;
+    hipLaunchKernelGGL((symb_norm_fwd_kernel<RMS, WAVES, NV>), dim3((p.T + rows - 1) / rows), dim3(WAVES < 4 ? 256 : WAVES * 64), 0, s, p);
+}
+template <bool RMS>
+void launch_norm_fwd(const NormFwdParams& p, hipStream_t s) {
+    const int vecs = p.width / 8;
+    if (vecs <= 64) return launch_norm_fwd<RMS, 1, 1>(p, s);
+    if (vecs <= 256) return launch_norm_fwd<RMS, 1, 4>(p, s);
+    if (vecs <= 512) return launch_norm_fwd<RMS, 4, 2>(p, s);
+    if (vecs <= 768) return launch_norm_fwd<RMS, 4, 3>(p, s);
+    if (vecs <= 1024) return launch_norm_fwd<RMS, 4, 4>(p, s);
+    return launch_norm_fwd<RMS, 4, 8>(p, s);
+}
+template <bool RMS, int WAVES, int NV>
+void launch_norm_bwd(const NormBwdParams& p, int chunks, hipStream_t s) {
+    hipLaunchKernelGGL((symb_norm_bwd_kernel<RMS, WAVES, NV>), dim3(chunks), dim3(WAVES * 64), 0, s, p);
+}
+template <bool RMS>
+void launch_norm_bwd(const NormBwdParams& p, int chunks, hipStream_t s) {
+    const int vecs = p.width / 8;
+    if (vecs <= 256) return launch_norm_bwd<RMS, 4, 1>(p, chunks, s);
+    if (vecs <= 512) return launch_norm_bwd<RMS, 4, 2>(p, chunks, s);
+    if (vecs <= 768) return launch_norm_bwd<RMS, 4, 3>(p, chunks, s);
+    if (vecs <= 1024) return launch_norm_bwd<RMS, 4, 4>(p, chunks, s);
+    return launch_norm_bwd<RMS, 16, 2>(p, chunks, s);
+}
+
+// ---- key/value cache --------------------------------------------------------------------------
+symb_status check_kv(symb_handle h, const symb_kv_batch* b, const symb_kv_cache* c) {
+    if (!b) return fail(h, SYMB_ERR_INVALID_ARG, "batch is null");
+    if (!c) return fail(h, SYMB_ERR_INVALID_ARG, "cache is null");
+    const symb_status st = check_segments(h, b->num_segments, b->seg_offsets);
+    if (st != SYMB_OK) return st;
+    if (c->num_pages <= 0 || c->kv_heads <= 0) return fail(h, SYMB_ERR_INVALID_ARG, "num_pages and kv_heads must be positive");
+    if (c->kv_heads > 8192) return fail(h, SYMB_ERR_UNSUPPORTED, "%d key heads: 8192 at most", c->kv_heads);
+    if (c->head_dim != 64 && c->head_dim != 128) return fail(h, SYMB_ERR_UNSUPPORTED, "head_dim %d: 64 or 128", c->head_dim);
+    if (c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128)
+        return fail(h, SYMB_ERR_UNSUPPORTED, "page_tokens %d: 32, 64 or 128", c->page_tokens);
+    if (b->num_segments && !b->past) return fail(h, SYMB_ERR_INVALID_ARG, "past is null");
+    if (b->table_stride < 0 || (int64_t)b->num_segments * b->table_stride > INT32_MAX)
+        return fail(h, SYMB_ERR_UNSUPPORTED, "page table of %d x %d entries", b->num_segments, b->table_stride);
+    for (int i = 0; i < b->num_segments; ++i) {
+        const int64_t n = b->seg_offsets[i + 1] - b->seg_offsets[i], len = (int64_t)b->past[i] + n;
+        if (b->past[i] < 0) return fail(h, SYMB_ERR_INVALID_ARG, "past of segment %d is negative", i);
+        if (!n) continue;
+        if (len > INT32_MAX - 1024) return fail(h, SYMB_ERR_UNSUPPORTED, "segment %d has %lld tokens", i, (long long)len);
+        if ((len + c->page_tokens - 1) / c->page_tokens > b->table_stride)
+            return fail(h, SYMB_ERR_INVALID_ARG, "segment %d has %lld tokens, its row of the page table %d pages", i, (long long)len, b->table_stride);
+    }
+    return SYMB_OK;
+}
+symb_status check_kv_pointers(symb_handle h, const symb_kv_batch* b, const symb_kv_cache* c) {
+    if (!c->k || !c->v || !c->k_scale || !c->v_scale) return fail(h, SYMB_ERR_INVALID_ARG, "cache pointers are required");
+    if (misaligned16(c->k) || misaligned16(c->v)) return fail(h, SYMB_ERR_INVALID_ARG, "cache pointers must be 16-byte aligned");
+    if (!b->page_table || ((uintptr_t)b->page_table & 3)) return fail(h, SYMB_ERR_INVALID_ARG, "page_table is null or misaligned");
+    return SYMB_OK;
+}
+symb_status check_rows(symb_handle h, const void* p, int64_t stride, int64_t width, const char* what) {
+    if (!p) return fail(h, SYMB_ERR_INVALID_ARG, "%s is null", what);
+    if (misaligned16(p)) return fail(h, SYMB_ERR_INVALID_ARG, "%s is not 16-byte aligned", what);
+    if (stride < width || stride % 8) return fail(h, SYMB_ERR_INVALID_ARG, "%s has rows %lld elements apart: a multiple of 8, %lld at least", what, (long long)stride, (long long)width);
+    return SYMB_OK;
+}
+int page_shift(const symb_kv_cache* c) { return c->page_tokens == 32 ? 5 : c->page_tokens == 64 ? 6 : 7; }
+
+template <int D>
+void launch_append(const KvAppendParams& p, int pages, bool few, int ny, hipStream_t s) {
+    if (few) hipLaunchKernelGGL((symb_kv_append_kernel<D, 64>), dim3(pages, ny), dim3(64), 0, s, p);
+    else hipLaunchKernelGGL((symb_kv_append_kernel<D, 256>), dim3(pages, ny), dim3(256), 0, s, p);
+}
+
+// The work of one attention call.
+struct KvPlan {
+    std::vector<KvRowsItem> rows;
+    std::vector<KvJoinItem> joins;
+    int part_rows = 0;                    // rows of partial results, of one key head
+};
+// Chunks of 128 tokens that a workgroup takes: its four wavefronts two each at least (a shorter run costs more in joining than it gains), and as many as leave kKvGroups workgroups.
+constexpr int kKvGroups = 1024, kKvLeast = 8;
+KvPlan plan_attention(const symb_kv_batch* b, const symb_kv_cache* c, int q_heads, int window) {
+    KvPlan plan;
+    const int group = q_heads / c->kv_heads;
+    auto walk = [&](auto&& f) {                       // f(segment, first row, its rows, first chunk, end)
+        for (int i = 0; i < b->num_segments; ++i) {
+            const int64_t rows = (int64_t)(b->seg_offsets[i + 1] - b->seg_offsets[i]) * group;
+            for (int64_t r0 = 0; r0 < rows; r0 += 16) {
+                const int64_t first = b->past[i] + r0 / group, last = b->past[i] + std::min(r0 + 15, rows - 1) / group;
+                const int64_t lo = window ? std::max<int64_t>(first + 1 - window, 0) : 0;
+                f(i, (int)r0, (int)rows, (int)(lo / kKvChunk), (int)last + 1);
+            }
+        }
+    };
+    int64_t chunks = 0;
+    walk([&](int, int, int, int c0, int end) { chunks += (end + kKvChunk - 1) / kKvChunk - c0; });
+    const int64_t quota = std::max<int64_t>(kKvLeast, (chunks * c->kv_heads + kKvGroups - 1) / kKvGroups);
+    walk([&](int i, int r0, int rows, int c0, int end) {
+        const int n = (end + kKvChunk - 1) / kKvChunk - c0, parts = (int)((n + quota - 1) / quota);
+        if (parts > 1) plan.joins.push_back(KvJoinItem{b->seg_offsets[i], rows, r0, plan.part_rows, parts});
+        for (int k = 0; k < parts; ++k) {
+            const int from = c0 + (int)((int64_t)n * k / parts), to = c0 + (int)((int64_t)n * (k + 1) / parts);
+            plan.rows.push_back(KvRowsItem{i * b->table_stride, b->seg_offsets[i], rows, b->past[i], r0, from * kKvChunk,
+                                           k + 1 < parts ? to * kKvChunk : end, parts > 1 ? plan.part_rows : -1});
+            if (parts > 1) plan.part_rows += 16;
+        }
+    });
+    return plan;
+}
+size_t part_ml_bytes(const KvPlan& plan, int kv_heads) { return align_up((size_t)plan.part_rows * kv_heads * 2 * sizeof(float), 256); }
+size_t part_bytes(const KvPlan& plan, const symb_kv_cache* c) {
+    return plan.part_rows ? part_ml_bytes(plan, c->kv_heads) + (size_t)plan.part_rows * c->kv_heads * c->head_dim * sizeof(float) : 0;
+}
+symb_status check_attention(symb_handle h, const symb_kv_batch* b, const symb_kv_cache* c, int32_t q_heads, int32_t window) {
+    const symb_status st = check_kv(h, b, c);
+    if (st != SYMB_OK) return st;
+    if (q_heads <= 0 || q_heads % c->kv_heads) return fail(h, SYMB_ERR_INVALID_ARG, "q_heads must be a positive multiple of kv_heads");
+    if (window < 0) return fail(h, SYMB_ERR_INVALID_ARG, "window is negative");
+    for (int i = 0; i < b->num_segments; ++i)
+        if ((int64_t)(b->seg_offsets[i + 1] - b->seg_offsets[i]) * (q_heads / c->kv_heads) > INT32_MAX - 1024)
+            return fail(h, SYMB_ERR_UNSUPPORTED, "segment %d has too many rows", i);
+    return SYMB_OK;
+}
+
+template <int D>
+void launch_rows(const KvAttentionParams& p, size_t items, hipStream_t s) {
+    const dim3 grid((unsigned)(items * p.kv_heads));
+    if (p.cap > 0.f) hipLaunchKernelGGL((symb_kv_rows_kernel<D, true>), grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((symb_kv_rows_kernel<D, false>), grid, dim3(256), 0, s, p);
+}
+
+}  // namespace
+
+extern "C" {
+
+symb_status symb_norm_workspace_bytes(const symb_norm_batch* b, size_t* out) {
+    return guarded(nullptr, [&]() -> symb_status {
+        if (!out) return fail(nullptr, SYMB_ERR_INVALID_ARG, "out is null");
+        symb_status st = check_norm(nullptr, b);
+        if (st != SYMB_OK) return st;
+        NormPlan plan;
+        if ((st = plan_norm(nullptr, b, plan)) != SYMB_OK) return st;
+        *out = 2 * norm_part_bytes(plan, b->width);
+        return SYMB_OK;
+    });
+}
+
+symb_status symb_norm_fwd(symb_handle h, const symb_norm_batch* b, const void* X, void* Y, void* stream) {
+    return guarded(h, [&]() -> symb_status {
+        symb_status st = check_handle(h);
+        if (st != SYMB_OK) return st;
+        CallGuard guard(h);
+        if ((st = check_norm(h, b)) != SYMB_OK) return st;
+        const int T = b->seg_offsets[b->num_segments];
+        if (!T) return SYMB_OK;
+        if (!X || !Y) return fail(h, SYMB_ERR_INVALID_ARG, "X and Y are required");
+        if (misaligned16(X) || misaligned16(Y)) return fail(h, SYMB_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+        hipStream_t s = (hipStream_t)stream;
+        const std::vector<NormDesc> nd = norm_descs(b);
+        Blob blob;
+        const size_t o_off = blob.add(b->seg_offsets, (size_t)b->num_segments + 1), o_nd = blob.add(nd.data(), nd.size());
+        unsigned char* dev = nullptr;
+        if ((st = upload(h, blob, s, &dev)) != SYMB_OK) return st;
+        const NormFwdParams p{(const bf16*)X, (bf16*)Y, (const int32_t*)(dev + o_off), (const NormDesc*)(dev + o_nd), b->num_segments, T, b->width, b->eps, b->weight_base};
+        if (b->kind == SYMB_NORM_RMS) launch_norm_fwd<true>(p, s);
+        else launch_norm_fwd<false>(p, s);
+        SYMB_HIP(h, hipGetLastError());
+        guard.completed = true;
+        return seal_slot(h);
+    });
+}
+
+symb_status symb_norm_bwd(symb_handle h, const symb_norm_batch* b, const void* X, const void* dY, void* dX, uint32_t flags, void* ws, size_t ws_bytes, void* stream) {
+    return guarded(h, [&]() -> symb_status {
+        symb_status st = check_handle(h);
+        if (st != SYMB_OK) return st;
+        CallGuard guard(h);
+        if ((st = check_norm(h, b)) != SYMB_OK) return st;
+        if (flags != SYMB_GRAD_OVERWRITE && flags != SYMB_GRAD_ACCUMULATE) return fail(h, SYMB_ERR_INVALID_ARG, "unknown flags %u", flags);
+        NormPlan plan;
+        if ((st = plan_norm(h, b, plan)) != SYMB_OK) return st;
+        const int T = b->seg_offsets[b->num_segments];
+        if (!T && (plan.groups.empty() || flags == SYMB_GRAD_ACCUMULATE)) return SYMB_OK;
+        if (T && (!X || !dY || !dX)) return fail(h, SYMB_ERR_INVALID_ARG, "X, dY and dX are required");
+        if (misaligned16(X) || misaligned16(dY) || misaligned16(dX) || misaligned16(ws)) return fail(h, SYMB_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+        const size_t part = norm_part_bytes(plan, b->width);
+        if (2 * part > ws_bytes || (part && !ws)) return fail(h, SYMB_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : 0, 2 * part);
+        if (plan.groups.size() > 65535) return fail(h, SYMB_ERR_UNSUPPORTED, "%zu different weight gradients: 65535 at most", plan.groups.size());
+        hipStream_t s = (hipStream_t)stream;
+        const std::vector<NormDesc> nd = norm_descs(b);
+        Blob blob;
+        const size_t o_nd = blob.add(nd.data(), nd.size()), o_ch = blob.add(plan.chunks.data(), plan.chunks.size()), o_gr = blob.add(plan.groups.data(), plan.groups.size());
+        unsigned char* dev = nullptr;
+        if ((st = upload(h, blob, s, &dev)) != SYMB_OK) return st;
+        float *part_w = (float*)ws, *part_b = (float*)((unsigned char*)ws + part);
+        if (T) {
+            const NormBwdParams p{(const bf16*)X, (const bf16*)dY, (bf16*)dX, (const NormDesc*)(dev + o_nd), (const NormChunk*)(dev + o_ch), part_w, part_b, b->width, b->eps, b->weight_base};
+            if (b->kind == SYMB_NORM_RMS) launch_norm_bwd<true>(p, (int)plan.chunks.size(), s);
+            else launch_norm_bwd<false>(p, (int)plan.chunks.size(), s);
+            SYMB_HIP(h, hipGetLastError());
+        }
+        if (!plan.groups.empty()) {
+            const NormReduceParams p{part_w, part_b, (const NormGroup*)(dev + o_gr), b->width, flags == SYMB_GRAD_ACCUMULATE};
+            hipLaunchKernelGGL(symb_norm_reduce_kernel, dim3((b->width + 255) / 256, (unsigned)plan.groups.size()), dim3(256), 0, s, p);
+            SYMB_HIP(h, hipGetLastError());
+        }
+        guard.completed = true;
+        return seal_slot(h);
+    });
+}
+
+symb_status symb_kv_append(symb_handle h, const symb_kv_batch* b, const symb_kv_cache* cache, const symb_rotation* rotation, const void* q, int64_t q_stride, int32_t q_heads,
+                           void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* stream) {
+    return guarded(h, [&]() -> symb_status {
+        symb_status st = check_handle(h);
+        if (st != SYMB_OK) return st;
+        CallGuard guard(h);
+        if ((st = check_kv(h, b, cache)) != SYMB_OK) return st;
+        if (q_heads < 0) return fail(h, SYMB_ERR_INVALID_ARG, "q_heads is negative");
+        const int S = b->num_segments, P = cache->page_tokens, D = cache->head_dim;
+        int64_t most = 0;
+        for (int i = 0; i < S; ++i)
+            if (b->seg_offsets[i + 1] > b->seg_offsets[i]) most = std::max<int64_t>(most, (int64_t)b->past[i] + b->seg_offsets[i + 1] - b->seg_offsets[i]);
+        if (rotation) {
+            if (rotation->dim <= 0 || rotation->dim % 16 || rotation->dim > D) return fail(h, SYMB_ERR_INVALID_ARG, "rotation of %d elements: a multiple of 16, at most head_dim", rotation->dim);
+            if (rotation->pairs != SYMB_ROTATE_HALVES && rotation->pairs != SYMB_ROTATE_ADJACENT) return fail(h, SYMB_ERR_INVALID_ARG, "unknown pairing %d", rotation->pairs);
+            if (rotation->positions < most) return fail(h, SYMB_ERR_INVALID_ARG, "rotation table of %d positions, %lld needed", rotation->positions, (long long)most);
+        }
+        if (b->seg_offsets[S] == 0) return SYMB_OK;
+        if ((q_heads > 0) != (q != nullptr)) return fail(h, SYMB_ERR_INVALID_ARG, "q_heads is %d and q is %s", q_heads, q ? "given" : "null");
+        if ((st = check_kv_pointers(h, b, cache)) != SYMB_OK) return st;
+        if (rotation && (!rotation->table || misaligned16(rotation->table))) return fail(h, SYMB_ERR_INVALID_ARG, "rotation table is null or not 16-byte aligned");
+        if ((st = check_rows(h, k, k_stride, (int64_t)cache->kv_heads * D, "k")) != SYMB_OK) return st;
+        if ((st = check_rows(h, v, v_stride, (int64_t)cache->kv_heads * D, "v")) != SYMB_OK) return st;
+        if (q && (st = check_rows(h, q, q_stride, (int64_t)q_heads * D, "q")) != SYMB_OK) return st;
+        if (q && (st = check_rows(h, q_out, q_out_stride, (int64_t)q_heads * D, "q_out")) != SYMB_OK) return st;
+        std::vector<KvPage> pages;
+        int rows = 0;
+        for (int i = 0; i < S; ++i)
+            for (int64_t at = 0, n = b->seg_offsets[i + 1] - b->seg_offsets[i]; at < n;) {
+                const int64_t pos = b->past[i] + at, take = std::min(n - at, P - pos % P);
+                pages.push_back(KvPage{(int32_t)((int64_t)i * b->table_stride + pos / P), (int32_t)(b->seg_offsets[i] + at), (int32_t)take, (int32_t)pos});
+                rows = std::max(rows, (int)take);
+                at += take;
+            }
+        const bool few = rows <= kKvFewRows;
+        const int heads_q = std::max(1, (few ? 64 : 256) / (rows * (D / 16)));
+        const int64_t ny = 2 * (int64_t)cache->kv_heads + (q_heads + heads_q - 1) / heads_q;
+        if (ny > 65535) return fail(h, SYMB_ERR_UNSUPPORTED, "%d query heads beside %d key heads", q_heads, cache->kv_heads);
+        hipStream_t s = (hipStream_t)stream;
+        Blob blob;
+        const size_t o_pg = blob.add(pages.data(), pages.size());
+        unsigned char* dev = nullptr;
+        if ((st = upload(h, blob, s, &dev)) != SYMB_OK) return st;
+        KvAppendParams p{};
+        p.pages = (const KvPage*)(dev + o_pg);
+        p.page_table = b->page_table;
+        p.k = (unsigned char*)cache->k;
+        p.v = (unsigned char*)cache->v;
+        p.k_scale = (unsigned char*)cache->k_scale;
+        p.v_scale = (unsigned char*)cache->v_scale;
+        p.rotation = rotation ? (const float*)rotation->table : nullptr;
+        p.q_in = (const bf16*)q;
+        p.q_out = (bf16*)q_out;
+        p.k_in = (const bf16*)k;
+        p.v_in = (const bf16*)v;
+        p.q_stride = q_stride;
+        p.q_out_stride = q_out_stride;
+        p.k_stride = k_stride;
+        p.v_stride = v_stride;
+        p.num_pages = cache->num_pages;
+        p.kv_heads = cache->kv_heads;
+        p.q_heads = q_heads;
+        p.page_shift = page_shift(cache);
+        p.turned = rotation ? rotation->dim : 0;
+        p.adjacent = rotation && rotation->pairs == SYMB_ROTATE_ADJACENT;
+        p.heads_q = heads_q;
+        if (D == 128) launch_append<128>(p, (int)pages.size(), few, (int)ny, s);
+        else launch_append<64>(p, (int)pages.size(), few, (int)ny, s);
+        SYMB_HIP(h, hipGetLastError());
+        guard.completed = true;
+        return seal_slot(h);
+    });
+}
+
+symb_status symb_kv_workspace_bytes(const symb_kv_batch* b, const symb_kv_cache* cache, int32_t q_heads, int32_t window, size_t* out) {
+    return guarded(nullptr, [&]() -> symb_status {
+        if (!out) return fail(nullptr, SYMB_ERR_INVALID_ARG, "out is null");
+        const symb_status st = check_attention(nullptr, b, cache, q_heads, window);
+        if (st != SYMB_OK) return st;
+        *out = part_bytes(plan_attention(b, cache, q_heads, window), cache);
+        return SYMB_OK;
+    });
+}
+
+symb_status symb_kv_attention(symb_handle h, const symb_kv_batch* b, const symb_kv_cache* cache, const void* q, int64_t q_stride, int32_t q_heads, void* out, int64_t out_stride,
+                              float scale, int32_t window, float cap, void* ws, size_t ws_bytes, void* stream) {
+    return guarded(h, [&]() -> symb_status {
+        symb_status st = check_handle(h);
+        if (st != SYMB_OK) return st;
+        CallGuard guard(h);
+        if ((st = check_attention(h, b, cache, q_heads, window)) != SYMB_OK) return st;
+        if (!(scale > 0.f) || !std::isfinite(scale)) return fail(h, SYMB_ERR_INVALID_ARG, "scale must be positive and finite");
+        if (!(cap >= 0.f) || !std::isfinite(cap)) return fail(h, SYMB_ERR_INVALID_ARG, "cap must be finite and not negative");
+        if (b->seg_offsets[b->num_segments] == 0) return SYMB_OK;
+        if ((st = check_kv_pointers(h, b, cache)) != SYMB_OK) return st;
+        const int D = cache->head_dim;
+        if ((st = check_rows(h, q, q_stride, (int64_t)q_heads * D, "q")) != SYMB_OK) return st;
+        if ((st = check_rows(h, out, out_stride, (int64_t)q_heads * D, "out")) != SYMB_OK) return st;
+        const KvPlan plan = plan_attention(b, cache, q_heads, window);
+        const size_t need = part_bytes(plan, cache);
+        if (need && (!ws || ws_bytes < need)) return fail(h, SYMB_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : 0, need);
+        if (need && misaligned16(ws)) return fail(h, SYMB_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
+        if ((int64_t)plan.rows.size() * cache->kv_heads > INT32_MAX) return fail(h, SYMB_ERR_UNSUPPORTED, "%zu work items of %d key heads", plan.rows.size(), cache->kv_heads);
+        hipStream_t s = (hipStream_t)stream;
+        Blob blob;
+        const size_t o_rows = blob.add(plan.rows.data(), plan.rows.size()), o_join = blob.add(plan.joins.data(), plan.joins.size());
+        unsigned char* dev = nullptr;
+        if ((st = upload(h, blob, s, &dev)) != SYMB_OK) return st;
+        constexpr float kLog2e = 1.442695041f;
+        KvAttentionParams p{};
+        p.items = (const KvRowsItem*)(dev + o_rows);
+        p.page_table = b->page_table;
+        p.k = (const unsigned char*)cache->k;
+        p.v = (const unsigned char*)cache->v;
+        p.k_scale = (const unsigned char*)cache->k_scale;
+        p.v_scale = (const unsigned char*)cache->v_scale;
+        p.q = (const bf16*)q;
+        p.out = (bf16*)out;
+        p.part_ml = (float*)ws;
+        p.part_o = (float*)((unsigned char*)ws + part_ml_bytes(plan, cache->kv_heads));
+        p.q_stride = q_stride;
+        p.out_stride = out_stride;
+        p.num_pages = cache->num_pages;
+        p.kv_heads = cache->kv_heads;
+        p.group = q_heads / cache->kv_heads;
+        p.page_shift = page_shift(cache);
+        p.window = window;
+        p.part_rows = plan.part_rows;
+        p.scale = cap > 0.f ? scale / cap : scale * kLog2e;
+        p.cap = cap * kLog2e;
+        if (D == 128) launch_rows<128>(p, plan.rows.size(), s);
+        else launch_rows<64>(p, plan.rows.size(), s);
+        SYMB_HIP(h, hipGetLastError());
+        if (!plan.joins.empty()) {
+            const KvJoinParams jp{(const KvJoinItem*)(dev + o_join), p.part_o, p.part_ml, p.out, out_stride, p.kv_heads, p.group, p.part_rows};
+            const dim3 grid((unsigned)(plan.joins.size() * p.kv_heads));
+            if (D == 128) hipLaunchKernelGGL((symb_kv_join_kernel<128>), grid, dim3(256), 0, s, jp);
+            else hipLaunchKernelGGL((symb_kv_join_kernel<64>), grid, dim3(256), 0, s, jp);
+            SYMB_HIP(h, hipGetLastError());
+        }
+        guard.completed = true;
+        return seal_slot(h);
+    });
+}
+
+}  // extern "C"
