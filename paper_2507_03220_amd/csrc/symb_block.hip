@@ -185,37 +185,48 @@ void launch_append(const KvAppendParams& p, int pages, bool few, int ny, hipStre
 // The work of one attention call.
 struct KvPlan {
     std::vector<KvRowsItem> rows;
+    std::vector<KvTileItem> tiles;
     std::vector<KvJoinItem> joins;
-    int part_rows = 0;                    // rows of partial results, of one key head
+    int64_t part_rows = 0;                // rows of partial results, of one key head
 };
-// Chunks of 128 tokens that a workgroup takes: its four wavefronts two each at least (a shorter run costs more in joining than it gains), and as many as leave kKvGroups workgroups.
-constexpr int kKvGroups = 1024, kKvLeast = 8;
+// Segments of up to kKvFew rows for a key head go to the kernel of 16-row items, others to the tiles of 128 rows.
+constexpr int kKvFew = 32;
+// Workgroups that a launch should have, and chunks (128 tokens for 16 rows, 64 for a tile) that one of them takes at least: a shorter run costs more in joining than it gains.
+constexpr int kKvGroups = 1024, kKvLeast = 8, kKvTileGroups = 512, kKvTileLeast = 16;
 KvPlan plan_attention(const symb_kv_batch* b, const symb_kv_cache* c, int q_heads, int window) {
     KvPlan plan;
     const int group = q_heads / c->kv_heads;
-    auto walk = [&](auto&& f) {                       // f(segment, first row, its rows, first chunk, end)
+    // f(segment, its rows, first row, first chunk, chunks, last token + 1) for runs of `step` rows
+    auto walk = [&](bool few, int step, int chunk, auto&& f) {
         for (int i = 0; i < b->num_segments; ++i) {
             const int64_t rows = (int64_t)(b->seg_offsets[i + 1] - b->seg_offsets[i]) * group;
-            for (int64_t r0 = 0; r0 < rows; r0 += 16) {
-                const int64_t first = b->past[i] + r0 / group, last = b->past[i] + std::min(r0 + 15, rows - 1) / group;
-                const int64_t lo = window ? std::max<int64_t>(first + 1 - window, 0) : 0;
-                f(i, (int)r0, (int)rows, (int)(lo / kKvChunk), (int)last + 1);
+            if ((rows <= kKvFew) != few) continue;
+            for (int64_t r0 = 0; r0 < rows; r0 += step) {
+                const int64_t first = b->past[i] + r0 / group, last = b->past[i] + std::min(r0 + step - 1, rows - 1) / group;
+                const int64_t lo = window ? std::max<int64_t>(first + 1 - window, 0) : 0, c0 = lo / chunk;
+                f(i, (int)rows, (int)r0, (int)c0, (int)((last + chunk) / chunk - c0), (int)last + 1);
             }
         }
     };
-    int64_t chunks = 0;
-    walk([&](int, int, int, int c0, int end) { chunks += (end + kKvChunk - 1) / kKvChunk - c0; });
-    const int64_t quota = std::max<int64_t>(kKvLeast, (chunks * c->kv_heads + kKvGroups - 1) / kKvGroups);
-    walk([&](int i, int r0, int rows, int c0, int end) {
-        const int n = (end + kKvChunk - 1) / kKvChunk - c0, parts = (int)((n + quota - 1) / quota);
-        if (parts > 1) plan.joins.push_back(KvJoinItem{b->seg_offsets[i], rows, r0, plan.part_rows, parts});
-        for (int k = 0; k < parts; ++k) {
-            const int from = c0 + (int)((int64_t)n * k / parts), to = c0 + (int)((int64_t)n * (k + 1) / parts);
-            plan.rows.push_back(KvRowsItem{i * b->table_stride, b->seg_offsets[i], rows, b->past[i], r0, from * kKvChunk,
-                                           k + 1 < parts ? to * kKvChunk : end, parts > 1 ? plan.part_rows : -1});
-            if (parts > 1) plan.part_rows += 16;
-        }
-    });
+    auto fill = [&](bool few, int step, int chunk, int groups, int least, auto& items) {
+        int64_t chunks = 0;
+        walk(few, step, chunk, [&](int, int, int, int, int n, int) { chunks += n; });
+        const int64_t quota = std::max<int64_t>(least, (chunks * c->kv_heads + groups - 1) / groups);
+        walk(few, step, chunk, [&](int i, int rows, int r0, int c0, int n, int end) {
+            const int parts = (int)((n + quota - 1) / quota);
+            if (parts > 1)
+                for (int r = r0; r < std::min(r0 + step, rows); r += 16) plan.joins.push_back(KvJoinItem{b->seg_offsets[i], rows, r, (int32_t)(plan.part_rows + r - r0), parts, step});
+            for (int k = 0; k < parts; ++k) {
+                const int from = c0 + (int)((int64_t)n * k / parts), to = c0 + (int)((int64_t)n * (k + 1) / parts);
+                items.push_back({i * b->table_stride, b->seg_offsets[i], rows, b->past[i], r0, from * chunk, k + 1 < parts ? to * chunk : end, parts > 1 ? (int32_t)plan.part_rows : -1});
+                if (parts > 1) plan.part_rows += step;
+            }
+        });
+        // the longest first: what is left over at the end is short
+        std::stable_sort(items.begin(), items.end(), [](const auto& x, const auto& y) { return x.end - x.begin > y.end - y.begin; });
+    };
+    fill(true, 16, kKvChunk, kKvGroups, kKvLeast, plan.rows);
+    fill(false, kKvTileRows, kKvTileChunk, kKvTileGroups, kKvTileLeast, plan.tiles);
     return plan;
 }
 size_t part_ml_bytes(const KvPlan& plan, int kv_heads) { return align_up((size_t)plan.part_rows * kv_heads * 2 * sizeof(float), 256); }
@@ -233,11 +244,23 @@ symb_status check_attention(symb_handle h, const symb_kv_batch* b, const symb_kv
     return SYMB_OK;
 }
 
-template <int D>
-void launch_rows(const KvAttentionParams& p, size_t items, hipStream_t s) {
-    const dim3 grid((unsigned)(items * p.kv_heads));
-    if (p.cap > 0.f) hipLaunchKernelGGL((symb_kv_rows_kernel<D, true>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((symb_kv_rows_kernel<D, false>), grid, dim3(256), 0, s, p);
+template <int D, bool CAP>
+symb_status launch_attention(symb_handle h, KvAttentionParams p, const KvPlan& plan, const unsigned char* rows, const unsigned char* tiles, const KvJoinParams& jp, hipStream_t s) {
+    if (!plan.tiles.empty()) {
+        p.items = tiles;
+        hipLaunchKernelGGL((symb_kv_tile_kernel<D, CAP>), dim3((unsigned)(plan.tiles.size() * p.kv_heads)), dim3(256), 0, s, p);
+        SYMB_HIP(h, hipGetLastError());
+    }
+    if (!plan.rows.empty()) {
+        p.items = rows;
+        hipLaunchKernelGGL((symb_kv_rows_kernel<D, CAP>), dim3((unsigned)(plan.rows.size() * p.kv_heads)), dim3(256), 0, s, p);
+        SYMB_HIP(h, hipGetLastError());
+    }
+    if (!plan.joins.empty()) {
+        hipLaunchKernelGGL((symb_kv_join_kernel<D>), dim3((unsigned)(plan.joins.size() * p.kv_heads)), dim3(256), 0, s, jp);
+        SYMB_HIP(h, hipGetLastError());
+    }
+    return SYMB_OK;
 }
 
 }  // namespace
@@ -422,15 +445,15 @@ symb_status symb_kv_attention(symb_handle h, const symb_kv_batch* b, const symb_
         const size_t need = part_bytes(plan, cache);
         if (need && (!ws || ws_bytes < need)) return fail(h, SYMB_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : 0, need);
         if (need && misaligned16(ws)) return fail(h, SYMB_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
-        if ((int64_t)plan.rows.size() * cache->kv_heads > INT32_MAX) return fail(h, SYMB_ERR_UNSUPPORTED, "%zu work items of %d key heads", plan.rows.size(), cache->kv_heads);
+        if ((int64_t)(plan.rows.size() + plan.tiles.size() + plan.joins.size()) * cache->kv_heads > INT32_MAX || plan.part_rows > INT32_MAX)
+            return fail(h, SYMB_ERR_UNSUPPORTED, "%zu work items of %d key heads", plan.rows.size() + plan.tiles.size(), cache->kv_heads);
         hipStream_t s = (hipStream_t)stream;
         Blob blob;
-        const size_t o_rows = blob.add(plan.rows.data(), plan.rows.size()), o_join = blob.add(plan.joins.data(), plan.joins.size());
+        const size_t o_rows = blob.add(plan.rows.data(), plan.rows.size()), o_tiles = blob.add(plan.tiles.data(), plan.tiles.size()), o_join = blob.add(plan.joins.data(), plan.joins.size());
         unsigned char* dev = nullptr;
         if ((st = upload(h, blob, s, &dev)) != SYMB_OK) return st;
         constexpr float kLog2e = 1.442695041f;
         KvAttentionParams p{};
-        p.items = (const KvRowsItem*)(dev + o_rows);
         p.page_table = b->page_table;
         p.k = (const unsigned char*)cache->k;
         p.v = (const unsigned char*)cache->v;
@@ -447,19 +470,13 @@ symb_status symb_kv_attention(symb_handle h, const symb_kv_batch* b, const symb_
         p.group = q_heads / cache->kv_heads;
         p.page_shift = page_shift(cache);
         p.window = window;
-        p.part_rows = plan.part_rows;
+        p.part_rows = (int32_t)plan.part_rows;
         p.scale = cap > 0.f ? scale / cap : scale * kLog2e;
         p.cap = cap * kLog2e;
-        if (D == 128) launch_rows<128>(p, plan.rows.size(), s);
-        else launch_rows<64>(p, plan.rows.size(), s);
-        SYMB_HIP(h, hipGetLastError());
-        if (!plan.joins.empty()) {
-            const KvJoinParams jp{(const KvJoinItem*)(dev + o_join), p.part_o, p.part_ml, p.out, out_stride, p.kv_heads, p.group, p.part_rows};
-            const dim3 grid((unsigned)(plan.joins.size() * p.kv_heads));
-            if (D == 128) hipLaunchKernelGGL((symb_kv_join_kernel<128>), grid, dim3(256), 0, s, jp);
-            else hipLaunchKernelGGL((symb_kv_join_kernel<64>), grid, dim3(256), 0, s, jp);
-            SYMB_HIP(h, hipGetLastError());
-        }
+        const KvJoinParams jp{(const KvJoinItem*)(dev + o_join), p.part_o, p.part_ml, p.out, out_stride, p.kv_heads, p.group, p.part_rows};
+        st = D == 128 ? (cap > 0.f ? launch_attention<128, true>(h, p, plan, dev + o_rows, dev + o_tiles, jp, s) : launch_attention<128, false>(h, p, plan, dev + o_rows, dev + o_tiles, jp, s))
+                      : (cap > 0.f ? launch_attention<64, true>(h, p, plan, dev + o_rows, dev + o_tiles, jp, s) : launch_attention<64, false>(h, p, plan, dev + o_rows, dev + o_tiles, jp, s));
+        if (st != SYMB_OK) return st;
         guard.completed = true;
         return seal_slot(h);
     });
