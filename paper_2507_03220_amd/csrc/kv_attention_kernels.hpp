@@ -4,21 +4,16 @@
 //
 // computed in one pass over the tokens: m, the sum and the unnormalised output are kept in fp32 and scaled when m grows.
 //
-// Both products run on v_mfma_scale_f32_16x16x128_f8f6f4 with the cache's bytes as they lie, E8M0 scales included: nothing is widened, and a page's scale
-// costs no instruction.  A bf16 query has eight significant bits, two E4M3 terms: q = (hi + lo / 16) 2^e exactly for elements within 2^-14 of the row's largest
-// (others to 2^-18 of it), one product each.  The weights 2^(l x - m) enter the second product the same way, with nine significant bits, one more than a
-// bf16 weight has.  Two products at twice bf16's rate cost what one bf16 product would, and the widening of keys and values (two instructions for
-// every four bytes and 16 rows) falls away.  Inside one instruction, the matrix unit drops what lies more than about 2^-15 below its largest product: measured
-// relative errors of 1e-5 to 5e-5 of a sum, not growing with the number of instructions (the accumulator is full fp32), a hundredth of the output's rounding.
+// Scores: v_mfma_scale_f32_*_f8f6f4 takes the keys' bytes as they lie and their page's E8M0 scale beside them, so no key is widened.  A bf16 query has eight significant bits,
+// two E4M3 terms: q = (hi + lo / 16) 2^e exactly for elements within 2^-14 of the row's largest (others to 2^-18 of it), one product each, which at twice
+// bf16's rate is what a bf16 product would cost.  Inside one instruction the matrix unit drops what lies more than about 2^-15 below its largest product: measured
+// relative errors of 1e-5 to 5e-5 of a sum, not growing with the number of instructions (the accumulator is full fp32).
+// Outputs: weights as bf16 (2^-9 of each; their sum is taken before they are rounded), values widened to bf16, exactly, scale included (v_cvt_scalef32_pk_bf16_fp8: two
+// elements in 4 clocks).  The weights as two E4M3 terms would spare that, but v_cvt_pk_fp8_f32 takes 16 clocks for two elements: 22 clocks a weight against 2,
+// and the widening is done once for many rows.
 //
-// The scores are formed as K Q^T, tokens down the rows of the result: a lane then holds 32 tokens of ONE query row, in the order in which the
+// The scores are formed as K Q^T, tokens down the rows of the result: a lane then holds tokens of ONE query row, in the order in which the
 // instruction wants them as the right operand of V^T P^T.  No score crosses lanes but for the row's maximum and sum, and none goes through shared memory.
-// In a chunk of 128 tokens, lane (n = lane % 16, g = lane / 16) gives
-//   left operand, keys    tile s (0..7): token kv_token(s, n), elements 16g .. 16g+15 and (head of 128) 64+16g ..
-//   right operand         query row n, the same elements
-//   result                tokens kv_token(s, 4g + r), r = 0..3, of row n: with s = 0..3 the tokens 16g .. 16g+15, with s = 4..7 64+16g ..
-//   left operand, values  channel 16j + n, tokens 16g .. 16g+15 and 64+16g .., 16 bytes each as they lie in the cache
-//   scales                of the 32 elements (tokens) 32g .. 32g+31 of row (channel) n
 #pragma once
 #include <type_traits>
 
@@ -26,20 +21,29 @@
 
 namespace symb {
 
+// ---- up to 48 rows ----------------------------------------------------------------------------------------------------------------
+// In a chunk of 128 tokens, lane (n = lane % 16, g = lane / 16) gives
+//   left operand, keys    tile s (0..7): token kv_token(s, n), elements 16g .. 16g+15 and (head of 128) 64+16g .., its page's scale
+//   right operand         query row n, the same elements
+//   result                tokens kv_token(s, 4g + r), r = 0..3, of row n: with s = 0..3 the tokens 16g .. 16g+15, with s = 4..7 64+16g ..
+//   left operand, values  channel 16j + n, step q (0..3): tokens 64(q/2) + 16g + 8(q%2) .. +7, half of 16 bytes as they lie in the cache
 constexpr int kKvChunk = 128;             // tokens
+// A row's weights are 2^(x - m) with an m that its largest x may exceed by up to this: the outputs need not be scaled whenever a larger score comes.  bf16 and fp32 hold the
+// weights just as well.
+constexpr float kKvSlack = 8.f;
 
-// A run of tokens for up to 16 query rows of one key head.  Row r of a segment's key head is query head r % group of token r / group.
-struct KvRowsItem {
+// A run of tokens for some of the query rows of one key head.  Row r of a segment's key head is query head r % group of token r / group.
+struct KvItem {
     int32_t table;                        // the segment's first entry in the page table
     int32_t row0, rows;                   // its first row in the batch; its rows times the query heads of a key head
     int32_t past;
     int32_t r0;                           // the item's first row
-    int32_t begin, end;                   // tokens: a multiple of 128; one past the last that any of the rows sees
+    int32_t begin, end;                   // tokens: a multiple of the chunk; one past the last that any of the rows sees
     int32_t part;                         // partial result's first row, -1: the item is all there is
 };
 
 struct KvAttentionParams {
-    const void* items;                    // KvRowsItem or KvTileItem
+    const KvItem* items;
     const int32_t* page_table;
     const unsigned char* k;
     const unsigned char* v;
@@ -114,6 +118,13 @@ __device__ __forceinline__ floatx4 kv_mfma(const intx8& a, const intx8& b, const
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, sa, 0, sb);
 }
 
+// Behind the last matrix instruction of a loop, before its results are read in other code: the 19 wait states that the longest of them needs.
+__device__ __forceinline__ void kv_settle() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 15\n\ts_nop 3");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // A score in log2 units.
 template <bool CAP>
 __device__ __forceinline__ float kv_score(const KvAttentionParams& p, float s) {
@@ -123,259 +134,267 @@ __device__ __forceinline__ float kv_score(const KvAttentionParams& p, float s) {
     return p.cap * (1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * 2.885390082f) + 1.f));
 }
 
-// The pages of a chunk as one lane needs them.  Only pages of the tokens lo .. hi-1 are looked up (others are hidden: any page will do); a number outside
-// the pool is reported, and page 0 read in its place.
-struct KvChunk {
-    int kpage[2], vpage[2];               // of tile s: kpage[s / 4]; of the value tokens 16g and 64+16g
-    int kscale[2], vscale;
-};
+// The page of a token.  Only pages of the tokens lo .. hi-1 are looked up (others are hidden: any page will do); a number outside the pool is reported, and page 0
+// read in its place.
 __device__ __forceinline__ int kv_page(const KvAttentionParams& p, int table, int token, int lo, int hi, bool& bad) {
     const int page = p.page_table[table + (max(min(token, hi - 1), lo) >> p.page_shift)];
     const bool in = (unsigned)page < (unsigned)p.num_pages;
     bad |= !in;
     return in ? page : 0;
 }
-__device__ __forceinline__ void kv_pages(KvChunk& c, const KvAttentionParams& p, int table, int t0, int lo, int hi, int n, int g, bool& bad) {
-    int pg[4];                                                     // the same in all lanes
-#pragma unroll
-    for (int i = 0; i < 4; ++i) pg[i] = kv_page(p, table, t0 + 32 * i, lo, hi, bad);
-    c.kpage[0] = n & 8 ? pg[1] : pg[0];
-    c.kpage[1] = n & 8 ? pg[3] : pg[2];
-    c.vpage[0] = g & 2 ? pg[1] : pg[0];
-    c.vpage[1] = g & 2 ? pg[3] : pg[2];
-    c.vscale = g & 2 ? (g & 1 ? pg[3] : pg[2]) : (g & 1 ? pg[1] : pg[0]);
+__device__ __forceinline__ float kv_scale(int byte) { return as_float(byte << 23); }
+// Eight E4M3 values times a power of two as bf16.
+__device__ __forceinline__ bf16x8 kv_widen(int a, int b, float scale) {
+    typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+    const bf16x2 w[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true)};
+    return bf16x8{w[0][0], w[0][1], w[1][0], w[1][1], w[2][0], w[2][1], w[3][0], w[3][1]};
+}
+__device__ __forceinline__ bf16x8 kv_pack8(float a, float b, float c, float d, float e, float f, float g, float h) {
+    return __builtin_bit_cast(bf16x8, intx4{(int)pack2_bf16(a, b), (int)pack2_bf16(c, d), (int)pack2_bf16(e, f), (int)pack2_bf16(g, h)});
 }
 
-// The value operand of one channel with the bytes outside [lo, hi) cleared: what a hidden token holds must not meet a weight, 0 x NaN being NaN.
-__device__ __forceinline__ int kv_keep(int w, int t, int lo, int hi) {     // bytes t .. t+3
+// What a hidden token holds must not meet a weight, 0 x NaN being NaN.  Where not every row sees every token, values of tokens that no row sees (outside lo .. hi-1) are cleared, and so
+// are NaN, infinities with them, among the others; if there are any, the rows that see them get them in a pass of its own: ones in their places times ones where a row sees the token.
+__device__ __forceinline__ int kv_keep_bytes(int t, int lo, int hi) {      // of four tokens' bytes, t .. t+3: ones where a token is in lo .. hi-1
     const int a = lo - t, b = hi - t;
     const unsigned below = b >= 4 ? ~0u : b > 0 ? (1u << (8 * b)) - 1 : 0u;
     const unsigned above = a <= 0 ? ~0u : a < 4 ? ~0u << (8 * a) : 0u;
-    return (int)((unsigned)w & below & above);
+    return (int)(below & above);
 }
-
-// 0x80 in the place of each byte that is NaN.
-__device__ __forceinline__ unsigned kv_nan_bytes(int w) { return (((unsigned)w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
-
-// Four wavefronts share an item's tokens, chunk by chunk, and join through shared memory.  Keys and values go straight from memory into the operands' registers: a
-// wavefront has up to 32 KB on their way, keys of the next chunk asked for as soon as the scores of this one are formed.
-template <int D, bool CAP>
-SYMB_KERNEL __launch_bounds__(256, D == 64 ? 2 : 1) void symb_kv_rows_kernel(KvAttentionParams p) {
+// 0xff in the place of each E4M3 byte that is NaN, or (at a scale of 2^120) 256 or more: 2^128.
+__device__ __forceinline__ int kv_nan_bytes(int w, int scale_byte) {
+    const unsigned top = (((unsigned)w & 0x7f7f7f7fu) + (scale_byte >= 247 ? 0x08080808u : 0x01010101u)) & 0x80808080u;
+    return (int)((top >> 7) * 255u);
+}
+// Four wavefronts share an item's tokens, chunk by chunk, each for all of its R x 16 rows, and join through shared memory.  Keys and values go straight from memory into
+// registers: a wavefront has up to 32 KB on their way, keys of the next chunk asked for as soon as the scores of this one are formed.
+template <int D, int R, bool CAP>
+SYMB_KERNEL __launch_bounds__(256, R == 1 ? 2 : 1) void symb_kv_rows_kernel(KvAttentionParams p) {
     constexpr int kTiles = D / 16, kWords = D / 64;
     __shared__ float join[4][16][D + 4];
-    __shared__ float stat[4][16][2];
-    const KvRowsItem it = ((const KvRowsItem*)p.items)[blockIdx.x / p.kv_heads];
+    __shared__ float stat[R][4][16][2];
+    const KvItem it = p.items[blockIdx.x / p.kv_heads];
     const int h = blockIdx.x % p.kv_heads;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-    const int r = it.r0 + n, pos = it.past + r / p.group;
-    const bool valid = r < it.rows;
-    const int see_hi = valid ? pos + 1 : 0, see_lo = p.window ? max(pos + 1 - p.window, 0) : 0;       // tokens this lane's row sees
-    // tokens that every row of the item sees, and those that some row does
-    const int last = min(it.r0 + 15, it.rows - 1);
+    // tokens that this lane's rows see; those that every row of the item sees, and those that some row does
+    int see_hi[R], see_lo[R];
+    const int last = min(it.r0 + 16 * R - 1, it.rows - 1);
     const int all_hi = it.past + it.r0 / p.group + 1, all_lo = p.window ? max(it.past + last / p.group + 1 - p.window, 0) : 0;
     const int any_hi = it.past + last / p.group + 1, any_lo = p.window ? max(all_hi - p.window, 0) : 0;
-    KvQuery<D> q;
-    kv_query<D>(q, p.q + (int64_t)(it.row0 + r / p.group) * p.q_stride + (h * p.group + r % p.group) * D, valid, g);
+    KvQuery<D> q[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int row = it.r0 + 16 * r + n, pos = it.past + row / p.group;
+        const bool valid = row < it.rows;
+        see_hi[r] = valid ? pos + 1 : 0;
+        see_lo[r] = p.window ? max(pos + 1 - p.window, 0) : 0;
+        kv_query<D>(q[r], p.q + (int64_t)(it.row0 + row / p.group) * p.q_stride + (h * p.group + row % p.group) * D, valid, g);
+    }
     bool bad = false;
-    floatx4 o[kTiles];
+    floatx4 o[R][kTiles];
+    float m[R], l[R];
 #pragma unroll
-    for (int j = 0; j < kTiles; ++j) o[j] = floatx4{0, 0, 0, 0};
-    float m = -INFINITY, l = 0.f;
-    intx4 kb[8][kWords];
-    const int P = 1 << p.page_shift;
-    KvChunk c;
-    auto ask_keys = [&](int t0) {
-        kv_pages(c, p, it.table, t0, any_lo, it.end, n, g, bad);
+    for (int r = 0; r < R; ++r) {
+        m[r] = -INFINITY;
+        l[r] = 0.f;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int64_t block = (int64_t)c.kpage[u] * p.kv_heads + h;
-            const unsigned char* at = p.k + (block << p.page_shift) * D + 16 * g;
-            c.kscale[u] = p.k_scale[block];
+        for (int j = 0; j < kTiles; ++j) o[r][j] = floatx4{0, 0, 0, 0};
+    }
+    const int in_page = (1 << p.page_shift) - 1;
+    for (int t0 = it.begin + wave * kKvChunk; t0 < it.end; t0 += 4 * kKvChunk) {
+        intx4 kb[8][kWords], vb[kTiles][2];
+        int kscale[2], vscale[2];
+        {
+            int kpage[2], vpage[2];
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const unsigned char* row = at + ((t0 + kv_token(4 * u + s, n)) & (P - 1)) * D;
+            for (int u = 0; u < 2; ++u) {
+                const int first = kv_page(p, it.table, t0 + 64 * u, any_lo, it.end, bad), second = kv_page(p, it.table, t0 + 64 * u + 32, any_lo, it.end, bad);     // (the same in all lanes)
+                kpage[u] = n & 8 ? second : first;
+                vpage[u] = g & 2 ? second : first;
+            }
 #pragma unroll
-                for (int w = 0; w < kWords; ++w) kb[4 * u + s][w] = *(const intx4*)(row + 64 * w);
+            for (int u = 0; u < 2; ++u) {
+                const int64_t block = (int64_t)kpage[u] * p.kv_heads + h;
+                const unsigned char* at = p.k + ((block << p.page_shift) + ((t0 + kv_token(4 * u, n)) & in_page)) * D + 16 * g;
+                kscale[u] = p.k_scale[block];
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+#pragma unroll
+                    for (int w = 0; w < kWords; ++w) kb[4 * u + s][w] = *(const intx4*)(at + 4 * s * D + 64 * w);
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int64_t block = (int64_t)vpage[u] * p.kv_heads + h;
+                const unsigned char* at = p.v + ((block * D + n) << p.page_shift) + ((t0 + 64 * u + 16 * g) & in_page);
+                vscale[u] = p.v_scale[block];
+#pragma unroll
+                for (int j = 0; j < kTiles; ++j) vb[j][u] = *(const intx4*)(at + ((16 * j) << p.page_shift));
             }
         }
-        c.vscale = p.v_scale[(int64_t)c.vscale * p.kv_heads + h];
-    };
-    int t0 = it.begin + wave * kKvChunk;
-    if (t0 < it.end) ask_keys(t0);
-    for (; t0 < it.end; t0 += 4 * kKvChunk) {
-        intx4 vb[kTiles][2];
+        const bool whole = t0 >= all_lo && t0 + kKvChunk <= all_hi;                    // every row sees all of it
+        bf16x8 w[R][4];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const unsigned char* at = p.v + ((((int64_t)c.vpage[u] * p.kv_heads + h) * D + n) << p.page_shift) + ((t0 + 64 * u + 16 * g) & (P - 1));
+        for (int r = 0; r < R; ++r) {
+            floatx4 s[8];
 #pragma unroll
-            for (int j = 0; j < kTiles; ++j) vb[j][u] = *(const intx4*)(at + ((int64_t)(16 * j) << p.page_shift));
-        }
-        const int vscale = c.vscale;
-        floatx4 s[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int ks = c.kscale[i >> 2];
-            if constexpr (D == 128) {
-                const intx8 a = __builtin_shufflevector(kb[i][0], kb[i][1], 0, 1, 2, 3, 4, 5, 6, 7);
-                s[i] = kv_mfma(a, q.hi, floatx4{0, 0, 0, 0}, ks, q.hi_scale);
-                s[i] = kv_mfma(a, q.lo, s[i], ks, q.lo_scale);
-            } else {
-                const intx8 a = __builtin_shufflevector(kb[i][0], kb[i][0], 0, 1, 2, 3, 4, 5, 6, 7);
-                s[i] = kv_mfma(a, q.hi, floatx4{0, 0, 0, 0}, ks, q.hi_scale);
+            for (int i = 0; i < 8; ++i) {
+                const int ks = kscale[i >> 2];
+                const intx8 a = __builtin_shufflevector(kb[i][0], kb[i][kWords - 1], 0, 1, 2, 3, 4, 5, 6, 7);
+                s[i] = kv_mfma(a, q[r].hi, floatx4{0, 0, 0, 0}, ks, q[r].hi_scale);
+                if constexpr (D == 128) s[i] = kv_mfma(a, q[r].lo, s[i], ks, q[r].lo_scale);
             }
-        }
-        if (t0 + 4 * kKvChunk < it.end) ask_keys(t0 + 4 * kKvChunk);
-        const bool whole = t0 >= all_lo && t0 + kKvChunk <= all_hi;
-        float top = -INFINITY;
+            if constexpr (CAP) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+                for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float x = kv_score<CAP>(p, s[i][e]);
-                if (!whole) {
-                    const int t = t0 + kv_token(i, 4 * g + e);
-                    x = t < see_hi && t >= see_lo ? x : -INFINITY;
-                }
-                s[i][e] = x;
-                top = fmaxf(top, x);
+                    for (int e = 0; e < 4; ++e) s[i][e] = kv_score<true>(p, s[i][e]);
             }
-        top = fmaxf(m, across_rows(top, Max()));
-        const float base = top == -INFINITY ? 0.f : top;           // (a row that has seen nothing yet)
-        const float shrink = __builtin_amdgcn_exp2f(m - base);
-        m = top;
-        l *= shrink;
-        // weights times 256, so that their lower term stays within E4M3 down to 2^-21 of the largest
-        intx8 hi, lo;
+            kv_settle();
+            if (!whole) {
+                asm volatile("");                                  // (a branch: as a selection it would cost every chunk three instructions a score)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float y[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                y[e] = __builtin_amdgcn_exp2f(s[i][e] - base + 8.f);
-                l += y[e];
-            }
-            int a, b;
-            kv_two_terms(y[0], y[1], y[2], y[3], a, b);
-            hi[i] = a;
-            lo[i] = b;
-        }
-#pragma unroll
-        for (int j = 0; j < kTiles; ++j) o[j] *= shrink;
-        if (!whole) {
-            // a NaN among the values of a token that only some rows see: cleared, and given to the rows that see it
-            bool nan = false;
-#pragma unroll
-            for (int j = 0; j < kTiles; ++j)
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const int v = kv_keep(vb[j][u][w], t0 + 64 * u + 16 * g + 4 * w, any_lo, any_hi);
-                        vb[j][u][w] = v;
-                        nan |= kv_nan_bytes(v) != 0;
-                    }
-            if (__any(nan)) {
-                intx8 seen;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    int v = 0;
+                for (int i = 0; i < 8; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int t = t0 + kv_token(i, 4 * g + e);
-                        if (t < see_hi && t >= see_lo) v |= 0x38 << (8 * e);                   // 1
+                        s[i][e] = t < see_hi[r] && t >= see_lo[r] ? s[i][e] : -INFINITY;
                     }
-                    seen[i] = v;
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top = fmaxf(top, s[i][e]);
+            const float factor = CAP ? 1.f : p.scale;              // (without a cap the scores stay as they are: it goes into the exponent)
+            top = across_rows(top, Max()) * factor;
+            // m follows the row's maximum once that has outgrown it 2^kKvSlack-fold
+            if (__any(top > m[r] + kKvSlack)) {
+                top = fmaxf(m[r], top);
+                const float shrink = __builtin_amdgcn_exp2f(m[r] - (top == -INFINITY ? 0.f : top));
+                m[r] = top;
+                l[r] *= shrink;
+#pragma unroll
+                for (int j = 0; j < kTiles; ++j) o[r][j] *= shrink;
+            }
+            const float base = m[r] == -INFINITY ? 0.f : -m[r];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[i][e] = __builtin_amdgcn_exp2f(s[i][e] * factor + base);
+                    l[r] += s[i][e];
                 }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[r][i] = kv_pack8(s[2 * i][0], s[2 * i][1], s[2 * i][2], s[2 * i][3], s[2 * i + 1][0], s[2 * i + 1][1], s[2 * i + 1][2], s[2 * i + 1][3]);
+            __builtin_amdgcn_sched_barrier(0);                     // (one group's scores, two tiles' widened values at a time: all at once do not fit the registers)
+        }
+        if (!whole) {
+            int keep[8], found = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) keep[i] = kv_keep_bytes(t0 + 64 * (i >> 2) + 16 * g + 4 * (i & 3), any_lo, any_hi);
+#pragma unroll
+            for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    vb[j][i >> 2][i & 3] &= keep[i];
+                    found |= kv_nan_bytes(vb[j][i >> 2][i & 3], vscale[i >> 2]);
+                }
+            if (__any(found != 0)) {
 #pragma unroll
                 for (int j = 0; j < kTiles; ++j) {
                     intx8 is;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const int v = vb[j][i >> 2][i & 3];
-                        const unsigned mask = (kv_nan_bytes(v) >> 7) * 255u;
-                        is[i] = (int)(mask & 0x38383838u);
-                        vb[j][i >> 2][i & 3] = (int)((unsigned)v & ~mask);
+                        const int nan = kv_nan_bytes(vb[j][i >> 2][i & 3], vscale[i >> 2]);
+                        is[i] = nan & 0x38383838;                  // (1)
+                        vb[j][i >> 2][i & 3] &= ~nan;
                     }
-                    const floatx4 cnt = kv_mfma(is, seen, floatx4{0, 0, 0, 0}, 127, 127);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (cnt[e] != 0.f) o[j][e] = NAN;
+                    for (int r = 0; r < R; ++r) {
+                        intx8 seen;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) seen[i] = 0x38383838 & kv_keep_bytes(t0 + 64 * (i >> 2) + 16 * g + 4 * (i & 3), see_lo[r], see_hi[r]);
+                        const floatx4 cnt = kv_mfma(is, seen, floatx4{0, 0, 0, 0}, 127, 127);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[r][j][e] += cnt[e] != 0.f ? NAN : 0.f;
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }
+        const float scale[2] = {kv_scale(vscale[0]), kv_scale(vscale[1])};
 #pragma unroll
         for (int j = 0; j < kTiles; ++j) {
-            const intx8 a = __builtin_shufflevector(vb[j][0], vb[j][1], 0, 1, 2, 3, 4, 5, 6, 7);
-            o[j] = kv_mfma(a, hi, o[j], vscale, 127);
-            o[j] = kv_mfma(a, lo, o[j], vscale, 123);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bf16x8 v = kv_widen(vb[j][i >> 1][2 * (i & 1)], vb[j][i >> 1][2 * (i & 1) + 1], scale[i >> 1]);
+#pragma unroll
+                for (int r = 0; r < R; ++r) o[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[r][i], o[r][j], 0, 0, 0);
+            }
+            if (j & 1) __builtin_amdgcn_sched_barrier(0);
+        }
+        kv_settle();                                               // (the next chunk may scale the outputs at once)
+    }
+    // the four wavefronts' results: o 2^(m - M) added up, and so the sums
+    const bool any_bad = __any(bad);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        l[r] = across_rows(l[r], Add());
+        if (any_bad) m[r] = NAN;
+        if (g == 0) {
+            stat[r][wave][n][0] = m[r];
+            stat[r][wave][n][1] = l[r];
         }
     }
-    l = across_rows(l, Add());
-    if (__any(bad)) m = NAN;
-    // the four wavefronts' results: o 2^(m - M) added up, and so the sums
-    if (g == 0) {
-        stat[wave][n][0] = m;
-        stat[wave][n][1] = l;
-    }
-    __syncthreads();
-    float M = -INFINITY, sum = 0.f;
-    bool nan = false;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        M = fmaxf(M, stat[w][n][0]);
-        nan |= stat[w][n][0] != stat[w][n][0];
-    }
-    const float base = M == -INFINITY ? 0.f : M;
+    for (int r = 0; r < R; ++r) {
+        __syncthreads();
+        float M = -INFINITY, sum = 0.f;
+        bool nan = false;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) sum += stat[w][n][1] * __builtin_amdgcn_exp2f(stat[w][n][0] - base);
-    const float mine = nan ? NAN : __builtin_amdgcn_exp2f(m - base);
+        for (int k = 0; k < 4; ++k) {
+            M = fmaxf(M, stat[r][k][n][0]);
+            nan |= stat[r][k][n][0] != stat[r][k][n][0];
+        }
+        const float base = M == -INFINITY ? 0.f : M;
 #pragma unroll
-    for (int j = 0; j < kTiles; ++j) *(floatx4*)&join[wave][n][16 * j + 4 * g] = o[j] * mine;
-    if (wave == 0 && g == 0) {
-        // (stat's first row is read by the lanes of this column alone from here on)
-        if (it.part >= 0 && valid) {
-            float* ml = p.part_ml + ((int64_t)h * p.part_rows + it.part + n) * 2;
-            ml[0] = nan ? NAN : M;
+        for (int k = 0; k < 4; ++k) sum += stat[r][k][n][1] * __builtin_amdgcn_exp2f(stat[r][k][n][0] - base);
+        if (nan) M = sum = NAN;
+        // without parts the outputs leave here as they are: the division goes into the factor
+        const float mine = __builtin_amdgcn_exp2f(m[r] - base) * (it.part >= 0 ? 1.f : 1.f / sum);
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j) *(floatx4*)&join[wave][n][16 * j + 4 * g] = o[r][j] * mine;
+        if (it.part >= 0 && wave == 0 && g == 0 && it.r0 + 16 * r + n < it.rows) {
+            float* ml = p.part_ml + ((int64_t)h * p.part_rows + it.part + 16 * r + n) * 2;
+            ml[0] = M;
             ml[1] = sum;
         }
-    }
-    __syncthreads();
-    if (wave == 0 && g == 0) stat[0][n][1] = sum;
-    __syncthreads();
-    for (int i = threadIdx.x; i < 16 * D / 4; i += 256) {
-        const int row = i / (D / 4), d = i % (D / 4) * 4, rr = it.r0 + row;
-        if (rr >= it.rows) continue;
-        floatx4 v = *(const floatx4*)&join[0][row][d];
+        __syncthreads();
+        for (int i = threadIdx.x; i < 16 * D / 4; i += 256) {
+            const int row = i / (D / 4), d = i % (D / 4) * 4, rr = it.r0 + 16 * r + row;
+            if (rr >= it.rows) continue;
+            floatx4 v = *(const floatx4*)&join[0][row][d];
 #pragma unroll
-        for (int w = 1; w < 4; ++w) v += *(const floatx4*)&join[w][row][d];
-        if (it.part >= 0) {
-            *(floatx4*)(p.part_o + ((int64_t)h * p.part_rows + it.part + row) * D + d) = v;
-        } else {
-            const float s = stat[0][row][1];
-            *(intx2*)(p.out + (int64_t)(it.row0 + rr / p.group) * p.out_stride + (h * p.group + rr % p.group) * D + d) =
-                intx2{(int)pack2_bf16(v[0] / s, v[1] / s), (int)pack2_bf16(v[2] / s, v[3] / s)};
+            for (int k = 1; k < 4; ++k) v += *(const floatx4*)&join[k][row][d];
+            if (it.part >= 0)
+                *(floatx4*)(p.part_o + ((int64_t)h * p.part_rows + it.part + 16 * r + row) * D + d) = v;
+            else
+                *(intx2*)(p.out + (int64_t)(it.row0 + rr / p.group) * p.out_stride + (h * p.group + rr % p.group) * D + d) = intx2{(int)pack2_bf16(v[0], v[1]), (int)pack2_bf16(v[2], v[3])};
         }
     }
 }
 
 // ---- tiles of 128 rows ------------------------------------------------------------------------------------------------------------
-// Prompts: four wavefronts with 32 rows each on the same tokens, 64 at a time through shared memory.  The products are v_mfma_scale_f32_32x32x64_f8f6f4, scores
-// again as K Q^T: in a chunk of 64 tokens, lane (n = lane % 32, g = lane / 32) gives
+// Prompts: four wavefronts with 32 rows each on the same tokens, 64 at a time through shared memory, keys as they are, values widened on the way.  In a chunk of 64
+// tokens, lane (n = lane % 32, g = lane / 32) gives
 //   left operand, keys    tile u (0, 1): token kv_tile_token(u, n), elements 64w + 16g .. and 64w + 32 + 16g .. (w: half of a head of 128)
 //   right operand         query row n, the same elements
-//   result                element 4a + b: token 32u + 16g + 4a + b of row n
-//   left operand, values  channel 32j + n, tokens 16g .. 16g+15 and 32 + 16g ..
-//   scales                of the 32 tokens (elements) 32g .. 32g+31
+//   result                element e: token 32u + 16(e / 8) + 8g + e % 8 of row n
+//   left operand, values  channel 32j + n, step q (0..3): tokens 16q + 8g .. +7
 constexpr int kKvTileRows = 128, kKvTileChunk = 64;
 
-struct KvTileItem {
-    int32_t table, row0, rows, past;      // as in KvRowsItem
-    int32_t r0;
-    int32_t begin, end;                   // begin: a multiple of 64
-    int32_t part;
-};
-
-__device__ __forceinline__ int kv_tile_token(int u, int m) { return 32 * u + 16 * ((m >> 2) & 1) + 4 * (m >> 3) + (m & 3); }
+__device__ __forceinline__ int kv_tile_token(int u, int m) { return 32 * u + 16 * (m >> 4) + 8 * ((m >> 2) & 1) + 4 * ((m >> 3) & 1) + (m & 3); }
 
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float kv_floatx16;
 __device__ __forceinline__ kv_floatx16 kv_mfma32(const intx8& a, const intx8& b, const kv_floatx16& c, int sa, int sb) {
@@ -388,17 +407,16 @@ __device__ __forceinline__ float across_halves(float v, F f) {
     return f(as_float((int)b[0]), as_float((int)b[1]));
 }
 
-// Where vector c (16 bytes) of a row lies in shared memory.  A wavefront's reads take the same vector of 32 rows: any 16 lanes in a row's order meet all 64 banks once.
-__device__ __forceinline__ int kv_lds_key(int D, int t, int c) {          // D: bytes of a token
-    return D == 128 ? t * 128 + 16 * (c ^ (((t >> 1) & 3) | ((t >> 4) & 1) << 2)) : t * 64 + 16 * (c ^ (((t >> 2) & 1) | ((t >> 4) & 1) << 1));
-}
-__device__ __forceinline__ int kv_lds_value(int d, int c) { return d * 64 + 16 * (c ^ ((d >> 2) & 3)); }
+// Where vector c (16 bytes) of a row lies in shared memory: of a token's key (`bytes` long) or a channel's 64 values (128 bytes).  A wavefront's reads take the same vector of 32
+// rows: any 16 lanes meet all 64 banks once.
+__device__ __forceinline__ int kv_lds(int bytes, int row, int c) { return row * bytes + 16 * (c ^ (bytes == 128 ? (row >> 1) & 7 : (row >> 2) & 3)); }
 
 template <int D, bool CAP>
 SYMB_KERNEL __launch_bounds__(256, 2) void symb_kv_tile_kernel(KvAttentionParams p) {
     constexpr int kHalves = D / 64, kTiles = D / 32, kVecs = D / 64;       // kVecs: vectors of keys (and of values) a thread moves a chunk
-    __shared__ __attribute__((aligned(16))) unsigned char keys[2][64 * D], values[2][64 * D];
-    const KvTileItem it = ((const KvTileItem*)p.items)[blockIdx.x / p.kv_heads];
+    __shared__ __attribute__((aligned(16))) unsigned char keys[2][64 * D], values[2][128 * D];
+    __shared__ int noted[2];
+    const KvItem it = p.items[blockIdx.x / p.kv_heads];
     const int h = blockIdx.x % p.kv_heads, tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 31, g = lane >> 5;
     const int w0 = it.r0 + 32 * wave, r = w0 + n, pos = it.past + r / p.group;
@@ -409,6 +427,8 @@ SYMB_KERNEL __launch_bounds__(256, 2) void symb_kv_tile_kernel(KvAttentionParams
     const bool some = w0 < it.rows;
     const int all_hi = it.past + w0 / p.group + 1, any_hi = some ? min(it.past + last / p.group + 1, it.end) : 0;
     const int any_lo = p.window ? max(all_hi - p.window, 0) : 0, all_lo = p.window ? max(it.past + last / p.group + 1 - p.window, 0) : 0;
+    // of all the tile's rows: the tokens that all see, and the first that any sees
+    const int tile_all_hi = it.past + it.r0 / p.group + 1, tile_all_lo = p.window ? max(it.past + min(it.r0 + kKvTileRows - 1, it.rows - 1) / p.group + 1 - p.window, 0) : 0;
     const int tile_lo = p.window ? max(it.past + it.r0 / p.group + 1 - p.window, 0) : 0;
 
     intx8 qh[kHalves], ql[kHalves];
@@ -451,17 +471,17 @@ SYMB_KERNEL __launch_bounds__(256, 2) void symb_kv_tile_kernel(KvAttentionParams
     // the tokens 32i .. 32i+31, so that a page's address is the same in a wavefront's lanes.
     const int in_page = (1 << p.page_shift) - 1, kt = tid / (D / 16), kc = tid % (D / 16), vd = D == 128 ? tid >> 1 : (tid & 127) >> 1, vc = tid & 1;
     const int k_off = (kt & in_page & 31) * D + 16 * kc, v_off = (vd << p.page_shift) + 16 * vc;
-    const int k_lds = kv_lds_key(D, kt, kc);                       // (32 tokens on: a fixed distance)
+    const int k_lds = kv_lds(D, kt, kc);                       // (32 tokens on: a fixed distance)
     intx4 kv[kVecs], vv[kVecs];
-    int kscale[2], vscale, next_kscale[2], next_vscale;
+    int kscale[2], next_kscale[2], next_vscale[2];
     auto ask = [&](int t0) {
         int64_t block[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             block[u] = (int64_t)kv_page(p, it.table, t0 + 32 * u, tile_lo, it.end, bad) * p.kv_heads + h;
             next_kscale[u] = p.k_scale[block[u]];
+            next_vscale[u] = p.v_scale[block[u]];
         }
-        next_vscale = p.v_scale[g ? block[1] : block[0]];
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {
             const int u = D == 128 ? i : wave >> 1, slot = (t0 + 32 * u) & in_page;
@@ -469,128 +489,144 @@ SYMB_KERNEL __launch_bounds__(256, 2) void symb_kv_tile_kernel(KvAttentionParams
             vv[i] = *(const intx4*)(p.v + ((block[u] * D) << p.page_shift) + slot + v_off);
         }
     };
-    auto put = [&](int buf) {
+    // Where not every row of the tile sees the whole chunk, its values are cleaned on the way: tokens that no row sees are cleared, and so is NaN among the
+    // others, which is noted (by the chunk's first token: a note of an earlier chunk means nothing).
+    auto put = [&](int buf, int t0) {
+        const bool edge = t0 < tile_all_lo || t0 + kKvTileChunk > tile_all_hi;
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {
+            const int u = D == 128 ? i : wave >> 1;
             *(intx4*)(keys[buf] + k_lds + 32 * D * i) = kv[i];
-            *(intx4*)(values[buf] + kv_lds_value(vd, vc + 2 * (D == 128 ? i : wave >> 1))) = vv[i];
+            if (edge) {
+                int found = 0;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int v = vv[i][w] & kv_keep_bytes(t0 + 32 * u + 16 * vc + 4 * w, tile_lo, it.end), nan = kv_nan_bytes(v, next_vscale[u]);
+                    found |= nan;
+                    vv[i][w] = v & ~nan;
+                }
+                if (found) noted[buf] = t0;
+            }
+            const float scale = kv_scale(next_vscale[u]);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) *(bf16x8*)(values[buf] + kv_lds(128, vd, 4 * u + 2 * vc + c)) = kv_widen(vv[i][2 * c], vv[i][2 * c + 1], scale);
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) kscale[u] = next_kscale[u];
-        vscale = next_vscale;
     };
-    // One chunk; WHOLE: all of the wavefront's rows see all of it.
-    auto chunk = [&](auto WHOLE, int t0, int buf) {
-        constexpr bool whole = decltype(WHOLE)::value;
-        kv_floatx16 s[2];
+    // NaN that `put` has cleared, to the rows that see it: ones in its places times ones where a row sees the token.
+    auto give_nan = [&](int t0) {
+        for (int q = 0; q < 4; ++q) {
+            const int t = t0 + 16 * q + 8 * g;
+            const int64_t block = (int64_t)kv_page(p, it.table, t0 + 16 * q, tile_lo, it.end, bad) * p.kv_heads + h;
+            const int byte = p.v_scale[block];
+            intx4 seen;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int t = kv_tile_token(0, n);
+            for (int i = 0; i < 4; ++i) seen[i] = (t + 2 * i >= see_lo && t + 2 * i < see_hi ? 0x3f80 : 0) | (t + 2 * i + 1 >= see_lo && t + 2 * i + 1 < see_hi ? 0x3f800000 : 0);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[u][e] = 0.f;
+            for (int j = 0; j < kTiles; ++j) {
+                const intx2 v = *(const intx2*)(p.v + ((block * D + 32 * j + n) << p.page_shift) + (t & in_page));
+                intx4 is;
 #pragma unroll
-            for (int w = 0; w < kHalves; ++w) {
-                const unsigned char* at = keys[buf] + 32 * D * u;
-                const intx4 a = *(const intx4*)(at + kv_lds_key(D, t, 4 * w + g)), b = *(const intx4*)(at + kv_lds_key(D, t, 4 * w + 2 + g));
-                const intx8 k = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-                s[u] = kv_mfma32(k, qh[w], s[u], kscale[u], q_scale);
-                s[u] = kv_mfma32(k, ql[w], s[u], kscale[u], q_scale - 4);
-            }
-        }
-        // without a cap the scores stay as they are: their factor goes into the exponent
-        float top = -INFINITY;
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                if (CAP) s[u][e] = kv_score<true>(p, s[u][e]);
-                if (!whole) {
-                    const int t = t0 + 32 * u + 16 * g + e;
-                    s[u][e] = t < see_hi && t >= see_lo ? s[u][e] : -INFINITY;
+                for (int i = 0; i < 4; ++i) {
+                    const int nan = kv_nan_bytes(v[i >> 1] & kv_keep_bytes(t + 4 * (i >> 1), tile_lo, it.end), byte) >> (16 * (i & 1));
+                    is[i] = (nan & 1 ? 0x3f80 : 0) | (nan & 0x100 ? 0x3f800000 : 0);
                 }
-                top = fmaxf(top, s[u][e]);
+                kv_floatx16 cnt;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) cnt[e] = 0.f;
+                cnt = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, is), __builtin_bit_cast(bf16x8, seen), cnt, 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[j][e] += cnt[e] != 0.f ? NAN : 0.f;
             }
-        const float factor = CAP ? 1.f : p.scale;
-        top = across_halves(top, Max()) * factor;
-        // m follows the row's maximum once that has outgrown it 16-fold: weights up to 2^(4 + 4)
-        if (__any(top > m + 4.f)) {
-            top = fmaxf(m, top);
-            const float shrink = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top));
-            m = top;
-            l *= shrink;
-#pragma unroll
-            for (int j = 0; j < kTiles; ++j) o[j] *= shrink;
-        }
-        const float base = 4.f - (m == -INFINITY ? 0.f : m);
-        intx8 hi, lo;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float y[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                y[e] = __builtin_amdgcn_exp2f(s[i >> 2][4 * (i & 3) + e] * factor + base);
-                l += y[e];
-            }
-            int a, b;
-            kv_two_terms(y[0], y[1], y[2], y[3], a, b);
-            hi[i] = a;
-            lo[i] = b;
-        }
-#pragma unroll
-        for (int j = 0; j < kTiles; ++j) {
-            const unsigned char* at = values[buf] + 32 * 64 * j;
-            intx4 a = *(const intx4*)(at + kv_lds_value(n, g)), b = *(const intx4*)(at + kv_lds_value(n, 2 + g));
-            if constexpr (!whole) {
-                bool nan = false;
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    a[w] = kv_keep(a[w], t0 + 16 * g + 4 * w, any_lo, any_hi);
-                    b[w] = kv_keep(b[w], t0 + 32 + 16 * g + 4 * w, any_lo, any_hi);
-                    nan |= (kv_nan_bytes(a[w]) | kv_nan_bytes(b[w])) != 0;
-                }
-                if (__any(nan)) {
-                    // a NaN among the values of a token that only some rows see: cleared, and given to the rows that see it
-                    intx8 seen, is;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        int v = 0;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int t = t0 + 32 * (i >> 2) + 16 * g + 4 * (i & 3) + e;
-                            if (t < see_hi && t >= see_lo) v |= 0x38 << (8 * e);           // 1
-                        }
-                        seen[i] = v;
-                        const int w = i < 4 ? a[i & 3] : b[i & 3];
-                        const unsigned mask = (kv_nan_bytes(w) >> 7) * 255u;
-                        is[i] = (int)(mask & 0x38383838u);
-                        if (i < 4) a[i & 3] = (int)((unsigned)w & ~mask);
-                        else b[i & 3] = (int)((unsigned)w & ~mask);
-                    }
-                    kv_floatx16 cnt;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) cnt[e] = 0.f;
-                    cnt = kv_mfma32(is, seen, cnt, 127, 127);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) o[j][e] += cnt[e] != 0.f ? NAN : 0.f;
-                }
-            }
-            const intx8 v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-            o[j] = kv_mfma32(v, hi, o[j], vscale, 127);
-            o[j] = kv_mfma32(v, lo, o[j], vscale, 123);
         }
     };
+    const int t_lane = kv_tile_token(0, n);
+    if (tid < 2) noted[tid] = -1;
     ask(it.begin);
-    put(0);
+    __syncthreads();
+    put(0, it.begin);
     __syncthreads();
     int buf = 0;
     for (int t0 = it.begin; t0 < it.end; t0 += kKvTileChunk, buf ^= 1) {
         const bool more = t0 + kKvTileChunk < it.end;
         if (more) ask(t0 + kKvTileChunk);
-        if (t0 >= all_lo && t0 + kKvTileChunk <= all_hi) chunk(std::true_type(), t0, buf);             // (the same in all lanes)
-        else if (t0 < any_hi && t0 + kKvTileChunk > any_lo) chunk(std::false_type(), t0, buf);
-        if (more) put(buf ^ 1);
+        if (t0 < any_hi && t0 + kKvTileChunk > any_lo) {           // (the same in all lanes)
+            kv_floatx16 s[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[u][e] = 0.f;
+#pragma unroll
+                for (int w = 0; w < kHalves; ++w) {
+                    const unsigned char* at = keys[buf] + 32 * D * u;
+                    const intx4 a = *(const intx4*)(at + kv_lds(D, t_lane, 4 * w + g)), b = *(const intx4*)(at + kv_lds(D, t_lane, 4 * w + 2 + g));
+                    const intx8 k = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+                    s[u] = kv_mfma32(k, qh[w], s[u], kscale[u], q_scale);
+                    s[u] = kv_mfma32(k, ql[w], s[u], kscale[u], q_scale - 4);
+                }
+            }
+            if constexpr (CAP) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[u][e] = kv_score<true>(p, s[u][e]);
+            }
+            kv_settle();
+            if (t0 < all_lo || t0 + kKvTileChunk > all_hi) {       // not every row sees all of it
+                asm volatile("");                                  // (a branch: as a selection it would cost every chunk)
+                const int hi = see_hi - t0 - 8 * g, lo = see_lo - t0 - 8 * g;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int t = 32 * u + 16 * (e >> 3) + (e & 7);
+                        s[u][e] = t < hi && t >= lo ? s[u][e] : -INFINITY;
+                    }
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
+            const float factor = CAP ? 1.f : p.scale;              // (without a cap the scores stay as they are: it goes into the exponent)
+            top = across_halves(top, Max()) * factor;
+            if (__any(top > m + kKvSlack)) {
+                top = fmaxf(m, top);
+                const float shrink = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top));
+                m = top;
+                l *= shrink;
+#pragma unroll
+                for (int j = 0; j < kTiles; ++j) o[j] *= shrink;
+            }
+            const float base = m == -INFINITY ? 0.f : -m;
+            bf16x8 w[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float y[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    y[e] = __builtin_amdgcn_exp2f(s[q >> 1][8 * (q & 1) + e] * factor + base);
+                    l += y[e];
+                }
+                w[q] = kv_pack8(y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7]);
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int j = 0; j < kTiles; ++j) {
+                    const bf16x8 v = *(const bf16x8*)(values[buf] + 32 * 128 * j + kv_lds(128, n, 2 * q + g));
+                    o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[q], o[j], 0, 0, 0);
+                }
+            if (noted[buf] == t0) {
+                kv_settle();
+                give_nan(t0);
+            }
+        }
+        if (more) put(buf ^ 1, t0 + kKvTileChunk);
         __syncthreads();
     }
+    kv_settle();
     l = across_halves(l, Add());
     if (__any(bad)) m = NAN;
     if (!valid) return;

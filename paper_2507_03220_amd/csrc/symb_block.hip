@@ -184,23 +184,23 @@ void launch_append(const KvAppendParams& p, int pages, bool few, int ny, hipStre
 
 // The work of one attention call.
 struct KvPlan {
-    std::vector<KvRowsItem> rows;
-    std::vector<KvTileItem> tiles;
+    std::vector<KvItem> rows[3];          // of up to 16, 32, 48 rows
+    std::vector<KvItem> tiles;
     std::vector<KvJoinItem> joins;
     int64_t part_rows = 0;                // rows of partial results, of one key head
 };
-// Segments of up to kKvFew rows for a key head go to the kernel of 16-row items, others to the tiles of 128 rows.
-constexpr int kKvFew = 32;
+// Segments of up to kKvFew rows for a key head go to the kernel whose items are all of them, others to the tiles of 128 rows.
+constexpr int kKvFew = 48;
 // Workgroups that a launch should have, and chunks (128 tokens for 16 rows, 64 for a tile) that one of them takes at least: a shorter run costs more in joining than it gains.
 constexpr int kKvGroups = 1024, kKvLeast = 8, kKvTileGroups = 512, kKvTileLeast = 16;
 KvPlan plan_attention(const symb_kv_batch* b, const symb_kv_cache* c, int q_heads, int window) {
     KvPlan plan;
     const int group = q_heads / c->kv_heads;
-    // f(segment, its rows, first row, first chunk, chunks, last token + 1) for runs of `step` rows
-    auto walk = [&](bool few, int step, int chunk, auto&& f) {
+    // f(segment, its rows, first row, first chunk, chunks, last token + 1) for runs of `step` rows of the segments with more than `least` and up to `most`
+    auto walk = [&](int64_t least, int64_t most, int step, int chunk, auto&& f) {
         for (int i = 0; i < b->num_segments; ++i) {
             const int64_t rows = (int64_t)(b->seg_offsets[i + 1] - b->seg_offsets[i]) * group;
-            if ((rows <= kKvFew) != few) continue;
+            if (rows <= least || rows > most) continue;
             for (int64_t r0 = 0; r0 < rows; r0 += step) {
                 const int64_t first = b->past[i] + r0 / group, last = b->past[i] + std::min(r0 + step - 1, rows - 1) / group;
                 const int64_t lo = window ? std::max<int64_t>(first + 1 - window, 0) : 0, c0 = lo / chunk;
@@ -208,11 +208,8 @@ KvPlan plan_attention(const symb_kv_batch* b, const symb_kv_cache* c, int q_head
             }
         }
     };
-    auto fill = [&](bool few, int step, int chunk, int groups, int least, auto& items) {
-        int64_t chunks = 0;
-        walk(few, step, chunk, [&](int, int, int, int, int n, int) { chunks += n; });
-        const int64_t quota = std::max<int64_t>(least, (chunks * c->kv_heads + groups - 1) / groups);
-        walk(few, step, chunk, [&](int i, int rows, int r0, int c0, int n, int end) {
+    auto fill = [&](int64_t least, int64_t most, int step, int chunk, int64_t quota, std::vector<KvItem>& items) {
+        walk(least, most, step, chunk, [&](int i, int rows, int r0, int c0, int n, int end) {
             const int parts = (int)((n + quota - 1) / quota);
             if (parts > 1)
                 for (int r = r0; r < std::min(r0 + step, rows); r += 16) plan.joins.push_back(KvJoinItem{b->seg_offsets[i], rows, r, (int32_t)(plan.part_rows + r - r0), parts, step});
@@ -225,8 +222,15 @@ KvPlan plan_attention(const symb_kv_batch* b, const symb_kv_cache* c, int q_head
         // the longest first: what is left over at the end is short
         std::stable_sort(items.begin(), items.end(), [](const auto& x, const auto& y) { return x.end - x.begin > y.end - y.begin; });
     };
-    fill(true, 16, kKvChunk, kKvGroups, kKvLeast, plan.rows);
-    fill(false, kKvTileRows, kKvTileChunk, kKvTileGroups, kKvTileLeast, plan.tiles);
+    // chunks a workgroup: as many as leave `groups` workgroups
+    auto quota = [&](int64_t least, int64_t most, int step, int chunk, int groups, int at_least) {
+        int64_t chunks = 0;
+        walk(least, most, step, chunk, [&](int, int, int, int, int n, int) { chunks += n; });
+        return std::max<int64_t>(at_least, (chunks * c->kv_heads + groups - 1) / groups);
+    };
+    const int64_t few = quota(0, kKvFew, kKvFew, kKvChunk, kKvGroups, kKvLeast);
+    for (int r = 0; r < 3; ++r) fill(16 * r, 16 * (r + 1), 16 * (r + 1), kKvChunk, few, plan.rows[r]);
+    fill(kKvFew, INT64_MAX, kKvTileRows, kKvTileChunk, quota(kKvFew, INT64_MAX, kKvTileRows, kKvTileChunk, kKvTileGroups, kKvTileLeast), plan.tiles);
     return plan;
 }
 size_t part_ml_bytes(const KvPlan& plan, int kv_heads) { return align_up((size_t)plan.part_rows * kv_heads * 2 * sizeof(float), 256); }
@@ -245,15 +249,16 @@ symb_status check_attention(symb_handle h, const symb_kv_batch* b, const symb_kv
 }
 
 template <int D, bool CAP>
-symb_status launch_attention(symb_handle h, KvAttentionParams p, const KvPlan& plan, const unsigned char* rows, const unsigned char* tiles, const KvJoinParams& jp, hipStream_t s) {
-    if (!plan.tiles.empty()) {
-        p.items = tiles;
-        hipLaunchKernelGGL((symb_kv_tile_kernel<D, CAP>), dim3((unsigned)(plan.tiles.size() * p.kv_heads)), dim3(256), 0, s, p);
-        SYMB_HIP(h, hipGetLastError());
-    }
-    if (!plan.rows.empty()) {
-        p.items = rows;
-        hipLaunchKernelGGL((symb_kv_rows_kernel<D, CAP>), dim3((unsigned)(plan.rows.size() * p.kv_heads)), dim3(256), 0, s, p);
+symb_status launch_attention(symb_handle h, KvAttentionParams p, const KvPlan& plan, const KvItem* const (&items)[4], const KvJoinParams& jp, hipStream_t s) {
+    for (int i = 0; i < 4; ++i) {
+        const size_t n = i < 3 ? plan.rows[i].size() : plan.tiles.size();
+        if (!n) continue;
+        p.items = items[i];
+        const dim3 grid((unsigned)(n * p.kv_heads));
+        if (i == 0) hipLaunchKernelGGL((symb_kv_rows_kernel<D, 1, CAP>), grid, dim3(256), 0, s, p);
+        else if (i == 1) hipLaunchKernelGGL((symb_kv_rows_kernel<D, 2, CAP>), grid, dim3(256), 0, s, p);
+        else if (i == 2) hipLaunchKernelGGL((symb_kv_rows_kernel<D, 3, CAP>), grid, dim3(256), 0, s, p);
+        else hipLaunchKernelGGL((symb_kv_tile_kernel<D, CAP>), grid, dim3(256), 0, s, p);
         SYMB_HIP(h, hipGetLastError());
     }
     if (!plan.joins.empty()) {
@@ -445,11 +450,14 @@ symb_status symb_kv_attention(symb_handle h, const symb_kv_batch* b, const symb_
         const size_t need = part_bytes(plan, cache);
         if (need && (!ws || ws_bytes < need)) return fail(h, SYMB_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : 0, need);
         if (need && misaligned16(ws)) return fail(h, SYMB_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
-        if ((int64_t)(plan.rows.size() + plan.tiles.size() + plan.joins.size()) * cache->kv_heads > INT32_MAX || plan.part_rows > INT32_MAX)
-            return fail(h, SYMB_ERR_UNSUPPORTED, "%zu work items of %d key heads", plan.rows.size() + plan.tiles.size(), cache->kv_heads);
+        size_t work = plan.tiles.size() + plan.joins.size();
+        for (const auto& r : plan.rows) work += r.size();
+        if ((int64_t)work * cache->kv_heads > INT32_MAX || plan.part_rows > INT32_MAX) return fail(h, SYMB_ERR_UNSUPPORTED, "%zu work items of %d key heads", work, cache->kv_heads);
         hipStream_t s = (hipStream_t)stream;
         Blob blob;
-        const size_t o_rows = blob.add(plan.rows.data(), plan.rows.size()), o_tiles = blob.add(plan.tiles.data(), plan.tiles.size()), o_join = blob.add(plan.joins.data(), plan.joins.size());
+        size_t o_items[4];
+        for (int i = 0; i < 4; ++i) o_items[i] = i < 3 ? blob.add(plan.rows[i].data(), plan.rows[i].size()) : blob.add(plan.tiles.data(), plan.tiles.size());
+        const size_t o_join = blob.add(plan.joins.data(), plan.joins.size());
         unsigned char* dev = nullptr;
         if ((st = upload(h, blob, s, &dev)) != SYMB_OK) return st;
         constexpr float kLog2e = 1.442695041f;
@@ -474,8 +482,9 @@ symb_status symb_kv_attention(symb_handle h, const symb_kv_batch* b, const symb_
         p.scale = cap > 0.f ? scale / cap : scale * kLog2e;
         p.cap = cap * kLog2e;
         const KvJoinParams jp{(const KvJoinItem*)(dev + o_join), p.part_o, p.part_ml, p.out, out_stride, p.kv_heads, p.group, p.part_rows};
-        st = D == 128 ? (cap > 0.f ? launch_attention<128, true>(h, p, plan, dev + o_rows, dev + o_tiles, jp, s) : launch_attention<128, false>(h, p, plan, dev + o_rows, dev + o_tiles, jp, s))
-                      : (cap > 0.f ? launch_attention<64, true>(h, p, plan, dev + o_rows, dev + o_tiles, jp, s) : launch_attention<64, false>(h, p, plan, dev + o_rows, dev + o_tiles, jp, s));
+        const KvItem* const items[4] = {(const KvItem*)(dev + o_items[0]), (const KvItem*)(dev + o_items[1]), (const KvItem*)(dev + o_items[2]), (const KvItem*)(dev + o_items[3])};
+        if (D == 128) st = cap > 0.f ? launch_attention<128, true>(h, p, plan, items, jp, s) : launch_attention<128, false>(h, p, plan, items, jp, s);
+        else st = cap > 0.f ? launch_attention<64, true>(h, p, plan, items, jp, s) : launch_attention<64, false>(h, p, plan, items, jp, s);
         if (st != SYMB_OK) return st;
         guard.completed = true;
         return seal_slot(h);
