@@ -8,6 +8,7 @@ library is missing, `lib()` raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from dataclasses import dataclass
 from typing import Optional, Sequence
@@ -197,25 +198,25 @@ def _int32s(values):
     return (C.c_int32 * max(len(v), 1))(*v)
 
 
-def _shaped(t, what: str, dtype: str, dims: int):
-    """The tensor as the C ABI takes it, or ValueError: `dims` dimensions of that type."""
-    if t.dim() != dims or not str(t.dtype).endswith(dtype):
-        raise ValueError(f"{what}: {dims} dimensions of {dtype} expected, got {tuple(t.shape)} of {t.dtype}")
-    return t
+@functools.lru_cache(maxsize=None)
+def _dtype(name: str):
+    import torch
+    return getattr(torch, name)
 
 
 def _dense(t, what: str, dtype: str, dims: int):
-    if not _shaped(t, what, dtype, dims).is_contiguous():
-        raise ValueError(f"{what} must be dense")
+    """The tensor as the C ABI takes it, or ValueError: `dims` dense dimensions of that type."""
+    if t.dtype is not _dtype(dtype) or t.dim() != dims or not t.is_contiguous():
+        raise ValueError(f"{what}: {dims} dense dimensions of {dtype} expected, got {tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
     return t
 
 
-def _head_rows(t, what: str, T: int, heads: int, dim: int) -> int:
+def _head_rows(t, what: str, shape) -> int:
     """Row stride of a [T][heads][dim] bf16 tensor whose rows may lie apart."""
-    _shaped(t, what, "bfloat16", 3)
-    if tuple(t.shape) != (T, heads, dim) or t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
-        raise ValueError(f"{what}: [{T}][{heads}][{dim}] with whole rows expected, got {tuple(t.shape)}, strides {t.stride()}")
-    return t.stride(0) if T > 1 else max(t.stride(0), heads * dim)
+    apart, head, element = t.stride() if t.dim() == 3 else (0, 0, 0)
+    if t.dtype is not _dtype("bfloat16") or t.shape != shape or element != 1 or (head != shape[2] and shape[1] > 1):
+        raise ValueError(f"{what}: {list(shape)} of bfloat16 with whole rows expected, got {tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
+    return apart if shape[0] > 1 else max(apart, shape[1] * shape[2])
 
 
 @dataclass
@@ -243,9 +244,10 @@ class NormBatch:
         self._off, self._keep = _int32s(seg_offsets), list(norms)
         self._norms = (symb_norm * max(S, 1))(*[(_ptr(n.weight), _ptr(n.bias), _ptr(n.dweight), _ptr(n.dbias)) for n in norms])
         self.c = symb_norm_batch(self.width, S, self._off, self._norms, int(kind), float(eps), float(weight_base))
+        self._ref = C.byref(self.c)
 
     def ref(self):
-        return C.byref(self.c)
+        return self._ref
 
 
 class KvCache:
@@ -261,6 +263,7 @@ class KvCache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.num_pages, self.kv_heads, self.page_tokens, self.head_dim = k.shape
         self.c = symb_kv_cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), self.num_pages, self.kv_heads, self.head_dim, self.page_tokens)
+        self._ref = C.byref(self.c)
 
     @classmethod
     def empty(cls, num_pages: int, kv_heads: int, head_dim: int, page_tokens: int = 64, device="cuda"):
@@ -270,7 +273,7 @@ class KvCache:
                    make(num_pages, kv_heads, dtype=torch.float8_e8m0fnu), make(num_pages, kv_heads, dtype=torch.float8_e8m0fnu))
 
     def ref(self):
-        return C.byref(self.c)
+        return self._ref
 
 
 class KvBatch:
@@ -284,9 +287,10 @@ class KvBatch:
             raise ValueError(f"page_table has {page_table.shape[0]} rows for {self.S} segments")
         self._off, self._past, self.page_table = _int32s(seg_offsets), _int32s(past), page_table
         self.c = symb_kv_batch(self.S, self._off, self._past, _ptr(page_table), page_table.shape[1] if page_table is not None else int(table_stride))
+        self._ref = C.byref(self.c)
 
     def ref(self):
-        return C.byref(self.c)
+        return self._ref
 
 
 class Rotation:
@@ -295,9 +299,10 @@ class Rotation:
     def __init__(self, table, pairs: int = SYMB_ROTATE_HALVES):
         self.table = _dense(table, "table", "float32", 2)
         self.c = symb_rotation(table.data_ptr(), table.shape[0], table.shape[1], int(pairs))
+        self._ref = C.byref(self.c)
 
     def ref(self):
-        return C.byref(self.c)
+        return self._ref
 
 
 # ---- entry points, same names as the C ABI ----------------------------------------------------
@@ -476,30 +481,33 @@ def symb_norm_workspace_bytes(batch: NormBatch) -> int:
     return int(out.value)
 
 
-def _norm_rows(batch: NormBatch, **tensors) -> None:
-    for what, t in tensors.items():
-        if tuple(_dense(t, what, "bfloat16", 2).shape) != (batch.T, batch.width):
-            raise ValueError(f"{what}: [{batch.T}][{batch.width}] expected, got {tuple(t.shape)}")
+def _norm_rows(batch: NormBatch, *tensors) -> None:
+    bf16, shape = _dtype("bfloat16"), (batch.T, batch.width)
+    for t in tensors:
+        if t.dtype is not bf16 or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"dense [{batch.T}][{batch.width}] of bfloat16 expected, got {tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
 
 
 def symb_norm_fwd(handle, batch: NormBatch, X, Y, stream: int = 0) -> None:
-    _norm_rows(batch, X=X, Y=Y)
-    _check(lib().symb_norm_fwd(handle, batch.ref(), X.data_ptr(), Y.data_ptr(), stream or None), handle)
+    _norm_rows(batch, X, Y)
+    _check((_lib or lib()).symb_norm_fwd(handle, batch._ref, X.data_ptr(), Y.data_ptr(), stream or None), handle)
 
 
 def symb_norm_bwd(handle, batch: NormBatch, X, dY, dX, flags: int = SYMB_GRAD_OVERWRITE, ws=None, stream: int = 0) -> None:
-    _norm_rows(batch, X=X, dY=dY, dX=dX)
+    _norm_rows(batch, X, dY, dX)
     wp, wb = _ws_args(ws)
-    _check(lib().symb_norm_bwd(handle, batch.ref(), X.data_ptr(), dY.data_ptr(), dX.data_ptr(), int(flags), wp, wb, stream or None), handle)
+    _check((_lib or lib()).symb_norm_bwd(handle, batch._ref, X.data_ptr(), dY.data_ptr(), dX.data_ptr(), flags, wp, wb, stream or None), handle)
 
 
 def symb_kv_append(handle, batch: KvBatch, cache: KvCache, rotation: Optional[Rotation], q, q_out, k, v, stream: int = 0) -> None:
     """q, q_out [T][q_heads][head_dim] (both None: keys and values only), k, v [T][kv_heads][head_dim]; rows may lie apart."""
-    T, H, D = batch.T, cache.kv_heads, cache.head_dim
-    heads = 0 if q is None else q.shape[1]
-    _check(lib().symb_kv_append(handle, batch.ref(), cache.ref(), None if rotation is None else rotation.ref(), _ptr(q),
-                                _head_rows(q, "q", T, heads, D) if heads else 0, heads, _ptr(q_out), _head_rows(q_out, "q_out", T, heads, D) if heads else 0,
-                                k.data_ptr(), _head_rows(k, "k", T, H, D), v.data_ptr(), _head_rows(v, "v", T, H, D), stream or None), handle)
+    shape, heads, q_at, q_apart, out_at, out_apart = (batch.T, cache.kv_heads, cache.head_dim), 0, None, 0, None, 0
+    if q is not None:
+        heads = q.shape[1]
+        q_shape = (batch.T, heads, cache.head_dim)
+        q_at, q_apart, out_at, out_apart = q.data_ptr(), _head_rows(q, "q", q_shape), q_out.data_ptr(), _head_rows(q_out, "q_out", q_shape)
+    _check((_lib or lib()).symb_kv_append(handle, batch._ref, cache._ref, None if rotation is None else rotation._ref, q_at, q_apart, heads, out_at, out_apart, k.data_ptr(),
+                                          _head_rows(k, "k", shape), v.data_ptr(), _head_rows(v, "v", shape), stream or None), handle)
 
 
 def symb_kv_workspace_bytes(batch: KvBatch, cache: KvCache, q_heads: int, window: int = 0) -> int:
@@ -510,7 +518,8 @@ def symb_kv_workspace_bytes(batch: KvBatch, cache: KvCache, q_heads: int, window
 
 def symb_kv_attention(handle, batch: KvBatch, cache: KvCache, q, out, scale: float, window: int = 0, cap: float = 0.0, ws=None, stream: int = 0) -> None:
     """q, out [T][q_heads][head_dim]; rows may lie apart."""
-    T, heads, D = batch.T, q.shape[1], cache.head_dim
+    heads = q.shape[1]
+    shape = (batch.T, heads, cache.head_dim)
     wp, wb = _ws_args(ws)
-    _check(lib().symb_kv_attention(handle, batch.ref(), cache.ref(), q.data_ptr(), _head_rows(q, "q", T, heads, D), heads, out.data_ptr(),
-                                   _head_rows(out, "out", T, heads, D), float(scale), int(window), float(cap), wp, wb, stream or None), handle)
+    _check((_lib or lib()).symb_kv_attention(handle, batch._ref, cache._ref, q.data_ptr(), _head_rows(q, "q", shape), heads, out.data_ptr(), _head_rows(out, "out", shape),
+                                             scale, window, cap, wp, wb, stream or None), handle)

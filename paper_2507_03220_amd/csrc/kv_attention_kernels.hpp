@@ -664,32 +664,52 @@ struct KvJoinParams {
     int64_t out_stride;
     int32_t kv_heads, group, part_rows;
 };
+// A workgroup a row: a long context has dozens of parts, 1024 / D of which are read at once; joined in a fixed order.
 template <int D>
 SYMB_KERNEL __launch_bounds__(256) void symb_kv_join_kernel(KvJoinParams p) {
+    constexpr int kLanes = D / 4, kSets = 256 / kLanes;
+    __shared__ float top[4];
+    __shared__ floatx4 part[kSets][kLanes];
+    __shared__ float sums[kSets];
     const KvJoinItem it = p.items[blockIdx.x / p.kv_heads];
-    const int h = blockIdx.x % p.kv_heads;
-    for (int i = threadIdx.x; i < 16 * D / 4; i += 256) {
-        const int row = i / (D / 4), d = i % (D / 4) * 4, rr = it.r0 + row;
-        if (rr >= it.rows) continue;
-        const int64_t at = (int64_t)h * p.part_rows + it.part0 + row;
-        float M = -INFINITY, sum = 0.f;
-        bool nan = false;
-        for (int k = 0; k < it.parts; ++k) {
-            const float m = p.part_ml[(at + (int64_t)it.stride * k) * 2];
-            nan |= m != m;
-            M = fmaxf(M, m);
-        }
-        const float base = M == -INFINITY ? 0.f : M;
-        floatx4 v = floatx4{0, 0, 0, 0};
-        for (int k = 0; k < it.parts; ++k) {
-            const float f = __builtin_amdgcn_exp2f(p.part_ml[(at + (int64_t)it.stride * k) * 2] - base);
-            sum += p.part_ml[(at + (int64_t)it.stride * k) * 2 + 1] * f;
-            v += *(const floatx4*)(p.part_o + (at + (int64_t)it.stride * k) * D + d) * f;
-        }
-        if (nan) sum = NAN;
-        *(intx2*)(p.out + (int64_t)(it.row0 + rr / p.group) * p.out_stride + (h * p.group + rr % p.group) * D + d) =
-            intx2{(int)pack2_bf16(v[0] / sum, v[1] / sum), (int)pack2_bf16(v[2] / sum, v[3] / sum)};
+    const int h = blockIdx.x % p.kv_heads, row = it.r0 + blockIdx.y, tid = threadIdx.x;
+    if (row >= it.rows) return;
+    const int64_t at = (int64_t)h * p.part_rows + it.part0 + blockIdx.y;
+    float M = -INFINITY, bad = 0.f;
+    for (int k = tid; k < it.parts; k += 256) {
+        const float m = p.part_ml[(at + (int64_t)it.stride * k) * 2];
+        if (m != m) bad = 1.f;
+        M = fmaxf(M, m);
     }
+    M = across_wave(bad != 0.f ? INFINITY : M, Max());            // (no maximum is infinite without the row being NaN)
+    if ((tid & 63) == 0) top[tid >> 6] = M;
+    __syncthreads();
+    M = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+    const float base = M == -INFINITY ? 0.f : M;
+    const int set = tid / kLanes, d = tid % kLanes * 4;
+    float sum = 0.f;
+    floatx4 v = floatx4{0, 0, 0, 0};
+#pragma unroll 4
+    for (int k = set; k < it.parts; k += kSets) {
+        const int64_t a = at + (int64_t)it.stride * k;
+        const float f = __builtin_amdgcn_exp2f(p.part_ml[a * 2] - base);
+        sum += p.part_ml[a * 2 + 1] * f;
+        v += *(const floatx4*)(p.part_o + a * D + d) * f;
+    }
+    part[set][tid % kLanes] = v;
+    if (d == 0) sums[set] = sum;
+    __syncthreads();
+    if (tid >= kLanes) return;
+    sum = sums[0];
+    v = part[0][tid];
+#pragma unroll
+    for (int k = 1; k < kSets; ++k) {
+        sum += sums[k];
+        v += part[k][tid];
+    }
+    if (M == INFINITY) sum = NAN;
+    *(intx2*)(p.out + (int64_t)(it.row0 + row / p.group) * p.out_stride + (h * p.group + row % p.group) * D + d) =
+        intx2{(int)pack2_bf16(v[0] / sum, v[1] / sum), (int)pack2_bf16(v[2] / sum, v[3] / sum)};
 }
 
 }  // namespace symb

@@ -150,65 +150,68 @@ SYMB_KERNEL __launch_bounds__(WAVES * 64) void symb_norm_bwd_kernel(NormBwdParam
     const int nvec = p.width >> 3;
     const float inv = 1.f / p.width;
     float aw[NV][8] = {}, ab[NV][8] = {};
-    for (int k = 0; k < ch.rows; ++k) {
-        const int64_t at = (int64_t)(ch.row0 + k) * p.width;
-        NormVec x[NV], dy[NV];
+    NormVec w[NV], x[NV], dy[NV];
+    auto ask = [&](int64_t at) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = i * kLanes + lane;
-            x[i] = dy[i] = NormVec{{0, 0, 0, 0}};
-            if (c < nvec) {
-                x[i] = norm_load(p.X + at + c * 8);
-                dy[i] = norm_load(p.dY + at + c * 8);
-            }
+            if (c >= nvec) continue;
+            x[i] = norm_load(p.X + at + c * 8);
+            dy[i] = norm_load(p.dY + at + c * 8);
         }
+    };
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = i * kLanes + lane;
+        x[i] = dy[i] = NormVec{{0, 0, 0, 0}};          // (columns behind the last one count as zeros, weight included)
+        w[i] = nd.w && c < nvec ? norm_load(nd.w + c * 8) : NormVec{{0, 0, 0, 0}};
+    }
+    const float base = nd.w ? p.base : 1.f;
+    int64_t at = (int64_t)ch.row0 * p.width;
+    ask(at);
+    for (int k = 0; k < ch.rows; ++k, at += p.width) {
         float mu = 0.f, mg = 0.f, s[2];
         if (!RMS) {
             s[0] = s[1] = 0.f;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                float w[8];
-                if (i * kLanes + lane >= nvec) continue;
-                norm_weight(nd.w, p.base, (i * kLanes + lane) * 8, w);
+            for (int i = 0; i < NV; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     s[0] += x[i].get(j);
-                    s[1] += dy[i].get(j) * w[j];
+                    s[1] += dy[i].get(j) * (base + w[i].get(j));
                 }
-            }
             norm_sums<WAVES, 2>(s, lds, wave, 0);
             mu = s[0] * inv;
             mg = s[1] * inv;
         }
         s[0] = s[1] = 0.f;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            float w[8];
-            if (i * kLanes + lane >= nvec) continue;
-            norm_weight(nd.w, p.base, (i * kLanes + lane) * 8, w);
+        for (int i = 0; i < NV; ++i)
+            if (i * kLanes + lane < nvec)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float d = x[i].get(j) - mu;
-                s[0] += d * d;
-                s[1] += dy[i].get(j) * w[j] * d;
-            }
-        }
+                for (int j = 0; j < 8; ++j) {
+                    const float d = x[i].get(j) - mu;
+                    s[0] += d * d;
+                    s[1] += dy[i].get(j) * (base + w[i].get(j)) * d;
+                }
+        NormVec x0[NV], dy0[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) x0[i] = x[i], dy0[i] = dy[i];
+        if (k + 1 < ch.rows) ask(at + p.width);        // the next row's way, while the sums of this one cross the wavefronts
         norm_sums<WAVES, 2>(s, lds, wave, RMS ? k & 1 : 1);             // (one barrier a row: two rows in turn)
         const float r = 1.f / sqrtf(s[0] * inv + p.eps), mgz = s[1] * r * inv;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = i * kLanes + lane;
-            if (c >= nvec) continue;
-            float w[8], o[8];
-            norm_weight(nd.w, p.base, c * 8, w);
+            float o[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float z = (x[i].get(j) - mu) * r, g = dy[i].get(j);
-                o[j] = r * (g * w[j] - mg - z * mgz);
+                const float z = (x0[i].get(j) - mu) * r, g = dy0[i].get(j);
+                o[j] = r * (g * (base + w[i].get(j)) - mg - z * mgz);
                 aw[i][j] += g * z;
                 ab[i][j] += g;
             }
-            norm_store(p.dX + at + c * 8, o);
+            if (c < nvec) norm_store(p.dX + at + c * 8, o);
         }
     }
     if (ch.part < 0) return;
@@ -237,18 +240,30 @@ struct NormReduceParams {
     const NormGroup* groups;
     int32_t width, accumulate;
 };
+// 64 columns a workgroup, 16 parts at once; each lane's sum in the order of the parts, the 16 sums one after the other.
 SYMB_KERNEL __launch_bounds__(256) void symb_norm_reduce_kernel(NormReduceParams p) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= p.width) return;
+    __shared__ floatx4 sums[16][16];
+    const int lane = threadIdx.x & 15, set = threadIdx.x >> 4, c = blockIdx.x * 64 + lane * 4;
     const NormGroup g = p.groups[blockIdx.y];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         float* out = k ? g.db : g.dw;
-        if (!out) continue;
-        const float* part = (k ? p.part_b : p.part_w) + (int64_t)g.part0 * p.width + c;
-        float s = 0.f;
-        for (int i = 0; i < g.parts; ++i) s += part[(int64_t)i * p.width];
-        out[c] = p.accumulate ? out[c] + s : s;
+        if (!out) continue;                            // (the same in all lanes)
+        floatx4 s = floatx4{0, 0, 0, 0};
+        if (c < p.width) {
+            const float* part = (k ? p.part_b : p.part_w) + (int64_t)g.part0 * p.width + c;
+#pragma unroll 4
+            for (int i = set; i < g.parts; i += 16) s += *(const floatx4*)(part + (int64_t)i * p.width);
+        }
+        sums[set][lane] = s;
+        __syncthreads();
+        if (set == 0 && c < p.width) {
+#pragma unroll
+            for (int i = 1; i < 16; ++i) s += sums[i][lane];
+            if (p.accumulate) s += *(const floatx4*)(out + c);
+            *(floatx4*)(out + c) = s;
+        }
+        __syncthreads();
     }
 }
 

@@ -135,7 +135,7 @@ void launch_norm_bwd(const NormBwdParams& p, int chunks, hipStream_t s) {
     if (vecs <= 512) return launch_norm_bwd<RMS, 4, 2>(p, chunks, s);
     if (vecs <= 768) return launch_norm_bwd<RMS, 4, 3>(p, chunks, s);
     if (vecs <= 1024) return launch_norm_bwd<RMS, 4, 4>(p, chunks, s);
-    return launch_norm_bwd<RMS, 16, 2>(p, chunks, s);
+    return launch_norm_bwd<RMS, 8, 4>(p, chunks, s);
 }
 
 // ---- key/value cache --------------------------------------------------------------------------
@@ -187,6 +187,7 @@ struct KvPlan {
     std::vector<KvItem> rows[3];          // of up to 16, 32, 48 rows
     std::vector<KvItem> tiles;
     std::vector<KvJoinItem> joins;
+    int join_rows = 0;                    // the most rows of one of them
     int64_t part_rows = 0;                // rows of partial results, of one key head
 };
 // Segments of up to kKvFew rows for a key head go to the kernel whose items are all of them, others to the tiles of 128 rows.
@@ -212,7 +213,10 @@ KvPlan plan_attention(const symb_kv_batch* b, const symb_kv_cache* c, int q_head
         walk(least, most, step, chunk, [&](int i, int rows, int r0, int c0, int n, int end) {
             const int parts = (int)((n + quota - 1) / quota);
             if (parts > 1)
-                for (int r = r0; r < std::min(r0 + step, rows); r += 16) plan.joins.push_back(KvJoinItem{b->seg_offsets[i], rows, r, (int32_t)(plan.part_rows + r - r0), parts, step});
+                for (int r = r0; r < std::min(r0 + step, rows); r += 16) {
+                    plan.joins.push_back(KvJoinItem{b->seg_offsets[i], rows, r, (int32_t)(plan.part_rows + r - r0), parts, step});
+                    plan.join_rows = std::max(plan.join_rows, std::min(16, rows - r));
+                }
             for (int k = 0; k < parts; ++k) {
                 const int from = c0 + (int)((int64_t)n * k / parts), to = c0 + (int)((int64_t)n * (k + 1) / parts);
                 items.push_back({i * b->table_stride, b->seg_offsets[i], rows, b->past[i], r0, from * chunk, k + 1 < parts ? to * chunk : end, parts > 1 ? (int32_t)plan.part_rows : -1});
@@ -262,7 +266,7 @@ symb_status launch_attention(symb_handle h, KvAttentionParams p, const KvPlan& p
         SYMB_HIP(h, hipGetLastError());
     }
     if (!plan.joins.empty()) {
-        hipLaunchKernelGGL((symb_kv_join_kernel<D>), dim3((unsigned)(plan.joins.size() * p.kv_heads)), dim3(256), 0, s, jp);
+        hipLaunchKernelGGL((symb_kv_join_kernel<D>), dim3((unsigned)(plan.joins.size() * p.kv_heads), plan.join_rows), dim3(256), 0, s, jp);
         SYMB_HIP(h, hipGetLastError());
     }
     return SYMB_OK;
@@ -340,7 +344,7 @@ symb_status symb_norm_bwd(symb_handle h, const symb_norm_batch* b, const void* X
         }
         if (!plan.groups.empty()) {
             const NormReduceParams p{part_w, part_b, (const NormGroup*)(dev + o_gr), b->width, flags == SYMB_GRAD_ACCUMULATE};
-            hipLaunchKernelGGL(symb_norm_reduce_kernel, dim3((b->width + 255) / 256, (unsigned)plan.groups.size()), dim3(256), 0, s, p);
+            hipLaunchKernelGGL(symb_norm_reduce_kernel, dim3((b->width + 63) / 64, (unsigned)plan.groups.size()), dim3(256), 0, s, p);
             SYMB_HIP(h, hipGetLastError());
         }
         guard.completed = true;
