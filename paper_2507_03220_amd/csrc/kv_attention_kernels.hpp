@@ -22,12 +22,12 @@
 namespace symb {
 
 // ---- up to 48 rows ----------------------------------------------------------------------------------------------------------------
-// In a chunk of 128 tokens, lane (n = lane % 16, g = lane / 16) gives
-//   left operand, keys    tile s (0..7): token kv_token(s, n), elements 16g .. 16g+15 and (head of 128) 64+16g .., its page's scale
+// In a chunk of 64 tokens, lane (n = lane % 16, g = lane / 16) gives
+//   left operand, keys    tile s (0..3): token kv_token(s, n), elements 16g .. 16g+15 and (head of 128) 64+16g .., its page's scale
 //   right operand         query row n, the same elements
-//   result                tokens kv_token(s, 4g + r), r = 0..3, of row n: with s = 0..3 the tokens 16g .. 16g+15, with s = 4..7 64+16g ..
-//   left operand, values  channel 16j + n, step q (0..3): tokens 64(q/2) + 16g + 8(q%2) .. +7, half of 16 bytes as they lie in the cache
-constexpr int kKvChunk = 128;             // tokens
+//   result                tokens kv_token(s, 4g + r), r = 0..3, of row n: all four tiles' are the tokens 16g .. 16g+15
+//   left operand, values  channel 16j + n, step q (0, 1): tokens 16g + 8q .. +7, half of 16 bytes as they lie in the cache
+constexpr int kKvChunk = 64;              // tokens
 // A row's weights are 2^(x - m) with an m that its largest x may exceed by up to this: the outputs need not be scaled whenever a larger score comes.  bf16 and fp32 hold the
 // weights just as well.
 constexpr float kKvSlack = 8.f;
@@ -59,7 +59,7 @@ struct KvAttentionParams {
     float scale, cap;                     // cap > 0: its value in log2 units, and scale / cap in `scale`; else scale in log2 units
 };
 
-__device__ __forceinline__ int kv_token(int s, int m) { return 16 * (m >> 2) + 4 * (s & 3) + (m & 3) + 64 * (s >> 2); }
+__device__ __forceinline__ int kv_token(int s, int m) { return 16 * (m >> 2) + 4 * s + (m & 3); }
 
 // Four values as two E4M3 terms each, hi + lo / 16.
 __device__ __forceinline__ void kv_two_terms(float a, float b, float c, float d, int& hi, int& lo) {
@@ -134,14 +134,19 @@ __device__ __forceinline__ float kv_score(const KvAttentionParams& p, float s) {
     return p.cap * (1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * 2.885390082f) + 1.f));
 }
 
-// The page of a token.  Only pages of the tokens lo .. hi-1 are looked up (others are hidden: any page will do); a number outside the pool is reported, and page 0
-// read in its place.
-__device__ __forceinline__ int kv_page(const KvAttentionParams& p, int table, int token, int lo, int hi, bool& bad) {
-    const int page = p.page_table[table + (max(min(token, hi - 1), lo) >> p.page_shift)];
+// The page of a token, the same in all lanes, so through the scalar cache: page numbers then arrive beside the keys and values under way, not behind them.  Only pages of the tokens
+// lo .. hi-1 are looked up (others are hidden: any page will do); a number outside the pool is reported, and page 0 read in its place.
+__device__ __forceinline__ int kv_look_up(const KvAttentionParams& p, int table, int token, int lo, int hi) {
+    typedef const __attribute__((address_space(4))) int32_t* Table;
+    return ((Table)(uintptr_t)p.page_table)[table + (max(min(token, hi - 1), lo) >> p.page_shift)];
+}
+__device__ __forceinline__ int kv_in_pool(const KvAttentionParams& p, int page, bool& bad) {
     const bool in = (unsigned)page < (unsigned)p.num_pages;
     bad |= !in;
     return in ? page : 0;
 }
+__device__ __forceinline__ int kv_page(const KvAttentionParams& p, int table, int token, int lo, int hi, bool& bad) { return kv_in_pool(p, kv_look_up(p, table, token, lo, hi), bad); }
+
 __device__ __forceinline__ float kv_scale(int byte) { return as_float(byte << 23); }
 // Eight E4M3 values times a power of two as bf16.
 __device__ __forceinline__ bf16x8 kv_widen(int a, int b, float scale) {
@@ -168,7 +173,8 @@ __device__ __forceinline__ int kv_nan_bytes(int w, int scale_byte) {
     return (int)((top >> 7) * 255u);
 }
 // Four wavefronts share an item's tokens, chunk by chunk, each for all of its R x 16 rows, and join through shared memory.  Keys and values go straight from memory into
-// registers: a wavefront has up to 32 KB on their way, keys of the next chunk asked for as soon as the scores of this one are formed.
+// registers, the next chunk's keys and this one's values while this one's scores are formed: up to 16 KB on their way in every wavefront, and two wavefronts a SIMD for up to
+// 16 rows, one for more.
 template <int D, int R, bool CAP>
 SYMB_KERNEL __launch_bounds__(256, R == 1 ? 2 : 1) void symb_kv_rows_kernel(KvAttentionParams p) {
     constexpr int kTiles = D / 16, kWords = D / 64;
@@ -201,69 +207,67 @@ SYMB_KERNEL __launch_bounds__(256, R == 1 ? 2 : 1) void symb_kv_rows_kernel(KvAt
 #pragma unroll
         for (int j = 0; j < kTiles; ++j) o[r][j] = floatx4{0, 0, 0, 0};
     }
+    struct Keys {
+        intx4 k[4][kWords];
+        int scale;
+    };
     const int in_page = (1 << p.page_shift) - 1;
-    for (int t0 = it.begin + wave * kKvChunk; t0 < it.end; t0 += 4 * kKvChunk) {
-        intx4 kb[8][kWords], vb[kTiles][2];
-        int kscale[2], vscale[2];
-        {
-            int kpage[2], vpage[2];
+    int page0, page1, next0, next1;                                // of a chunk's first and last 32 tokens, in the pool; numbers of the chunk whose keys are asked for next
+    auto look_up = [&](int t) {
+        next0 = kv_look_up(p, it.table, t, any_lo, it.end);
+        next1 = kv_look_up(p, it.table, t + 32, any_lo, it.end);
+    };
+    auto ask_keys = [&](Keys& c, int t0) {
+        page0 = kv_in_pool(p, next0, bad);
+        page1 = kv_in_pool(p, next1, bad);
+        look_up(t0 + 4 * kKvChunk);
+        const int64_t block = (int64_t)(n & 8 ? page1 : page0) * p.kv_heads + h;
+        const unsigned char* k = p.k + ((block << p.page_shift) + ((t0 + kv_token(0, n)) & in_page)) * D + 16 * g;
+        c.scale = p.k_scale[block];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int first = kv_page(p, it.table, t0 + 64 * u, any_lo, it.end, bad), second = kv_page(p, it.table, t0 + 64 * u + 32, any_lo, it.end, bad);     // (the same in all lanes)
-                kpage[u] = n & 8 ? second : first;
-                vpage[u] = g & 2 ? second : first;
-            }
+        for (int s = 0; s < 4; ++s)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int64_t block = (int64_t)kpage[u] * p.kv_heads + h;
-                const unsigned char* at = p.k + ((block << p.page_shift) + ((t0 + kv_token(4 * u, n)) & in_page)) * D + 16 * g;
-                kscale[u] = p.k_scale[block];
+            for (int w = 0; w < kWords; ++w) c.k[s][w] = *(const intx4*)(k + 4 * s * D + 64 * w);
+    };
+    intx4 v[kTiles];
+    int vscale;
+    auto ask_values = [&](int t0) {
+        const int64_t block = (int64_t)(g & 2 ? page1 : page0) * p.kv_heads + h;
+        const unsigned char* at = p.v + ((block * D + n) << p.page_shift) + ((t0 + 16 * g) & in_page);
+        vscale = p.v_scale[block];
 #pragma unroll
-                for (int s = 0; s < 4; ++s)
-#pragma unroll
-                    for (int w = 0; w < kWords; ++w) kb[4 * u + s][w] = *(const intx4*)(at + 4 * s * D + 64 * w);
-            }
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int64_t block = (int64_t)vpage[u] * p.kv_heads + h;
-                const unsigned char* at = p.v + ((block * D + n) << p.page_shift) + ((t0 + 64 * u + 16 * g) & in_page);
-                vscale[u] = p.v_scale[block];
-#pragma unroll
-                for (int j = 0; j < kTiles; ++j) vb[j][u] = *(const intx4*)(at + ((16 * j) << p.page_shift));
-            }
-        }
+        for (int j = 0; j < kTiles; ++j) v[j] = *(const intx4*)(at + ((16 * j) << p.page_shift));
+    };
+    auto work = [&](const Keys& c, int t0) {
         const bool whole = t0 >= all_lo && t0 + kKvChunk <= all_hi;                    // every row sees all of it
-        bf16x8 w[R][4];
+        bf16x8 w[R][2];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            floatx4 s[8];
+            floatx4 s[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int ks = kscale[i >> 2];
-                const intx8 a = __builtin_shufflevector(kb[i][0], kb[i][kWords - 1], 0, 1, 2, 3, 4, 5, 6, 7);
-                s[i] = kv_mfma(a, q[r].hi, floatx4{0, 0, 0, 0}, ks, q[r].hi_scale);
-                if constexpr (D == 128) s[i] = kv_mfma(a, q[r].lo, s[i], ks, q[r].lo_scale);
+            for (int i = 0; i < 4; ++i) {
+                const intx8 a = __builtin_shufflevector(c.k[i][0], c.k[i][kWords - 1], 0, 1, 2, 3, 4, 5, 6, 7);
+                s[i] = kv_mfma(a, q[r].hi, floatx4{0, 0, 0, 0}, c.scale, q[r].hi_scale);
+                if constexpr (D == 128) s[i] = kv_mfma(a, q[r].lo, s[i], c.scale, q[r].lo_scale);
             }
             if constexpr (CAP) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[i][e] = kv_score<true>(p, s[i][e]);
             }
             kv_settle();
             if (!whole) {
                 asm volatile("");                                  // (a branch: as a selection it would cost every chunk three instructions a score)
+                const int hi = see_hi[r] - t0 - 16 * g, lo = see_lo[r] - t0 - 16 * g;
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int t = t0 + kv_token(i, 4 * g + e);
-                        s[i][e] = t < see_hi[r] && t >= see_lo[r] ? s[i][e] : -INFINITY;
-                    }
+                    for (int e = 0; e < 4; ++e) s[i][e] = 4 * i + e < hi && 4 * i + e >= lo ? s[i][e] : -INFINITY;
             }
             float top = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) top = fmaxf(top, s[i][e]);
             const float factor = CAP ? 1.f : p.scale;              // (without a cap the scores stay as they are: it goes into the exponent)
@@ -279,62 +283,80 @@ SYMB_KERNEL __launch_bounds__(256, R == 1 ? 2 : 1) void symb_kv_rows_kernel(KvAt
             }
             const float base = m[r] == -INFINITY ? 0.f : -m[r];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     s[i][e] = __builtin_amdgcn_exp2f(s[i][e] * factor + base);
                     l[r] += s[i][e];
                 }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[r][i] = kv_pack8(s[2 * i][0], s[2 * i][1], s[2 * i][2], s[2 * i][3], s[2 * i + 1][0], s[2 * i + 1][1], s[2 * i + 1][2], s[2 * i + 1][3]);
-            __builtin_amdgcn_sched_barrier(0);                     // (one group's scores, two tiles' widened values at a time: all at once do not fit the registers)
+            for (int i = 0; i < 2; ++i) w[r][i] = kv_pack8(s[2 * i][0], s[2 * i][1], s[2 * i][2], s[2 * i][3], s[2 * i + 1][0], s[2 * i + 1][1], s[2 * i + 1][2], s[2 * i + 1][3]);
         }
         if (!whole) {
-            int keep[8], found = 0;
+            int keep[4], found = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) keep[i] = kv_keep_bytes(t0 + 64 * (i >> 2) + 16 * g + 4 * (i & 3), any_lo, any_hi);
+            for (int i = 0; i < 4; ++i) keep[i] = kv_keep_bytes(t0 + 16 * g + 4 * i, any_lo, any_hi);
 #pragma unroll
             for (int j = 0; j < kTiles; ++j)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    vb[j][i >> 2][i & 3] &= keep[i];
-                    found |= kv_nan_bytes(vb[j][i >> 2][i & 3], vscale[i >> 2]);
+                for (int i = 0; i < 4; ++i) {
+                    v[j][i] &= keep[i];
+                    found |= kv_nan_bytes(v[j][i], vscale);
                 }
             if (__any(found != 0)) {
 #pragma unroll
-                for (int j = 0; j < kTiles; ++j) {
-                    intx8 is;
+                for (int r = 0; r < R; ++r) {
+                    intx8 seen, is;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int nan = kv_nan_bytes(vb[j][i >> 2][i & 3], vscale[i >> 2]);
-                        is[i] = nan & 0x38383838;                  // (1)
-                        vb[j][i >> 2][i & 3] &= ~nan;
+                    for (int i = 0; i < 4; ++i) {
+                        seen[i] = 0x38383838 & kv_keep_bytes(t0 + 16 * g + 4 * i, see_lo[r], see_hi[r]);           // (1)
+                        seen[4 + i] = is[4 + i] = 0;
                     }
 #pragma unroll
-                    for (int r = 0; r < R; ++r) {
-                        intx8 seen;
+                    for (int j = 0; j < kTiles; ++j) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) seen[i] = 0x38383838 & kv_keep_bytes(t0 + 64 * (i >> 2) + 16 * g + 4 * (i & 3), see_lo[r], see_hi[r]);
+                        for (int i = 0; i < 4; ++i) is[i] = kv_nan_bytes(v[j][i], vscale) & 0x38383838;
                         const floatx4 cnt = kv_mfma(is, seen, floatx4{0, 0, 0, 0}, 127, 127);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[r][j][e] += cnt[e] != 0.f ? NAN : 0.f;
+                        __builtin_amdgcn_sched_barrier(0);         // (one at a time: registers)
                     }
-                    __builtin_amdgcn_sched_barrier(0);
                 }
+#pragma unroll
+                for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[j][i] &= ~kv_nan_bytes(v[j][i], vscale);
             }
         }
-        const float scale[2] = {kv_scale(vscale[0]), kv_scale(vscale[1])};
+        const float scale = kv_scale(vscale);
 #pragma unroll
         for (int j = 0; j < kTiles; ++j) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const bf16x8 v = kv_widen(vb[j][i >> 1][2 * (i & 1)], vb[j][i >> 1][2 * (i & 1) + 1], scale[i >> 1]);
+            for (int i = 0; i < 2; ++i) {
+                const bf16x8 b = kv_widen(v[j][2 * i], v[j][2 * i + 1], scale);
 #pragma unroll
-                for (int r = 0; r < R; ++r) o[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[r][i], o[r][j], 0, 0, 0);
+                for (int r = 0; r < R; ++r) o[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, w[r][i], o[r][j], 0, 0, 0);
             }
             if (j & 1) __builtin_amdgcn_sched_barrier(0);
         }
         kv_settle();                                               // (the next chunk may scale the outputs at once)
+    };
+    Keys even, odd;
+    int t0 = it.begin + wave * kKvChunk;
+    if (t0 < it.end) {
+        look_up(t0);
+        ask_keys(even, t0);
+    }
+    while (t0 < it.end) {
+        const int t1 = t0 + 4 * kKvChunk, t2 = t1 + 4 * kKvChunk;
+        ask_values(t0);
+        if (t1 < it.end) ask_keys(odd, t1);
+        work(even, t0);
+        if (t1 >= it.end) break;
+        ask_values(t1);
+        if (t2 < it.end) ask_keys(even, t2);
+        work(odd, t1);
+        t0 = t2;
     }
     // the four wavefronts' results: o 2^(m - M) added up, and so the sums
     const bool any_bad = __any(bad);

@@ -63,8 +63,9 @@ struct NormPlan {
     std::vector<NormGroup> groups;
     int parts = 0;
 };
-// Enough chunks to give every CU several workgroups, and no shorter than kNormRows rows while that holds: a chunk's partial sums cost as much traffic as a row and a third.
-constexpr int kNormChunks = 1024, kNormRows = 4;
+// Three workgroups a CU are on it together: one round of them, and no chunk shorter than kNormRows rows while that holds (a chunk's partial sums cost as much traffic as a row and a
+// third).  20480 rows of 4608: 512 chunks 134 us, 768 124, 1024 131, 2048 130; with bias 170, 142, 151, 150; 10240 rows of 4096 64, 61, 68, 66.
+constexpr int kNormChunks = 768, kNormRows = 4;
 symb_status plan_norm(symb_handle h, const symb_norm_batch* b, NormPlan& plan) {
     const int S = b->num_segments, T = b->seg_offsets[S];
     std::vector<int> order(S);
@@ -124,18 +125,18 @@ void launch_norm_fwd(const NormFwdParams& p, hipStream_t s) {
     if (vecs <= 1024) return launch_norm_fwd<RMS, 4, 4>(p, s);
     return launch_norm_fwd<RMS, 4, 8>(p, s);
 }
-template <bool RMS, int WAVES, int NV>
+template <bool RMS, bool BIAS, int WAVES, int NV>
 void launch_norm_bwd(const NormBwdParams& p, int chunks, hipStream_t s) {
-    hipLaunchKernelGGL((symb_norm_bwd_kernel<RMS, WAVES, NV>), dim3(chunks), dim3(WAVES * 64), 0, s, p);
+    hipLaunchKernelGGL((symb_norm_bwd_kernel<RMS, BIAS, WAVES, NV>), dim3(chunks), dim3(WAVES * 64), 0, s, p);
 }
-template <bool RMS>
+template <bool RMS, bool BIAS>
 void launch_norm_bwd(const NormBwdParams& p, int chunks, hipStream_t s) {
     const int vecs = p.width / 8;
-    if (vecs <= 256) return launch_norm_bwd<RMS, 4, 1>(p, chunks, s);
-    if (vecs <= 512) return launch_norm_bwd<RMS, 4, 2>(p, chunks, s);
-    if (vecs <= 768) return launch_norm_bwd<RMS, 4, 3>(p, chunks, s);
-    if (vecs <= 1024) return launch_norm_bwd<RMS, 4, 4>(p, chunks, s);
-    return launch_norm_bwd<RMS, 8, 4>(p, chunks, s);
+    if (vecs <= 256) return launch_norm_bwd<RMS, BIAS, 4, 1>(p, chunks, s);
+    if (vecs <= 512) return launch_norm_bwd<RMS, BIAS, 4, 2>(p, chunks, s);
+    if (vecs <= 768) return launch_norm_bwd<RMS, BIAS, 4, 3>(p, chunks, s);
+    if (vecs <= 1024) return launch_norm_bwd<RMS, BIAS, 4, 4>(p, chunks, s);
+    return launch_norm_bwd<RMS, BIAS, 8, 4>(p, chunks, s);
 }
 
 // ---- key/value cache --------------------------------------------------------------------------
@@ -192,8 +193,8 @@ struct KvPlan {
 };
 // Segments of up to kKvFew rows for a key head go to the kernel whose items are all of them, others to the tiles of 128 rows.
 constexpr int kKvFew = 48;
-// Workgroups that a launch should have, and chunks (128 tokens for 16 rows, 64 for a tile) that one of them takes at least: a shorter run costs more in joining than it gains.
-constexpr int kKvGroups = 1024, kKvLeast = 8, kKvTileGroups = 512, kKvTileLeast = 16;
+// Workgroups that a launch should have, and chunks of 64 tokens that one of them takes at least: a shorter run costs more in joining than it gains.
+constexpr int kKvGroups = 512, kKvLeast = 16, kKvTileGroups = 512, kKvTileLeast = 16;
 KvPlan plan_attention(const symb_kv_batch* b, const symb_kv_cache* c, int q_heads, int window) {
     KvPlan plan;
     const int group = q_heads / c->kv_heads;
@@ -338,8 +339,10 @@ symb_status symb_norm_bwd(symb_handle h, const symb_norm_batch* b, const void* X
         float *part_w = (float*)ws, *part_b = (float*)((unsigned char*)ws + part);
         if (T) {
             const NormBwdParams p{(const bf16*)X, (const bf16*)dY, (bf16*)dX, (const NormDesc*)(dev + o_nd), (const NormChunk*)(dev + o_ch), part_w, part_b, b->width, b->eps, b->weight_base};
-            if (b->kind == SYMB_NORM_RMS) launch_norm_bwd<true>(p, (int)plan.chunks.size(), s);
-            else launch_norm_bwd<false>(p, (int)plan.chunks.size(), s);
+            const int n = (int)plan.chunks.size();
+            const bool rms = b->kind == SYMB_NORM_RMS, bias = std::any_of(plan.groups.begin(), plan.groups.end(), [](const NormGroup& g) { return g.db; });
+            if (bias) rms ? launch_norm_bwd<true, true>(p, n, s) : launch_norm_bwd<false, true>(p, n, s);
+            else rms ? launch_norm_bwd<true, false>(p, n, s) : launch_norm_bwd<false, false>(p, n, s);
             SYMB_HIP(h, hipGetLastError());
         }
         if (!plan.groups.empty()) {
