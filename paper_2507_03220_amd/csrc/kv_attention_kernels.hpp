@@ -44,6 +44,7 @@ struct KvItem {
 
 struct KvAttentionParams {
     const KvItem* items;
+    int32_t tiles;                        // how many of them are tiles of 128 rows: the first ones
     const int32_t* page_table;
     const unsigned char* k;
     const unsigned char* v;
@@ -175,13 +176,16 @@ __device__ __forceinline__ int kv_nan_bytes(int w, int scale_byte) {
 // Four wavefronts share an item's tokens, chunk by chunk, each for all of its R x 16 rows, and join through shared memory.  Keys and values go straight from memory into
 // registers, the next chunk's keys and this one's values while this one's scores are formed: up to 16 KB on their way in every wavefront, and two wavefronts a SIMD for up to
 // 16 rows, one for more.
+template <int D, int R>
+struct KvRowsShared {
+    float join[4][16][D + 4];
+    float stat[R][4][16][2];
+};
 template <int D, int R, bool CAP>
-SYMB_KERNEL __launch_bounds__(256, R == 1 ? 2 : 1) void symb_kv_rows_kernel(KvAttentionParams p) {
+__device__ __forceinline__ void kv_rows(const KvAttentionParams& p, const KvItem& it, int h, KvRowsShared<D, R>& shared) {
     constexpr int kTiles = D / 16, kWords = D / 64;
-    __shared__ float join[4][16][D + 4];
-    __shared__ float stat[R][4][16][2];
-    const KvItem it = p.items[blockIdx.x / p.kv_heads];
-    const int h = blockIdx.x % p.kv_heads;
+    auto& join = shared.join;
+    auto& stat = shared.stat;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     // tokens that this lane's rows see; those that every row of the item sees, and those that some row does
     int see_hi[R], see_lo[R];
@@ -433,13 +437,18 @@ __device__ __forceinline__ float across_halves(float v, F f) {
 // rows: any 16 lanes meet all 64 banks once.
 __device__ __forceinline__ int kv_lds(int bytes, int row, int c) { return row * bytes + 16 * (c ^ (bytes == 128 ? (row >> 1) & 7 : (row >> 2) & 3)); }
 
+template <int D>
+struct KvTileShared {
+    unsigned char keys[2][64 * D], values[2][128 * D];
+    int noted[2];
+};
 template <int D, bool CAP>
-SYMB_KERNEL __launch_bounds__(256, 2) void symb_kv_tile_kernel(KvAttentionParams p) {
+__device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem& it, int h, KvTileShared<D>& shared) {
     constexpr int kHalves = D / 64, kTiles = D / 32, kVecs = D / 64;       // kVecs: vectors of keys (and of values) a thread moves a chunk
-    __shared__ __attribute__((aligned(16))) unsigned char keys[2][64 * D], values[2][128 * D];
-    __shared__ int noted[2];
-    const KvItem it = p.items[blockIdx.x / p.kv_heads];
-    const int h = blockIdx.x % p.kv_heads, tid = threadIdx.x;
+    auto& keys = shared.keys;
+    auto& values = shared.values;
+    auto& noted = shared.noted;
+    const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 31, g = lane >> 5;
     const int w0 = it.r0 + 32 * wave, r = w0 + n, pos = it.past + r / p.group;
     const bool valid = r < it.rows;
@@ -672,6 +681,26 @@ SYMB_KERNEL __launch_bounds__(256, 2) void symb_kv_tile_kernel(KvAttentionParams
 #pragma unroll
         for (int a = 0; a < 4; ++a)
             *(intx2*)(out + 32 * j + 8 * a + 4 * g) = intx2{(int)pack2_bf16(o[j][4 * a] * inv, o[j][4 * a + 1] * inv), (int)pack2_bf16(o[j][4 * a + 2] * inv, o[j][4 * a + 3] * inv)};
+}
+
+// Tiles, and items of up to 16 rows behind them, in one launch: both have two wavefronts a SIMD, and a batch of prompts and decode steps is done when the longer of the two is.
+template <int D, bool CAP>
+SYMB_KERNEL __launch_bounds__(256, 2) void symb_kv_attention_kernel(KvAttentionParams p) {
+    __shared__ union __attribute__((aligned(16))) {
+        KvTileShared<D> tile;
+        KvRowsShared<D, 1> rows;
+    } shared;
+    const int i = blockIdx.x / p.kv_heads, h = blockIdx.x % p.kv_heads;
+    const KvItem it = p.items[i];
+    if (i < p.tiles) kv_tile<D, CAP>(p, it, h, shared.tile);
+    else kv_rows<D, 1, CAP>(p, it, h, shared.rows);
+}
+// Items of 17 to 48 rows: one wavefront a SIMD.
+template <int D, int R, bool CAP>
+SYMB_KERNEL __launch_bounds__(256, 1) void symb_kv_rows_kernel(KvAttentionParams p) {
+    __shared__ KvRowsShared<D, R> shared;
+    const KvItem it = p.items[blockIdx.x / p.kv_heads];
+    kv_rows<D, R, CAP>(p, it, blockIdx.x % p.kv_heads, shared);
 }
 
 // The parts of up to 16 rows' results: part i of row r at partial row part0 + stride i + r.

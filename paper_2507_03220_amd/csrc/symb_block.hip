@@ -185,57 +185,91 @@ void launch_append(const KvAppendParams& p, int pages, bool few, int ny, hipStre
 
 // The work of one attention call.
 struct KvPlan {
-    std::vector<KvItem> rows[3];          // of up to 16, 32, 48 rows
-    std::vector<KvItem> tiles;
+    std::vector<KvItem> items[3];         // tiles and, behind them, items of up to 16 rows; items of up to 32 rows; of up to 48
+    int tiles = 0;
     std::vector<KvJoinItem> joins;
     int join_rows = 0;                    // the most rows of one of them
     int64_t part_rows = 0;                // rows of partial results, of one key head
 };
-// Segments of up to kKvFew rows for a key head go to the kernel whose items are all of them, others to the tiles of 128 rows.
-constexpr int kKvFew = 48;
-// Workgroups that a launch should have, and chunks of 64 tokens that one of them takes at least: a shorter run costs more in joining than it gains.
-constexpr int kKvGroups = 512, kKvLeast = 16, kKvTileGroups = 512, kKvTileLeast = 16;
+// The kernels of an attention call: runs of `rows` rows of the segments with more than `over` and up to `upto` rows for a key head.  Both go over the tokens in chunks of 64.
+struct KvKernel {
+    int rows;
+    int64_t over, upto;
+    int slots;                            // workgroups that run at once: two a CU, one with the registers of 17 rows and more
+    int worth;                            // chunks that a workgroup has to be spared for parts to pay
+};
+// Joining parts costs a launch and a pass over them, 4 to 5 us.  A chunk takes a workgroup's wavefront (one in four goes to each) 0.9 us with up to 16 rows, 1.6 and 2.5 with 32 and 48, and a
+// tile's workgroup 1.2 us.
+constexpr KvKernel kKvKernels[4] = {{128, 48, INT64_MAX, 512, 4}, {16, 0, 16, 512, 20}, {32, 16, 32, 256, 12}, {48, 32, 48, 256, 8}};
+static_assert(kKvChunk == kKvTileChunk, "");
+
+// Chunks that a workgroup takes: as few as keep all workgroups on the chip at once, where that is possible and spares the longest run enough; else all of a run's, and where the runs
+// alone are more than that, what leaves about that many.
+int64_t plan_quota(const std::vector<int32_t>& chunks, int kv_heads, const KvKernel& k) {
+    int64_t most = 1, sum = 0;
+    for (const int32_t n : chunks) {
+        most = std::max<int64_t>(most, n);
+        sum += n;
+    }
+    int64_t low = std::max<int64_t>((sum * kv_heads + k.slots - 1) / k.slots, 4), high = most;
+    if ((int64_t)chunks.size() * kv_heads <= k.slots)
+        for (int64_t at = low; at < high;) {              // (the fewest in [low, most]: a part of every run is one workgroup for each head)
+            const int64_t mid = (at + high) / 2;
+            int64_t parts = 0;
+            for (const int32_t n : chunks) parts += (n + mid - 1) / mid;
+            if (parts * kv_heads <= k.slots) high = low = mid;
+            else at = low = mid + 1;
+        }
+    return most - low < k.worth ? most : low;
+}
+
 KvPlan plan_attention(const symb_kv_batch* b, const symb_kv_cache* c, int q_heads, int window) {
     KvPlan plan;
     const int group = q_heads / c->kv_heads;
-    // f(segment, its rows, first row, first chunk, chunks, last token + 1) for runs of `step` rows of the segments with more than `least` and up to `most`
-    auto walk = [&](int64_t least, int64_t most, int step, int chunk, auto&& f) {
+    std::vector<KvItem> runs;
+    std::vector<int32_t> chunks;
+    for (int kind = 0; kind < 4; ++kind) {
+        const KvKernel& kernel = kKvKernels[kind];
+        runs.clear();
+        chunks.clear();
         for (int i = 0; i < b->num_segments; ++i) {
             const int64_t rows = (int64_t)(b->seg_offsets[i + 1] - b->seg_offsets[i]) * group;
-            if (rows <= least || rows > most) continue;
-            for (int64_t r0 = 0; r0 < rows; r0 += step) {
-                const int64_t first = b->past[i] + r0 / group, last = b->past[i] + std::min(r0 + step - 1, rows - 1) / group;
-                const int64_t lo = window ? std::max<int64_t>(first + 1 - window, 0) : 0, c0 = lo / chunk;
-                f(i, (int)rows, (int)r0, (int)c0, (int)((last + chunk) / chunk - c0), (int)last + 1);
+            if (rows <= kernel.over || rows > kernel.upto) continue;
+            for (int64_t r0 = 0; r0 < rows; r0 += kernel.rows) {
+                const int64_t first = b->past[i] + r0 / group, last = b->past[i] + std::min(r0 + kernel.rows - 1, rows - 1) / group;
+                const int64_t begin = window ? std::max<int64_t>(first + 1 - window, 0) / kKvChunk * kKvChunk : 0;
+                runs.push_back(KvItem{i * b->table_stride, b->seg_offsets[i], (int32_t)rows, b->past[i], (int32_t)r0, (int32_t)begin, (int32_t)last + 1, -1});
+                chunks.push_back((int32_t)((last + kKvChunk - begin) / kKvChunk));
             }
         }
-    };
-    auto fill = [&](int64_t least, int64_t most, int step, int chunk, int64_t quota, std::vector<KvItem>& items) {
-        walk(least, most, step, chunk, [&](int i, int rows, int r0, int c0, int n, int end) {
-            const int parts = (int)((n + quota - 1) / quota);
-            if (parts > 1)
-                for (int r = r0; r < std::min(r0 + step, rows); r += 16) {
-                    plan.joins.push_back(KvJoinItem{b->seg_offsets[i], rows, r, (int32_t)(plan.part_rows + r - r0), parts, step});
-                    plan.join_rows = std::max(plan.join_rows, std::min(16, rows - r));
-                }
-            for (int k = 0; k < parts; ++k) {
-                const int from = c0 + (int)((int64_t)n * k / parts), to = c0 + (int)((int64_t)n * (k + 1) / parts);
-                items.push_back({i * b->table_stride, b->seg_offsets[i], rows, b->past[i], r0, from * chunk, k + 1 < parts ? to * chunk : end, parts > 1 ? (int32_t)plan.part_rows : -1});
-                if (parts > 1) plan.part_rows += step;
+        if (runs.empty()) continue;
+        const int64_t quota = plan_quota(chunks, c->kv_heads, kernel);
+        std::vector<KvItem>& items = plan.items[std::max(kind - 1, 0)];
+        const size_t at = items.size();
+        for (size_t j = 0; j < runs.size(); ++j) {
+            const KvItem& run = runs[j];
+            const int n = chunks[j], parts = (int)((n + quota - 1) / quota);
+            if (parts <= 1) {
+                items.push_back(run);
+                continue;
             }
-        });
+            for (int r = run.r0; r < std::min(run.r0 + kernel.rows, run.rows); r += 16) {
+                plan.joins.push_back(KvJoinItem{run.row0, run.rows, r, (int32_t)(plan.part_rows + r - run.r0), parts, kernel.rows});
+                plan.join_rows = std::max(plan.join_rows, std::min(16, run.rows - r));
+            }
+            for (int k = 0; k < parts; ++k) {
+                KvItem it = run;
+                it.begin = run.begin + (int)((int64_t)n * k / parts) * kKvChunk;
+                if (k + 1 < parts) it.end = run.begin + (int)((int64_t)n * (k + 1) / parts) * kKvChunk;
+                it.part = (int32_t)plan.part_rows;
+                plan.part_rows += kernel.rows;
+                items.push_back(it);
+            }
+        }
         // the longest first: what is left over at the end is short
-        std::stable_sort(items.begin(), items.end(), [](const auto& x, const auto& y) { return x.end - x.begin > y.end - y.begin; });
-    };
-    // chunks a workgroup: as many as leave `groups` workgroups
-    auto quota = [&](int64_t least, int64_t most, int step, int chunk, int groups, int at_least) {
-        int64_t chunks = 0;
-        walk(least, most, step, chunk, [&](int, int, int, int, int n, int) { chunks += n; });
-        return std::max<int64_t>(at_least, (chunks * c->kv_heads + groups - 1) / groups);
-    };
-    const int64_t few = quota(0, kKvFew, kKvFew, kKvChunk, kKvGroups, kKvLeast);
-    for (int r = 0; r < 3; ++r) fill(16 * r, 16 * (r + 1), 16 * (r + 1), kKvChunk, few, plan.rows[r]);
-    fill(kKvFew, INT64_MAX, kKvTileRows, kKvTileChunk, quota(kKvFew, INT64_MAX, kKvTileRows, kKvTileChunk, kKvTileGroups, kKvTileLeast), plan.tiles);
+        std::stable_sort(items.begin() + at, items.end(), [](const KvItem& x, const KvItem& y) { return x.end - x.begin > y.end - y.begin; });
+        if (kind == 0) plan.tiles = (int)items.size();
+    }
     return plan;
 }
 size_t part_ml_bytes(const KvPlan& plan, int kv_heads) { return align_up((size_t)plan.part_rows * kv_heads * 2 * sizeof(float), 256); }
@@ -254,16 +288,15 @@ symb_status check_attention(symb_handle h, const symb_kv_batch* b, const symb_kv
 }
 
 template <int D, bool CAP>
-symb_status launch_attention(symb_handle h, KvAttentionParams p, const KvPlan& plan, const KvItem* const (&items)[4], const KvJoinParams& jp, hipStream_t s) {
-    for (int i = 0; i < 4; ++i) {
-        const size_t n = i < 3 ? plan.rows[i].size() : plan.tiles.size();
-        if (!n) continue;
+symb_status launch_attention(symb_handle h, KvAttentionParams p, const KvPlan& plan, const KvItem* const (&items)[3], const KvJoinParams& jp, hipStream_t s) {
+    for (int i = 0; i < 3; ++i) {
+        if (plan.items[i].empty()) continue;
         p.items = items[i];
-        const dim3 grid((unsigned)(n * p.kv_heads));
-        if (i == 0) hipLaunchKernelGGL((symb_kv_rows_kernel<D, 1, CAP>), grid, dim3(256), 0, s, p);
+        p.tiles = i ? 0 : plan.tiles;
+        const dim3 grid((unsigned)(plan.items[i].size() * p.kv_heads));
+        if (i == 0) hipLaunchKernelGGL((symb_kv_attention_kernel<D, CAP>), grid, dim3(256), 0, s, p);
         else if (i == 1) hipLaunchKernelGGL((symb_kv_rows_kernel<D, 2, CAP>), grid, dim3(256), 0, s, p);
-        else if (i == 2) hipLaunchKernelGGL((symb_kv_rows_kernel<D, 3, CAP>), grid, dim3(256), 0, s, p);
-        else hipLaunchKernelGGL((symb_kv_tile_kernel<D, CAP>), grid, dim3(256), 0, s, p);
+        else hipLaunchKernelGGL((symb_kv_rows_kernel<D, 3, CAP>), grid, dim3(256), 0, s, p);
         SYMB_HIP(h, hipGetLastError());
     }
     if (!plan.joins.empty()) {
@@ -457,13 +490,13 @@ symb_status symb_kv_attention(symb_handle h, const symb_kv_batch* b, const symb_
         const size_t need = part_bytes(plan, cache);
         if (need && (!ws || ws_bytes < need)) return fail(h, SYMB_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : 0, need);
         if (need && misaligned16(ws)) return fail(h, SYMB_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
-        size_t work = plan.tiles.size() + plan.joins.size();
-        for (const auto& r : plan.rows) work += r.size();
+        size_t work = plan.joins.size();
+        for (const auto& r : plan.items) work += r.size();
         if ((int64_t)work * cache->kv_heads > INT32_MAX || plan.part_rows > INT32_MAX) return fail(h, SYMB_ERR_UNSUPPORTED, "%zu work items of %d key heads", work, cache->kv_heads);
         hipStream_t s = (hipStream_t)stream;
         Blob blob;
-        size_t o_items[4];
-        for (int i = 0; i < 4; ++i) o_items[i] = i < 3 ? blob.add(plan.rows[i].data(), plan.rows[i].size()) : blob.add(plan.tiles.data(), plan.tiles.size());
+        size_t o_items[3];
+        for (int i = 0; i < 3; ++i) o_items[i] = blob.add(plan.items[i].data(), plan.items[i].size());
         const size_t o_join = blob.add(plan.joins.data(), plan.joins.size());
         unsigned char* dev = nullptr;
         if ((st = upload(h, blob, s, &dev)) != SYMB_OK) return st;
@@ -489,7 +522,7 @@ symb_status symb_kv_attention(symb_handle h, const symb_kv_batch* b, const symb_
         p.scale = cap > 0.f ? scale / cap : scale * kLog2e;
         p.cap = cap * kLog2e;
         const KvJoinParams jp{(const KvJoinItem*)(dev + o_join), p.part_o, p.part_ml, p.out, out_stride, p.kv_heads, p.group, p.part_rows};
-        const KvItem* const items[4] = {(const KvItem*)(dev + o_items[0]), (const KvItem*)(dev + o_items[1]), (const KvItem*)(dev + o_items[2]), (const KvItem*)(dev + o_items[3])};
+        const KvItem* const items[3] = {(const KvItem*)(dev + o_items[0]), (const KvItem*)(dev + o_items[1]), (const KvItem*)(dev + o_items[2])};
         if (D == 128) st = cap > 0.f ? launch_attention<128, true>(h, p, plan, items, jp, s) : launch_attention<128, false>(h, p, plan, items, jp, s);
         else st = cap > 0.f ? launch_attention<64, true>(h, p, plan, items, jp, s) : launch_attention<64, false>(h, p, plan, items, jp, s);
         if (st != SYMB_OK) return st;

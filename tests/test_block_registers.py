@@ -56,7 +56,7 @@ def _next(code, labels, i):
 
 def test_results_of_matrix_instructions_are_waited_for(block_asm):
     checked = 0
-    for name, code, labels in _kernels(block_asm, r"symb_kv_(?:rows|tile)_kernel"):
+    for name, code, labels in _kernels(block_asm, r"symb_kv_(?:rows|attention)_kernel"):
         touched = [_regs(c.partition(" ")[2]) if not c.startswith(("s_", "ds_nop")) else set() for c in code]
         for i, c in enumerate(code):
             op, _, rest = c.partition(" ")
