@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB = os.path.join(HERE, "libsymb.so")
@@ -30,15 +31,26 @@ def build(force: bool = True, verbose: bool = False) -> str:
         return LIB
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     tmp = LIB + f".tmp{os.getpid()}"
-    cmd = [hipcc] + FLAGS + ["-o", tmp] + SOURCES
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    err = "\n".join(l for l in r.stderr.splitlines() if "packed-fp32-ops" not in l and l.strip())
-    if r.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + err)
-    if err and verbose:
-        print(err, file=sys.stderr)
+    flags = [f for f in FLAGS if f != "-shared"]
+    objects = [f"{tmp}.{i}.o" for i in range(len(SOURCES))]
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        err = "\n".join(l for l in r.stderr.splitlines() if "packed-fp32-ops" not in l and l.strip())
+        if r.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + err)
+        if err and verbose:
+            print(err, file=sys.stderr)
+    try:
+        with ThreadPoolExecutor(len(SOURCES)) as ex:
+            list(ex.map(lambda so: run([hipcc] + flags + ["-c", "-o", so[1], so[0]]), zip(SOURCES, objects)))
+        run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp] + objects)
+    finally:
+        for o in objects:
+            if os.path.exists(o):
+                os.remove(o)
     os.replace(tmp, LIB)
     return LIB
 

@@ -1,0 +1,114 @@
+"""The operators around the shared projections run together as a client's block uses them (paper_2507_03220_amd/block.py), against the 64-bit oracle of every step."""
+import numpy as np
+import pytest
+import torch
+
+import gpu_harness as gh
+import oracle
+from block_harness import bf16, host, offsets, stream
+from helpers import assert_close
+from oracle import block as ob
+from paper_2507_03220_amd import binding as sb
+from paper_2507_03220_amd import block as blk
+
+pytestmark = pytest.mark.gpu
+
+
+def _lora(rng, d_in, d_out, r, grads=False):
+    a = sb.Adapter(sb.SYMB_ADAPTER_LORA, r, 1.5, bf16(rng, r, d_in, std=d_in ** -0.5), bf16(rng, d_out, r, std=r ** -0.5))
+    if grads:
+        a.dA, a.dB = torch.full((r, d_in), float("nan"), device="cuda"), torch.full((d_out, r), float("nan"), device="cuda")
+    return a
+
+
+def test_a_fine_tuning_step_through_norm_and_projection():
+    rng = np.random.default_rng(1)
+    width, d_out, lens = 256, 384, [70, 3, 0, 129]
+    off = offsets(lens)
+    W, X, dY = bf16(rng, d_out, width, std=width ** -0.5), bf16(rng, 202, width, mean=0.3), bf16(rng, 202, d_out)
+    norms = [sb.Norm(bf16(rng, width, std=0.1, mean=1.0), bf16(rng, width, std=0.1), torch.empty(width, device="cuda"), torch.empty(width, device="cuda")) for _ in lens]
+    ads = [_lora(rng, width, d_out, r, True) for r in (8, 16, 4, 5)]
+    run = blk.NormedProjection(gh.handle(), W, lens, norms, ads)
+    run.forward(X, None, stream())
+    run.backward(X, dY, stream=stream())
+    torch.cuda.synchronize()
+    w, b = [host(n.weight) for n in norms], [host(n.bias) for n in norms]
+    # every step against its own definition on what it was given: the projections' bar is the one of tests/helpers.py
+    bits = gh.bf16_bits
+    oads = [oracle.Adapter(oracle.LORA, a.rank, a.scale, bits(a.A), bits(a.B)) for a in ads]
+    _, Yr = oracle.forward(off.astype(np.int32), oads, bits(run.N), bits(W))
+    assert_close(gh.bf16_to_f64(run.Y), Yr, "Y", out_bf16=True)
+    dNr = oracle.backward_input(off.astype(np.int32), oads, bits(dY), bits(W))
+    assert_close(gh.bf16_to_f64(run.dN), dNr, "dN", out_bf16=True)
+    want = ob.norm_fwd(off, host(X), w, b, True, 1e-5, 0.0)
+    np.testing.assert_allclose(host(run.N), want, rtol=2.0 ** -8, atol=1e-4)
+    dX, dw, db = ob.norm_bwd(off, host(X), host(run.dN), w, True, 1e-5, 0.0)
+    np.testing.assert_allclose(host(run.dX), dX, rtol=2.0 ** -8, atol=1e-3)
+    for i, n in enumerate(norms):
+        np.testing.assert_allclose(host(n.dweight), dw[i], rtol=1e-5, atol=1e-3)
+        np.testing.assert_allclose(host(n.dbias), db[i], rtol=1e-5, atol=1e-3)
+    # and the whole chain in 64 bits: two roundings to bf16 on the way, 2^-9 each of a tensor at most
+    chain, _, _ = ob.norm_bwd(off, host(X), dNr, w, True, 1e-5, 0.0)
+    assert np.linalg.norm(host(run.dX) - chain) / np.linalg.norm(chain) < 6e-3
+
+
+def test_prompts_and_decode_steps_of_many_clients():
+    """Prompts at once, then decode steps in changing company, then a prompt beside a decode step: each client's outputs are those of its own sequence, computed in 64 bits from the
+    cache that the block wrote."""
+    rng = np.random.default_rng(2)
+    width, heads, H, D, P = 256, 4, 2, 64, 32
+    W = {p: bf16(rng, o, i, std=i ** -0.5) for p, o, i in (("q", heads * D, width), ("k", H * D, width), ("v", H * D, width), ("o", width, heads * D))}
+    cache = sb.KvCache.empty(40, H, D, P)
+    table = blk.rotation_table(400, D)
+    block = blk.AttentionBlock(gh.handle(), W, heads, cache, sb.Rotation(table), window=90, cap=20.0)
+    clients = [blk.Client(sb.Norm(bf16(rng, width, std=0.1, mean=1.0)), {"q": _lora(rng, width, heads * D, 8), "v": _lora(rng, width, H * D, 4)}) for _ in range(4)]
+    fed = [[] for _ in clients]
+
+    def lin(x, p, c):
+        y = x @ host(W[p]).T
+        a = c.adapters.get(p)
+        return y if a is None else y + a.scale * (x @ host(a.A).T) @ host(a.B).T
+
+    def step(who, lens):
+        X = bf16(rng, sum(lens), width)
+        out = host(block.forward(X, lens, [clients[i] for i in who], stream()))
+        at = 0
+        for i, n in zip(who, lens):
+            c, x = clients[i], host(X[at:at + n])
+            fed[i].append(x)
+            if n:
+                pos = np.arange(c.past - n, c.past)
+                y = ob.norm_fwd([0, n], x, [host(c.norm.weight)], [None], False, 1e-6, 0.0)
+                q = ob.turn(lin(y, "q", c).reshape(n, heads, D), host(table), pos, D, False)
+                pages = torch.tensor(c.pages[:-(-c.past // P)]).cuda()
+                u8 = lambda t: t.view(torch.uint8)[pages]  # noqa: E731
+                K = host(u8(cache.k).view(torch.float8_e4m3fn)) * 2.0 ** (u8(cache.k_scale).cpu().numpy()[:, :, None, None].astype(float) - 127)
+                V = host(u8(cache.v).view(torch.float8_e4m3fn)) * 2.0 ** (u8(cache.v_scale).cpu().numpy()[:, :, None, None].astype(float) - 127)
+                K, V = K.transpose(0, 2, 1, 3).reshape(-1, H, D)[:c.past], V.transpose(0, 3, 1, 2).reshape(-1, H, D)[:c.past]
+                # the cache holds this step's keys: 2^-4 of each at most (E4M3), of a tensor a fortieth
+                k = ob.turn(lin(y, "k", c).reshape(n, H, D), host(table), pos, D, False)
+                assert np.linalg.norm(K[-n:] - k) / np.linalg.norm(k) < 0.04
+                att, _, _ = ob.attention([0, n], [c.past - n], [K], [V], q, D ** -0.5, 90, 20.0)
+                want = att.reshape(n, -1) @ host(W["o"]).T
+                # normed rows, queries and outputs are rounded to bf16 (2^-9 of a tensor), weights too; scores of size 2 or so move by 2^-8
+                rel = np.linalg.norm(out[at:at + n] - want) / np.linalg.norm(want)
+                assert rel < 1.5e-2, (i, rel)
+            at += n
+    step([0, 1, 2], [70, 33, 1])
+    step([2, 0, 1], [1, 1, 1])
+    step([0, 3, 1, 2], [1, 130, 0, 40])
+    for _ in range(3):
+        step([3, 2, 1, 0], [1, 1, 1, 1])
+    used = sum(len(c.pages) for c in clients)
+    assert len(block.free) == 40 - used and [c.past for c in clients] == [75, 37, 45, 133]
+    block.release(clients[0])
+    assert clients[0].past == 0 and len(block.free) == 40 - used + 3
+
+
+def test_the_example_runs():
+    import os
+    import subprocess
+    import sys
+    r = subprocess.run([sys.executable, "-m", "paper_2507_03220_amd.block"], capture_output=True, text=True, timeout=100, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0, r.stderr[-2000:]
+    assert "prompts" in r.stdout and "decode steps" in r.stdout and "fine-tuning" in r.stdout
