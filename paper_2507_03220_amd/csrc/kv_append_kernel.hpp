@@ -1,9 +1,12 @@
 // New keys and values into the paged 8-bit cache, keys and queries turned by their positions.
 //
-// One workgroup takes one page's share of a segment for one head: of the keys, of the values, or the queries of the same rows.  It holds the new
+// One workgroup takes one page's share of a segment for one head: of the keys or of the values; or the queries of the same rows, of one head (64 threads) or eight.  It holds the new
 // values in registers (fp32, turned), forms their largest magnitude, from it the page's scale 2^e with max / 2^e in (224, 448], and rounds once.  If the
 // page holds earlier tokens and its scale grows, those are read, scaled by the power of two that the scale grew by and held again.  Bound by memory: a new
-// key or value costs 2 bytes in and 1 out, a query 2 and 2.
+// key or value costs 2 bytes in and 1 out, a query 2 and 2, and the angles 4 for each element of a row unless several heads share what was loaded.
+// Measured: 8000 rows of 32 query and 32 key heads of 128 without turning (328 MB) in 69 us, 4.75 TB/s of the 4.93 that a large copy reaches; 6009 rows of 32 query and 16 key heads (175 MB) in 42 us where eight query
+// heads share the angles, 45 with one and 48 with sixteen (too few workgroups); 48 us also where the queries come behind the keys in the grid.  A decode step's call
+// is a launch, 10 to 11 us with the host's part.
 #pragma once
 #include "block_device.hpp"
 
@@ -30,15 +33,27 @@ struct KvAppendParams {
     int64_t q_stride, q_out_stride, k_stride, v_stride;
     int32_t num_pages, kv_heads, q_heads, page_shift;
     int32_t turned, adjacent;             // elements of a head that are turned; pairs side by side instead of half of them apart
-    int32_t heads_q;                      // query heads a workgroup
+    int32_t heads_q, q_groups;            // query heads a workgroup, workgroups for them
 };
 
 // Sixteen elements of a head's row, `slot` 0 .. D/16-1, in two chunks of eight that hold whole pairs.
 __device__ __forceinline__ bool kv_slot_halves(const KvAppendParams& p, int slot, bool turn) { return turn && slot * 16 < p.turned && !p.adjacent; }
 __device__ __forceinline__ int kv_chunk0(const KvAppendParams& p, int slot, bool turn) { return kv_slot_halves(p, slot, turn) ? slot : 2 * slot; }
 __device__ __forceinline__ int kv_chunk1(const KvAppendParams& p, int slot, bool turn) { return kv_slot_halves(p, slot, turn) ? slot + (p.turned >> 4) : 2 * slot + 1; }
-__device__ __forceinline__ void kv_load16(const KvAppendParams& p, const bf16* row, int slot, int pos, bool turn, float (&x)[16]) {
-    const intx4 a = *(const intx4*)(row + kv_chunk0(p, slot, turn) * 8), b = *(const intx4*)(row + kv_chunk1(p, slot, turn) * 8);
+struct KvAngles {                         // of a slot's eight pairs
+    float c[8], s[8];
+};
+__device__ __forceinline__ bool kv_turned(const KvAppendParams& p, int slot, bool turn) { return turn && slot * 16 < p.turned; }
+__device__ __forceinline__ void kv_angles(const KvAppendParams& p, int slot, int pos, KvAngles& a) {
+    const float* cs = p.rotation + (int64_t)pos * p.turned + slot * 8;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const floatx4 u = *(const floatx4*)(cs + 4 * h), w = *(const floatx4*)(cs + (p.turned >> 1) + 4 * h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a.c[4 * h + i] = u[i], a.s[4 * h + i] = w[i];
+    }
+}
+__device__ __forceinline__ void kv_turn(const KvAppendParams& p, const intx4 a, const intx4 b, int slot, bool turn, const KvAngles& t, float (&x)[16]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         x[2 * i] = bf16_lo((unsigned)a[i]);
@@ -46,21 +61,13 @@ __device__ __forceinline__ void kv_load16(const KvAppendParams& p, const bf16* r
         x[8 + 2 * i] = bf16_lo((unsigned)b[i]);
         x[8 + 2 * i + 1] = bf16_hi((unsigned)b[i]);
     }
-    if (!turn || slot * 16 >= p.turned) return;
-    const float* cs = p.rotation + (int64_t)pos * p.turned + slot * 8;
-    float c[8], s[8];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const floatx4 u = *(const floatx4*)(cs + 4 * h), w = *(const floatx4*)(cs + (p.turned >> 1) + 4 * h);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) c[4 * h + i] = u[i], s[4 * h + i] = w[i];
-    }
+    if (!kv_turned(p, slot, turn)) return;
     float u[8], w[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float first = p.adjacent ? x[2 * i] : x[i], second = p.adjacent ? x[2 * i + 1] : x[8 + i];
-        u[i] = first * c[i] - second * s[i];
-        w[i] = second * c[i] + first * s[i];
+        u[i] = first * t.c[i] - second * t.s[i];
+        w[i] = second * t.c[i] + first * t.s[i];
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = p.adjacent ? (i & 1 ? w[i >> 1] : u[i >> 1]) : (i < 8 ? u[i] : w[i - 8]);
@@ -83,24 +90,39 @@ SYMB_KERNEL __launch_bounds__(THREADS) void symb_kv_append_kernel(KvAppendParams
     const KvPage pg = p.pages[blockIdx.x];
     const int tid = threadIdx.x, P = 1 << p.page_shift;
     int y = blockIdx.y;
-    if (y >= 2 * p.kv_heads) {                                     // queries of the same rows
-        const int h0 = (y - 2 * p.kv_heads) * p.heads_q, nh = min(p.heads_q, p.q_heads - h0);
-        for (int i = tid; i < pg.rows * nh * kSlots; i += THREADS) {
-            const int slot = i % kSlots, hr = i / kSlots, h = h0 + hr % nh, r = hr / nh;
-            float x[16];
-            kv_load16(p, p.q_in + (int64_t)(pg.row0 + r) * p.q_stride + h * D, slot, pg.pos0 + r, true, x);
-            bf16* out = p.q_out + (int64_t)(pg.row0 + r) * p.q_out_stride + h * D;
-            intx4 a, b;
+    constexpr int kHeads = THREADS == 64 ? 1 : 4;
+    if (y < p.q_groups) {                                          // queries of the same rows, and of several heads: the angles of a row are the same for all
+        const int h0 = y * p.heads_q, nh = min(p.heads_q, p.q_heads - h0);
+        for (int i = tid; i < pg.rows * kSlots; i += THREADS) {
+            const int slot = i % kSlots, r = i / kSlots;
+            KvAngles t;
+            if (kv_turned(p, slot, true)) kv_angles(p, slot, pg.pos0 + r, t);
+            const bf16* in = p.q_in + (int64_t)(pg.row0 + r) * p.q_stride + h0 * D;
+            bf16* out = p.q_out + (int64_t)(pg.row0 + r) * p.q_out_stride + h0 * D;
+            const int c0 = kv_chunk0(p, slot, true) * 8, c1 = kv_chunk1(p, slot, true) * 8;
+            for (int h = 0; h < nh; h += kHeads, in += kHeads * D, out += kHeads * D) {
+                intx4 a[kHeads], b[kHeads];                        // (all loads first: q_out may be q, so the compiler may not move them over a store)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                a[j] = (int)pack2_bf16(x[2 * j], x[2 * j + 1]);
-                b[j] = (int)pack2_bf16(x[8 + 2 * j], x[8 + 2 * j + 1]);
+                for (int k = 0; k < kHeads; ++k)
+                    if (h + k < nh) a[k] = *(const intx4*)(in + k * D + c0), b[k] = *(const intx4*)(in + k * D + c1);
+#pragma unroll
+                for (int k = 0; k < kHeads; ++k) {
+                    if (h + k >= nh) break;
+                    float x[16];
+                    kv_turn(p, a[k], b[k], slot, true, t, x);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        a[k][j] = (int)pack2_bf16(x[2 * j], x[2 * j + 1]);
+                        b[k][j] = (int)pack2_bf16(x[8 + 2 * j], x[8 + 2 * j + 1]);
+                    }
+                    *(intx4*)(out + k * D + c0) = a[k];
+                    *(intx4*)(out + k * D + c1) = b[k];
+                }
             }
-            *(intx4*)(out + kv_chunk0(p, slot, true) * 8) = a;
-            *(intx4*)(out + kv_chunk1(p, slot, true) * 8) = b;
         }
         return;
     }
+    y -= p.q_groups;
     const int page = p.page_table[pg.table];
     if ((unsigned)page >= (unsigned)p.num_pages) return;           // (no such page: nothing is stored)
     const bool is_v = y >= p.kv_heads;
@@ -118,7 +140,10 @@ SYMB_KERNEL __launch_bounds__(THREADS) void symb_kv_append_kernel(KvAppendParams
     for (int q = 0; q < kPasses; ++q) {
         const int i = q * THREADS + tid;
         if (i < ntask) {
-            kv_load16(p, rows + (i / kSlots) * stride, i % kSlots, pg.pos0 + i / kSlots, !is_v, x[q]);
+            KvAngles t;
+            if (kv_turned(p, i % kSlots, !is_v)) kv_angles(p, i % kSlots, pg.pos0 + i / kSlots, t);
+            const bf16* row = rows + (i / kSlots) * stride;
+            kv_turn(p, *(const intx4*)(row + kv_chunk0(p, i % kSlots, !is_v) * 8), *(const intx4*)(row + kv_chunk1(p, i % kSlots, !is_v) * 8), i % kSlots, !is_v, t, x[q]);
 #pragma unroll
             for (int j = 0; j < 16; ++j) amax = fmaxf(amax, finite_abs(x[q][j]));
         }

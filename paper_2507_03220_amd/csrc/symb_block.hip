@@ -423,8 +423,8 @@ symb_status symb_kv_append(symb_handle h, const symb_kv_batch* b, const symb_kv_
                 at += take;
             }
         const bool few = rows <= kKvFewRows;
-        const int heads_q = std::max(1, (few ? 64 : 256) / (rows * (D / 16)));
-        const int64_t ny = 2 * (int64_t)cache->kv_heads + (q_heads + heads_q - 1) / heads_q;
+        const int heads_q = few ? 1 : 8, q_groups = (q_heads + heads_q - 1) / heads_q;
+        const int64_t ny = 2 * (int64_t)cache->kv_heads + q_groups;
         if (ny > 65535) return fail(h, SYMB_ERR_UNSUPPORTED, "%d query heads beside %d key heads", q_heads, cache->kv_heads);
         hipStream_t s = (hipStream_t)stream;
         Blob blob;
@@ -454,6 +454,7 @@ symb_status symb_kv_append(symb_handle h, const symb_kv_batch* b, const symb_kv_
         p.turned = rotation ? rotation->dim : 0;
         p.adjacent = rotation && rotation->pairs == SYMB_ROTATE_ADJACENT;
         p.heads_q = heads_q;
+        p.q_groups = q_groups;
         if (D == 128) launch_append<128>(p, (int)pages.size(), few, (int)ny, s);
         else launch_append<64>(p, (int)pages.size(), few, (int)ny, s);
         SYMB_HIP(h, hipGetLastError());
