@@ -185,13 +185,13 @@ void launch_append(const KvAppendParams& p, int pages, bool few, int ny, hipStre
 
 // The work of one attention call.
 struct KvPlan {
-    std::vector<KvItem> items[3];         // tiles and, behind them, items of up to 16 rows; items of up to 32 rows; of up to 48
+    std::vector<KvItem> items[3];         // tiles and, behind them, items of up to 16 rows; items of 32 rows; of 48
     int tiles = 0;
     std::vector<KvJoinItem> joins;
     int join_rows = 0;                    // the most rows of one of them
     int64_t part_rows = 0;                // rows of partial results, of one key head
 };
-// The kernels of an attention call: runs of `rows` rows of the segments with more than `over` and up to `upto` rows for a key head.  Both go over the tokens in chunks of 64.
+// The kernels of an attention call: runs of `rows` rows of the segments with more than `over` and up to `upto` rows for a key head.  All go over the tokens in chunks of 64.
 struct KvKernel {
     int rows;
     int64_t over, upto;
@@ -202,6 +202,10 @@ struct KvKernel {
 // tile's workgroup 1.2 us.
 constexpr KvKernel kKvKernels[4] = {{128, 48, INT64_MAX, 512, 4}, {16, 0, 16, 512, 20}, {32, 16, 32, 256, 12}, {48, 32, 48, 256, 8}};
 static_assert(kKvChunk == kKvTileChunk, "");
+// Up to 48 rows in one workgroup widen the values once instead of three times, but are a launch of their own, with a third of the workgroups.  Where all that they would do is less than this many
+// chunks of 16 rows, segments of 17 to 48 rows go 16 rows at a time into the first launch.  Both sides (48 query heads on one key head): 91 chunks 15.0 us with 48 rows, 9.4 with 16; 4850 22.6, 21.3;
+// 14400 32.4, 43; 35800 52.5, 87.6.  (32 key heads): 7700 30.5, 24.0; 17700 39.4, 35.9; 43600 77.4, 82.4.
+constexpr int64_t kKvWideWork = 12288;
 
 // Chunks that a workgroup takes: as few as keep all workgroups on the chip at once, where that is possible and spares the longest run enough; else all of a run's, and where the runs
 // alone are more than that, what leaves about that many.
@@ -228,8 +232,19 @@ KvPlan plan_attention(const symb_kv_batch* b, const symb_kv_cache* c, int q_head
     const int group = q_heads / c->kv_heads;
     std::vector<KvItem> runs;
     std::vector<int32_t> chunks;
+    int64_t wide = 0;
+    for (int i = 0; i < b->num_segments; ++i) {
+        const int64_t n = b->seg_offsets[i + 1] - b->seg_offsets[i], rows = n * group;
+        if (rows <= kKvKernels[1].upto || rows > kKvKernels[3].upto) continue;
+        const int64_t begin = window ? std::max<int64_t>((int64_t)b->past[i] + 1 - window, 0) / kKvChunk * kKvChunk : 0;
+        wide += (b->past[i] + n + kKvChunk - 1 - begin) / kKvChunk * ((rows + 15) / 16) * c->kv_heads;
+    }
     for (int kind = 0; kind < 4; ++kind) {
-        const KvKernel& kernel = kKvKernels[kind];
+        KvKernel kernel = kKvKernels[kind];
+        if (kind && wide < kKvWideWork) {
+            if (kind > 1) break;
+            kernel.upto = kKvKernels[3].upto;
+        }
         runs.clear();
         chunks.clear();
         for (int i = 0; i < b->num_segments; ++i) {
