@@ -437,6 +437,15 @@ __device__ __forceinline__ float across_halves(float v, F f) {
 // rows: any 16 lanes meet all 64 banks once.
 __device__ __forceinline__ int kv_lds(int bytes, int row, int c) { return row * bytes + 16 * (c ^ (bytes == 128 ? (row >> 1) & 7 : (row >> 2) & 3)); }
 
+// Where vector c of row `row` (0..31) of a wavefront's queries or outputs lies: 16 lanes that take the same vector of 16 rows, or a row's vectors, meet all banks once.
+template <int D>
+__device__ __forceinline__ int kv_strip(int row, int c) { return row * 2 * D + 16 * (c ^ (row & (D / 8 - 1))); }
+__device__ __forceinline__ void wave_sync() {                     // what a wavefront's lanes have written to shared memory, to its other lanes
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 template <int D>
 struct KvTileShared {
     unsigned char keys[2][64 * D], values[2][128 * D];
@@ -453,6 +462,11 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
     const int w0 = it.r0 + 32 * wave, r = w0 + n, pos = it.past + r / p.group;
     const bool valid = r < it.rows;
     const int see_hi = pos + 1, see_lo = p.window ? max(pos + 1 - p.window, 0) : 0;
+    // The wavefront's rows come and go in vectors of 16 bytes, whole rows side by side, and through its own part of the shared memory (before the first chunk, behind the last).  As each lane
+    // holds them, a row's pieces of 16 bytes would go one by one: 32 prompts of 256 tokens of 32 heads 73 us, so 65.
+    constexpr int kMoveRows = 512 / D, kMoves = 32 / kMoveRows;
+    const int move_row = lane / (D / 8), move_vec = lane % (D / 8), own_token = pos - it.past;
+    unsigned char* strip = (unsigned char*)&shared + wave * 64 * D;
     // of the wavefront's rows: the tokens that all see, and those that any sees (none at all: a wavefront behind the last row)
     const int last = min(w0 + 31, it.rows - 1);
     const bool some = w0 < it.rows;
@@ -462,15 +476,48 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
     const int tile_all_hi = it.past + it.r0 / p.group + 1, tile_all_lo = p.window ? max(it.past + min(it.r0 + kKvTileRows - 1, it.rows - 1) / p.group + 1 - p.window, 0) : 0;
     const int tile_lo = p.window ? max(it.past + it.r0 / p.group + 1 - p.window, 0) : 0;
 
+    bool bad = false;
+    // Keys and values of a chunk, from memory to registers and from there to shared memory: pass i of the workgroup (head of 128), or half i of it (head of 64), moves
+    // the tokens 32i .. 32i+31, so that a page's address is the same in a wavefront's lanes.
+    const int in_page = (1 << p.page_shift) - 1, kt = tid / (D / 16), kc = tid % (D / 16), vd = D == 128 ? tid >> 1 : (tid & 127) >> 1, vc = tid & 1;
+    const int k_off = (kt & in_page & 31) * D + 16 * kc, v_off = (vd << p.page_shift) + 16 * vc;
+    const int k_lds = kv_lds(D, kt, kc);                       // (32 tokens on: a fixed distance)
+    intx4 kv[kVecs], vv[kVecs];
+    int kscale[2], next_kscale[2], next_vscale[2];
+    auto ask = [&](int t0) {
+        int64_t block[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            block[u] = (int64_t)kv_page(p, it.table, t0 + 32 * u, tile_lo, it.end, bad) * p.kv_heads + h;
+            next_kscale[u] = p.k_scale[block[u]];
+            next_vscale[u] = p.v_scale[block[u]];
+        }
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+            const int u = D == 128 ? i : wave >> 1, slot = (t0 + 32 * u) & in_page;
+            kv[i] = *(const intx4*)(p.k + ((block[u] << p.page_shift) + slot) * D + k_off);
+            vv[i] = *(const intx4*)(p.v + ((block[u] * D) << p.page_shift) + slot + v_off);
+        }
+    };
+    ask(it.begin);                                                 // (on their way while the queries are split)
+    __builtin_amdgcn_sched_barrier(0);
     intx8 qh[kHalves], ql[kHalves];
     int q_scale;
     {
-        const bf16* q = p.q + (int64_t)(it.row0 + r / p.group) * p.q_stride + (h * p.group + r % p.group) * D;
+        intx4 w[kMoves];
+#pragma unroll
+        for (int i = 0; i < kMoves; ++i) {
+            const int row = kMoveRows * i + move_row, token = __shfl(own_token, row);
+            w[i] = intx4{0, 0, 0, 0};
+            if (w0 + row < it.rows) w[i] = *(const intx4*)(p.q + (int64_t)(it.row0 + token) * p.q_stride + (h * p.group + w0 + row - token * p.group) * D + 8 * move_vec);
+        }
+#pragma unroll
+        for (int i = 0; i < kMoves; ++i) *(intx4*)(strip + kv_strip<D>(kMoveRows * i + move_row, move_vec)) = w[i];
+        wave_sync();
         float x[D / 2], amax = 0.f;
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {                         // chunks of eight: elements 16g + 8(c % 2) + 32(c / 2)
-            intx4 w = intx4{0, 0, 0, 0};
-            if (valid) w = *(const intx4*)(q + 16 * g + 8 * (c & 1) + 32 * (c >> 1));
+            const intx4 w = *(const intx4*)(strip + kv_strip<D>(n, 2 * g + (c & 1) + 4 * (c >> 1)));
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 x[8 * c + 2 * i] = bf16_lo((unsigned)w[i]);
@@ -495,31 +542,9 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
     for (int j = 0; j < kTiles; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[j][e] = 0.f;
-    float m = -INFINITY, l = 0.f;
-    bool bad = false;
 
-    // Keys and values of a chunk, from memory to registers and from there to shared memory: pass i of the workgroup (head of 128), or half i of it (head of 64), moves
-    // the tokens 32i .. 32i+31, so that a page's address is the same in a wavefront's lanes.
-    const int in_page = (1 << p.page_shift) - 1, kt = tid / (D / 16), kc = tid % (D / 16), vd = D == 128 ? tid >> 1 : (tid & 127) >> 1, vc = tid & 1;
-    const int k_off = (kt & in_page & 31) * D + 16 * kc, v_off = (vd << p.page_shift) + 16 * vc;
-    const int k_lds = kv_lds(D, kt, kc);                       // (32 tokens on: a fixed distance)
-    intx4 kv[kVecs], vv[kVecs];
-    int kscale[2], next_kscale[2], next_vscale[2];
-    auto ask = [&](int t0) {
-        int64_t block[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            block[u] = (int64_t)kv_page(p, it.table, t0 + 32 * u, tile_lo, it.end, bad) * p.kv_heads + h;
-            next_kscale[u] = p.k_scale[block[u]];
-            next_vscale[u] = p.v_scale[block[u]];
-        }
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-            const int u = D == 128 ? i : wave >> 1, slot = (t0 + 32 * u) & in_page;
-            kv[i] = *(const intx4*)(p.k + ((block[u] << p.page_shift) + slot) * D + k_off);
-            vv[i] = *(const intx4*)(p.v + ((block[u] * D) << p.page_shift) + slot + v_off);
-        }
-    };
+    float m = -INFINITY, l = 0.f;
+
     // Where not every row of the tile sees the whole chunk, its values are cleaned on the way: tokens that no row sees are cleared, and so is NaN among the
     // others, which is noted (by the chunk's first token: a note of an earlier chunk means nothing).
     auto put = [&](int buf, int t0) {
@@ -574,7 +599,6 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
     };
     const int t_lane = kv_tile_token(0, n);
     if (tid < 2) noted[tid] = -1;
-    ask(it.begin);
     __syncthreads();
     put(0, it.begin);
     __syncthreads();
@@ -660,8 +684,8 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
     kv_settle();
     l = across_halves(l, Add());
     if (__any(bad)) m = NAN;
-    if (!valid) return;
     if (it.part >= 0) {
+        if (!valid) return;
         const int64_t at = (int64_t)h * p.part_rows + it.part + r - it.r0;
         if (g == 0) {
             p.part_ml[at * 2] = m;
@@ -675,17 +699,26 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
         return;
     }
     const float inv = (m != m ? m : 1.f) / l;
-    bf16* out = p.out + (int64_t)(it.row0 + r / p.group) * p.out_stride + (h * p.group + r % p.group) * D;
 #pragma unroll
     for (int j = 0; j < kTiles; ++j)
 #pragma unroll
         for (int a = 0; a < 4; ++a)
-            *(intx2*)(out + 32 * j + 8 * a + 4 * g) = intx2{(int)pack2_bf16(o[j][4 * a] * inv, o[j][4 * a + 1] * inv), (int)pack2_bf16(o[j][4 * a + 2] * inv, o[j][4 * a + 3] * inv)};
+            *(intx2*)(strip + kv_strip<D>(n, 4 * j + a) + 8 * g) = intx2{(int)pack2_bf16(o[j][4 * a] * inv, o[j][4 * a + 1] * inv), (int)pack2_bf16(o[j][4 * a + 2] * inv, o[j][4 * a + 3] * inv)};
+    wave_sync();
+    int at = lane;
+    asm volatile("" : "+v"(at));                                   // (formed here, not kept over the loop: registers)
+#pragma unroll
+    for (int i = 0; i < kMoves; ++i) {
+        const int row = kMoveRows * i + at / (D / 8), token = __shfl(see_hi - 1 - it.past, row);
+        if (w0 + row < it.rows)
+            *(intx4*)(p.out + (int64_t)(it.row0 + token) * p.out_stride + (h * p.group + w0 + row - token * p.group) * D + 8 * (at % (D / 8))) =
+                *(const intx4*)(strip + kv_strip<D>(row, at % (D / 8)));
+    }
 }
 
-// Tiles, and items of up to 16 rows behind them, in one launch: both have two wavefronts a SIMD, and a batch of prompts and decode steps is done when the longer of the two is.
+// Tiles, and items of up to 16 rows behind them, in one launch: both have two wavefronts a SIMD (head of 64: three; 16 heads of 8192 tokens 163 us, 196 with two), and a batch of prompts and decode steps is done when the longer of the two is.
 template <int D, bool CAP>
-SYMB_KERNEL __launch_bounds__(256, 2) void symb_kv_attention_kernel(KvAttentionParams p) {
+SYMB_KERNEL __launch_bounds__(256, D == 64 ? 3 : 2) void symb_kv_attention_kernel(KvAttentionParams p) {
     __shared__ union __attribute__((aligned(16))) {
         KvTileShared<D> tile;
         KvRowsShared<D, 1> rows;
