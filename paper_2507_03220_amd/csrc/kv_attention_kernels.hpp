@@ -795,5 +795,36 @@ SYMB_KERNEL __launch_bounds__(256) void symb_kv_join_kernel(KvJoinParams p) {
     *(intx2*)(p.out + (int64_t)(it.row0 + row / p.group) * p.out_stride + (h * p.group + row % p.group) * D + d) =
         intx2{(int)pack2_bf16(v[0] / sum, v[1] / sum), (int)pack2_bf16(v[2] / sum, v[3] / sum)};
 }
+// A workgroup for all of an item's rows, D / 4 lanes a row.
+template <int D>
+SYMB_KERNEL __launch_bounds__(256) void symb_kv_join_rows_kernel(KvJoinParams p) {
+    constexpr int kLanes = D / 4, kSets = 256 / kLanes;
+    const KvJoinItem it = p.items[blockIdx.x / p.kv_heads];
+    const int h = blockIdx.x % p.kv_heads, d = threadIdx.x % kLanes * 4;
+    for (int r = threadIdx.x / kLanes; r < min(16, it.rows - it.r0); r += kSets) {
+        const int row = it.r0 + r;
+        const int64_t at = (int64_t)h * p.part_rows + it.part0 + r;
+        float M = -INFINITY;
+        bool bad = false;
+        for (int k = 0; k < it.parts; ++k) {
+            const float m = p.part_ml[(at + (int64_t)it.stride * k) * 2];
+            bad |= m != m;
+            M = fmaxf(M, m);
+        }
+        const float base = M == -INFINITY ? 0.f : M;
+        float sum = 0.f;
+        floatx4 v = floatx4{0, 0, 0, 0};
+#pragma unroll 4
+        for (int k = 0; k < it.parts; ++k) {
+            const int64_t a = at + (int64_t)it.stride * k;
+            const float f = __builtin_amdgcn_exp2f(p.part_ml[a * 2] - base);
+            sum += p.part_ml[a * 2 + 1] * f;
+            v += *(const floatx4*)(p.part_o + a * D + d) * f;
+        }
+        if (bad) sum = NAN;
+        *(intx2*)(p.out + (int64_t)(it.row0 + row / p.group) * p.out_stride + (h * p.group + row % p.group) * D + d) =
+            intx2{(int)pack2_bf16(v[0] / sum, v[1] / sum), (int)pack2_bf16(v[2] / sum, v[3] / sum)};
+    }
+}
 
 }  // namespace symb

@@ -1,4 +1,5 @@
-"""Attention of segments with 17 to 48 rows for a key head, many enough that these rows go through kernels of their own (include/symb_block.h)."""
+"""Attention of segments with 17 to 48 rows for a key head, many enough that these rows go through kernels of their own, and of prompts whose tiles are split and joined
+(include/symb_block.h)."""
 import re
 from pathlib import Path
 
@@ -116,3 +117,22 @@ def test_wide_runs_with_a_page_outside_the_pool():
     table[0, :6], table[2, :5] = -1, 1 << 30               # behind the window nothing is looked up
     pg.batch = batch(table)
     _check(pg, K, V, q, copies, lambda *a: ob.attention(offsets(lens), past, *a), 60)
+
+
+@pytest.mark.parametrize("D,P,window,cap", [(128, 32, 400, 0.0), (128, 128, 0, 0.0), (64, 64, 500, 5.0), (64, 32, 0, 0.0)])
+def test_prompts_in_parts(D, P, window, cap):
+    """Long prompts of few key heads: too few tiles for the chip, so each is split, and thousands of rows are joined.  In a window some rows see nothing of a part."""
+    rng = np.random.default_rng(D + P)
+    H, group, lens, past = 2, 8, [600, 1, 9], [205, 700, 64]
+    pg = Pages(rng, lens, past, H, D, P)
+    K, V = pg.fill(rng)
+    assert sb.symb_kv_workspace_bytes(pg.batch, pg.cache, H * group, window) >= 8192 * H * (D + 2) * 4
+    V[0][410, 1, 5] = np.nan                               # a NaN that later rows see
+    pg.cache.v.view(torch.uint8)[int(pg.ids[0, 410 // P]), 1, 5, 410 % P] = 0xff
+    _check(pg, K, V, bf16(rng, sum(lens), H * group, D), 1, lambda *a: ob.attention(offsets(lens), past, *a), window, cap)
+    table = pg.table.clone()
+    table[0, 420 // P] = pg.N                              # a page outside the pool: NaN in the rows of the tiles that come to it
+    pg.batch = sb.KvBatch(offsets(lens), past, table)
+    out = host(attend(pg, bf16(rng, sum(lens), H * group, D), D ** -0.5, window, cap))
+    first = 420 // P * P - past[0]
+    assert np.isnan(out[max(first, 0):min(first + (window or 600), 600)]).all() and not np.isnan(out[:150]).any() and not np.isnan(out[600:]).any()
