@@ -63,9 +63,12 @@ struct NormPlan {
     std::vector<NormGroup> groups;
     int parts = 0;
 };
-// Three workgroups a CU are on it together: one round of them, and no chunk shorter than kNormRows rows while that holds (a chunk's partial sums cost as much traffic as a row and a
-// third).  20480 rows of 4608: 512 chunks 134 us, 768 124, 1024 131, 2048 130; with bias 170, 142, 151, 150; 10240 rows of 4096 64, 61, 68, 66.
+// Up to three workgroups a CU are on it together, so the rows are cut into 768 chunks at most, and into 512 or 256 where that many pay: a chunk's row takes 0.55 us, its partial sums 8 bytes a column
+// and gradient at 4.9 TB/s, least in all with rows^2 = kNormParts (gradients) (rows of the batch) width to a chunk.  20480 rows of 2048 with bias (1290 chunks by this): 768 chunks 61.8 us, 512 66.3;
+// 20480 of 4608 without (1219): 123.8, 122.0; 14 segments of 541 rows of 4096 (790): 47.7, 45.4; 5000 of 6144 with bias (367): 512 52.7, 256 49.7; 3000 of 4096 (500): 19.8, 20.6.
+// A few chunks more than that, as segments' rounding up would have it, cost a round: 770 of them 50.6 us.
 constexpr int kNormChunks = 768, kNormRows = 4;
+constexpr double kNormParts = 3e-6;
 symb_status plan_norm(symb_handle h, const symb_norm_batch* b, NormPlan& plan) {
     const int S = b->num_segments, T = b->seg_offsets[S];
     std::vector<int> order(S);
@@ -84,7 +87,27 @@ symb_status plan_norm(symb_handle h, const symb_norm_batch* b, NormPlan& plan) {
     std::sort(seen.begin(), seen.end());
     for (size_t i = 1; i < seen.size(); ++i)
         if (seen[i].first == seen[i - 1].first) return fail(h, SYMB_ERR_INVALID_ARG, "two segments share one of dweight and dbias, but not both");
-    const int rows = std::max(kNormRows, (T + kNormChunks - 1) / kNormChunks);
+    bool dw = false, db = false;
+    int longest = 0;
+    for (int i = 0; i < S; ++i) {
+        dw |= n[i].dweight != nullptr;
+        db |= n[i].dbias != nullptr;
+        longest = std::max(longest, b->seg_offsets[i + 1] - b->seg_offsets[i]);
+    }
+    const double fit = T / std::max(std::sqrt(kNormParts * (dw + db) * T * b->width), (double)kNormRows);
+    const int chunks = fit > 1250 ? kNormChunks : fit > 384 ? kNormChunks * 2 / 3 : kNormChunks / 3;
+    int rows = std::max(kNormRows, (T + chunks - 1) / chunks);
+    auto count = [&](int per) {
+        int64_t c = 0;
+        for (int i = 0; i < S; ++i) c += (b->seg_offsets[i + 1] - b->seg_offsets[i] + per - 1) / per;
+        return c;
+    };
+    if (rows < longest && count(longest) <= chunks)
+        for (int high = longest; rows < high;) {
+            const int mid = rows + (high - rows) / 2;
+            if (count(mid) <= chunks) high = mid;
+            else rows = mid + 1;
+        }
     for (int at = 0; at < S;) {
         int to = at + 1;
         while (to < S && key(order[to]) == key(order[at])) ++to;
