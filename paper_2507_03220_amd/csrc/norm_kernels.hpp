@@ -5,7 +5,8 @@
 //
 // Both are bound by memory: forward reads and writes a row once (4 bytes an element), backward reads x and dy and writes dx (6 bytes).  So a row is read
 // once, into registers as the bf16 pairs it came in, and everything else happens there: the mean first and then the squares about it (one pass with
-// sums of x and x^2 cancels where the mean is large beside the deviation), in fp32.
+// sums of x and x^2 cancels where the mean is large beside the deviation), in fp32.  Measured: 16384 rows of 6144 forward in 75 us, 5.4 TB/s; 20480 of 4608 backward 120 us, 4.7 TB/s, its partial
+// sums and their reduction (5 us) included.  A single row is a launch: the kernel 2.1 us, 8 with the host's part.
 #pragma once
 #include "block_device.hpp"
 

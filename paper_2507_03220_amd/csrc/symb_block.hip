@@ -138,13 +138,14 @@ void launch_norm_fwd(const NormFwdParams& p, hipStream_t s) {
     constexpr int rows = WAVES < 4 ? 4 / WAVES : 1;
     hipLaunchKernelGGL((symb_norm_fwd_kernel<RMS, WAVES, NV>), dim3((p.T + rows - 1) / rows), dim3(WAVES < 4 ? 256 : WAVES * 64), 0, s, p);
 }
+// One wavefront a row while its registers hold it well, four above (20000 rows of 768: 14.3 us with one, 20.8 with four; of 2048 34.7, 37.0; of 4096 71, 63.3), and no more vectors a lane than
+// the width asks for where that tells (20000 rows of 512 10.7 us with one, 12.1 with four; of 4096 63.3 with two, 64.5 with four; of 4608 and 6144 three are no better than four).
 template <bool RMS>
 void launch_norm_fwd(const NormFwdParams& p, hipStream_t s) {
     const int vecs = p.width / 8;
     if (vecs <= 64) return launch_norm_fwd<RMS, 1, 1>(p, s);
     if (vecs <= 256) return launch_norm_fwd<RMS, 1, 4>(p, s);
     if (vecs <= 512) return launch_norm_fwd<RMS, 4, 2>(p, s);
-    if (vecs <= 768) return launch_norm_fwd<RMS, 4, 3>(p, s);
     if (vecs <= 1024) return launch_norm_fwd<RMS, 4, 4>(p, s);
     return launch_norm_fwd<RMS, 4, 8>(p, s);
 }
@@ -152,12 +153,12 @@ template <bool RMS, bool BIAS, int WAVES, int NV>
 void launch_norm_bwd(const NormBwdParams& p, int chunks, hipStream_t s) {
     hipLaunchKernelGGL((symb_norm_bwd_kernel<RMS, BIAS, WAVES, NV>), dim3(chunks), dim3(WAVES * 64), 0, s, p);
 }
+// Likewise (20000 rows of 768 41 us with one vector, 76 with four; of 4096 110.1 with two, 112.2; 5000 of 16384 124 with eight wavefronts, 153 with four of eight vectors a lane).
 template <bool RMS, bool BIAS>
 void launch_norm_bwd(const NormBwdParams& p, int chunks, hipStream_t s) {
     const int vecs = p.width / 8;
     if (vecs <= 256) return launch_norm_bwd<RMS, BIAS, 4, 1>(p, chunks, s);
     if (vecs <= 512) return launch_norm_bwd<RMS, BIAS, 4, 2>(p, chunks, s);
-    if (vecs <= 768) return launch_norm_bwd<RMS, BIAS, 4, 3>(p, chunks, s);
     if (vecs <= 1024) return launch_norm_bwd<RMS, BIAS, 4, 4>(p, chunks, s);
     return launch_norm_bwd<RMS, BIAS, 8, 4>(p, chunks, s);
 }
@@ -221,8 +222,8 @@ struct KvKernel {
     int slots;                            // workgroups that run at once: two a CU, one with the registers of 17 rows and more
     int worth;                            // chunks that a workgroup has to be spared for parts to pay
 };
-// Joining parts costs a launch and a pass over them, 4 to 5 us.  A chunk takes a workgroup's wavefront (one in four goes to each) 0.9 us with up to 16 rows, 1.6 and 2.5 with 32 and 48, and a
-// tile's workgroup 1.2 us.
+// Joining parts costs a launch and a pass over them, 5 to 8 us.  A chunk takes a workgroup's wavefront (one in four goes to each) 0.9 us with up to 16 rows, 1.6 and 2.5 with 32 and 48, and a
+// tile's workgroup 1.2 us, 2.0 beside another on its CU.
 constexpr KvKernel kKvKernels[4] = {{128, 48, INT64_MAX, 512, 4}, {16, 0, 16, 512, 20}, {32, 16, 32, 256, 12}, {48, 32, 48, 256, 8}};
 static_assert(kKvChunk == kKvTileChunk, "");
 // Up to 48 rows in one workgroup widen the values once instead of three times, but are a launch of their own, with a third of the workgroups.  Where all that they would do is less than this many

@@ -108,7 +108,7 @@ def attend(pg, q, scale, window=0, cap=0.0, out=None, ws_fill=None):
 
 
 def attention_bound(want, mass, big):
-    """What the kernel's roundings allow.  Output: half a bf16 step, 2^-8 |out| with room.  Weights: nine significant bits, 2^-9 of each, and so of their sum; a
+    """What the kernel's roundings allow.  Output: half a bf16 step, 2^-8 |out| with room.  Weights: bf16, 2^-9 of each, their sum as much with room; a
     score's products lose up to 2^-14 of the largest of them each (128 terms in two instructions), 2^-7 of the largest in all, e^d - 1 < 1.1 d of a weight."""
     score = 1.1 * 2.0 ** -7 * big + 1e-5
     return 1.02 * 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2 * score) * mass + 1e-30
