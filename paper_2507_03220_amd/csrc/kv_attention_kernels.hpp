@@ -17,7 +17,7 @@
 //
 // Measured: a prompt of 8192 tokens, 32 query on 16 key heads of 128, 525 to 545 us or 1.0 PFLOP/s where a large bf16 product reaches 1.3: matrix instructions 44 % of the time, vector
 // instructions (softmax, and values on their way to shared memory) 47 %, and two wavefronts of a SIMD overlap the two only in part.  Decode steps are bound by memory: 48 clients with up to
-// 4096 tokens in the window, 538 MB, 98 us or 5.5 TB/s.  With 48 query heads on one key head (16 clients, contexts to 131072, 196 MB and 18.7 GFLOP) 53 us, half by vector work.
+// 4096 tokens in the window, 538 MB, 98 us or 5.5 TB/s.  With 48 query heads on one key head (16 clients, contexts to 131072, 196 MB and 18.7 GFLOP) 53 us, 3.7 TB/s: one wavefront a SIMD.
 #pragma once
 #include <type_traits>
 
