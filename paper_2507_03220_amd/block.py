@@ -6,6 +6,7 @@ libsymb.so.
 """
 from __future__ import annotations
 
+import contextlib
 from dataclasses import dataclass, field
 from typing import Dict, List, Sequence
 
@@ -25,6 +26,13 @@ def _offsets(lens: Sequence[int]) -> List[int]:
 
 def _workspace(n: int) -> torch.Tensor:
     return torch.empty(max(n, 256), device="cuda", dtype=torch.uint8)
+
+
+def _on(stream: int):
+    """Torch's own work (what it allocates, what it copies) in the order of `stream`."""
+    if stream == torch.cuda.current_stream().cuda_stream:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream())
 
 
 def rotation_table(positions: int, dim: int, base: float = 10000.0) -> torch.Tensor:
@@ -92,8 +100,18 @@ class AttentionBlock:
         c.pages, c.past = [], 0
 
     def forward(self, X: torch.Tensor, lens: Sequence[int], clients: Sequence[Client], stream: int = 0) -> torch.Tensor:
-        """X [T][width]: lens[i] new tokens of clients[i], in order.  Returns [T][width] and moves the clients' places on."""
+        """X [T][width]: lens[i] new tokens of clients[i], in order, no client twice.  Returns [T][width], there in the order of `stream`, and moves the clients' places on."""
+        if len(lens) != len(clients) or len({id(c) for c in clients}) != len(clients):
+            raise ValueError("one length for each client, and each client once")
+        if X.shape[0] != sum(lens):
+            raise ValueError(f"{X.shape[0]} rows for {sum(lens)} tokens")
+        with _on(stream):
+            return self._forward(X, lens, clients, stream)
+
+    def _forward(self, X: torch.Tensor, lens: Sequence[int], clients: Sequence[Client], stream: int) -> torch.Tensor:
         T, width = X.shape
+        if not T:
+            return torch.empty_like(X)
         H, D, off = self.cache.kv_heads, self.cache.head_dim, _offsets(lens)
         for c, n in zip(clients, lens):
             self._reserve(c, c.past + n)

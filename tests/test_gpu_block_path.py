@@ -105,6 +105,34 @@ def test_prompts_and_decode_steps_of_many_clients():
     assert clients[0].past == 0 and len(block.free) == 40 - used + 3
 
 
+def test_the_block_on_another_stream_and_its_refusals():
+    rng = np.random.default_rng(3)
+    width, H, D = 256, 2, 64
+    W = {p: bf16(rng, o, i, std=i ** -0.5) for p, o, i in (("q", H * D, width), ("k", H * D, width), ("v", H * D, width), ("o", width, H * D))}
+    new = lambda: blk.AttentionBlock(gh.handle(), W, H, sb.KvCache.empty(20, H, D, 32), sb.Rotation(blk.rotation_table(300, D)))  # noqa: E731
+    norm = sb.Norm(bf16(rng, width, std=0.1, mean=1.0))
+    X = bf16(rng, 101, width)
+
+    def steps(where):
+        block, clients = new(), [blk.Client(norm), blk.Client(norm)]
+        few = [X[i:i + 2].clone() for i in range(0, 20, 2)]
+        torch.cuda.synchronize()
+        outs = [block.forward(X, [100, 1], clients, where)] + [block.forward(x, [1, 1], clients, where) for x in few]
+        torch.cuda.synchronize()
+        return outs
+    side = torch.cuda.Stream()
+    for a, b in zip(steps(stream()), steps(side.cuda_stream)):
+        assert torch.equal(a, b)
+    block, c = new(), blk.Client(norm)
+    assert block.forward(X[:0], [0], [c]).shape == (0, width)
+    for rows, lens, clients in ((X[:2], [1, 1], [c, c]), (X[:2], [2], [c, blk.Client(norm)]), (X[:3], [2], [c])):
+        with pytest.raises(ValueError):
+            block.forward(rows, lens, clients)
+    with pytest.raises(RuntimeError):
+        block.forward(bf16(rng, 700, width), [700], [c])
+    assert c.past == 0
+
+
 def test_the_example_runs():
     import os
     import subprocess
