@@ -215,21 +215,22 @@ struct KvPlan {
     int join_rows = 0;                    // the most rows of one of them
     int64_t part_rows = 0;                // rows of partial results, of one key head
 };
-// The kernels of an attention call: runs of `rows` rows of the segments with more than `over` and up to `upto` rows for a key head.  All go over the tokens in chunks of 64.
+// The kernels of an attention call: runs of `rows` rows of a segment for a key head.  All go over the tokens in chunks of 64.
 struct KvKernel {
     int rows;
-    int64_t over, upto;
     int slots;                            // workgroups that run at once: two a CU, one with the registers of 17 rows and more
     int worth;                            // chunks that a workgroup has to be spared for parts to pay
 };
 // Joining parts costs a launch and a pass over them, 5 to 8 us.  A chunk takes a workgroup's wavefront (one in four goes to each) 0.9 us with up to 16 rows, 1.6 and 2.5 with 32 and 48, and a
 // tile's workgroup 1.2 us, 2.0 beside another on its CU.
-constexpr KvKernel kKvKernels[4] = {{128, 48, INT64_MAX, 512, 4}, {16, 0, 16, 512, 20}, {32, 16, 32, 256, 12}, {48, 32, 48, 256, 8}};
+constexpr KvKernel kKvKernels[4] = {{128, 512, 4}, {16, 512, 20}, {32, 256, 12}, {48, 256, 8}};
 static_assert(kKvChunk == kKvTileChunk, "");
-// Up to 48 rows in one workgroup widen the values once instead of three times, but are a launch of their own, with a third of the workgroups.  Where all that they would do is less than this many
-// chunks of 16 rows, segments of 17 to 48 rows go 16 rows at a time into the first launch.  Both sides (48 query heads on one key head): 91 chunks 15.0 us with 48 rows, 9.4 with 16; 4850 22.6, 21.3;
-// 14400 32.4, 43; 35800 52.5, 87.6.  (32 key heads): 7700 30.5, 24.0; 17700 39.4, 35.9; 43600 77.4, 82.4.
-constexpr int64_t kKvWideWork = 12288;
+// Which of them a segment's rows go to: up to 16 rows the second, above tiles (from 49 rows) or the kernels of 32 and 48 rows, where their work, counted in chunks of 16 rows, is worth it.
+// Those widen the values once for all their rows, but 16 rows at a time are more workgroups, four wavefronts side by side on a run's tokens, and no launch of their own.
+// Up to 48 rows, both sides (48 query heads on one key head): 91 chunks 15.0 us with 48 rows, 9.4 with 16; 4850 22.6, 21.3; 14400 32.4, 43; 35800 52.5, 87.6.  (32 key heads): 7700 30.5, 24.0;
+// 17700 39.4, 35.9; 43600 77.4, 82.4.  Prompts, where their runs of 16 rows fill the chip once at most: 1290 chunks in 512 runs 13.3 us in tiles, 9.5; 2400 in 256 20.0, 12.6; 6500 in 480 26.3, 18.9;
+// 12900 in 384 24.3, 15.9; 38000 in 512 41, 56; more runs than that: 2700 in 1024 13.5, 15.1; 3700 in 1500 11.0, 18.6.
+constexpr int64_t kKvWideWork = 12288, kKvFewRuns = 512;
 
 // Chunks that a workgroup takes: as few as keep all workgroups on the chip at once, where that is possible and spares the longest run enough; else all of a run's, and where the runs
 // alone are more than that, what leaves about that many.  (Tiles are not split then: they come longest first, and while some wait for a place the longest is not what the call waits for.
@@ -258,24 +259,24 @@ KvPlan plan_attention(const symb_kv_batch* b, const symb_kv_cache* c, int q_head
     const int group = q_heads / c->kv_heads;
     std::vector<KvItem> runs;
     std::vector<int32_t> chunks;
-    int64_t wide = 0;
+    int64_t work[2] = {0, 0}, tiled_runs = 0;                      // of up to 48 rows, of more
     for (int i = 0; i < b->num_segments; ++i) {
         const int64_t n = b->seg_offsets[i + 1] - b->seg_offsets[i], rows = n * group;
-        if (rows <= kKvKernels[1].upto || rows > kKvKernels[3].upto) continue;
-        const int64_t begin = window ? std::max<int64_t>((int64_t)b->past[i] + 1 - window, 0) / kKvChunk * kKvChunk : 0;
-        wide += (b->past[i] + n + kKvChunk - 1 - begin) / kKvChunk * ((rows + 15) / 16) * c->kv_heads;
+        if (rows <= kKvKernels[1].rows) continue;
+        const bool tiled = rows > kKvKernels[3].rows;
+        const int64_t begin = window ? std::max<int64_t>((int64_t)b->past[i] + 1 - window, 0) / kKvChunk * kKvChunk : 0, of16 = (rows + 15) / 16 * c->kv_heads;
+        work[tiled] += (b->past[i] + n + kKvChunk - 1 - begin) / kKvChunk * of16;
+        if (tiled) tiled_runs += of16;
     }
+    const bool wide = work[0] >= kKvWideWork, tiles = work[1] >= kKvWideWork || tiled_runs > kKvFewRuns;
+    auto kind_of = [&](int64_t rows) { return rows > kKvKernels[3].rows ? (tiles ? 0 : 1) : rows > kKvKernels[1].rows && wide ? (rows > kKvKernels[2].rows ? 3 : 2) : 1; };
     for (int kind = 0; kind < 4; ++kind) {
-        KvKernel kernel = kKvKernels[kind];
-        if (kind && wide < kKvWideWork) {
-            if (kind > 1) break;
-            kernel.upto = kKvKernels[3].upto;
-        }
+        const KvKernel& kernel = kKvKernels[kind];
         runs.clear();
         chunks.clear();
         for (int i = 0; i < b->num_segments; ++i) {
             const int64_t rows = (int64_t)(b->seg_offsets[i + 1] - b->seg_offsets[i]) * group;
-            if (rows <= kernel.over || rows > kernel.upto) continue;
+            if (!rows || kind_of(rows) != kind) continue;
             for (int64_t r0 = 0; r0 < rows; r0 += kernel.rows) {
                 const int64_t first = b->past[i] + r0 / group, last = b->past[i] + std::min(r0 + kernel.rows - 1, rows - 1) / group;
                 const int64_t begin = window ? std::max<int64_t>(first + 1 - window, 0) / kKvChunk * kKvChunk : 0;

@@ -1,5 +1,5 @@
-"""Attention of segments with 17 to 48 rows for a key head, many enough that these rows go through kernels of their own, and of prompts whose tiles are split and joined
-(include/symb_block.h)."""
+"""Attention of segments with 17 to 48 rows for a key head, many enough that these rows go through kernels of their own, and of prompts large enough for tiles, also for tiles that are
+split and joined (include/symb_block.h)."""
 import re
 from pathlib import Path
 
@@ -13,17 +13,20 @@ from paper_2507_03220_amd import binding as sb
 
 pytestmark = pytest.mark.gpu
 SOURCE = Path(sb.__file__).parent / "csrc" / "symb_block.hip"
-ENOUGH = int(re.search(r"kKvWideWork = (\d+);", SOURCE.read_text())[1])
+ENOUGH, RUNS = map(int, re.search(r"kKvWideWork = (\d+), kKvFewRuns = (\d+);", SOURCE.read_text()).groups())
 
 
 def _copies(lens, past, H, group, window):
-    """How often the segments have to be in the batch for that (chunks of 64 tokens times 16 rows, all key heads')."""
-    work = 0
+    """How often the segments have to be in the batch for that: chunks of 64 tokens times 16 rows of all key heads, or for tiles their runs of 16 rows."""
+    work = runs = 0
     for n, p in zip(lens, past):
+        of16 = H * -(-n * group // 16)
         if 16 < n * group <= 48:
             begin = max(p + 1 - window, 0) // 64 * 64 if window else 0
-            work += H * -(-(p + n - begin) // 64) * -(-n * group // 16)
-    return -(-ENOUGH // work)
+            work += -(-(p + n - begin) // 64) * of16
+        elif n * group > 48:
+            runs += of16
+    return max(-(-ENOUGH // work) if work else 1, RUNS // runs + 1 if runs else 1)
 
 
 def _many(rng, H, D, P, lens, past, copies, std=60.0):
@@ -136,3 +139,60 @@ def test_prompts_in_parts(D, P, window, cap):
     out = host(attend(pg, bf16(rng, sum(lens), H * group, D), D ** -0.5, window, cap))
     first = 420 // P * P - past[0]
     assert np.isnan(out[max(first, 0):min(first + (window or 600), 600)]).all() and not np.isnan(out[:150]).any() and not np.isnan(out[600:]).any()
+
+
+# ---- tiles ---------------------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("D,P", [(64, 32), (64, 64), (64, 128), (128, 32), (128, 64), (128, 128)])
+@pytest.mark.parametrize("H,group,lens,past", [
+    (2, 3, [17, 1, 40, 43], [0, 200, 90, 64]),             # tiles of 51 to 129 rows, one token beside them
+    (1, 8, [100, 3], [33, 1500]),
+    (3, 1, [150, 129, 64, 128], [0, 1, 63, 700]),          # tiles that end with, before and behind their last row
+    (4, 5, [77, 0, 11], [500, 3, 5]),
+])
+def test_tiles(D, P, H, group, lens, past):
+    _attention(D + P + H, H, group, D, P, lens, past)
+
+
+@pytest.mark.parametrize("D,P", [(64, 32), (128, 64)])
+@pytest.mark.parametrize("window", [1, 5, 100, 129, 4096])
+@pytest.mark.parametrize("cap", [0.0, 5.0])
+def test_tiles_with_window_and_cap(D, P, window, cap):
+    _attention(window + D, 2, 2, D, P, [70, 1, 130], [700, 3, 260], window, cap, q_std=2.0)
+
+
+@pytest.mark.parametrize("D,window", [(64, 0), (128, 0), (128, 40), (64, 100)])
+def test_tiles_with_nan_in_hidden_and_in_seen_tokens(D, window):
+    rng = np.random.default_rng(5)
+    H, P, group, lens, past = 2, 32, 2, [150, 3, 60], [10, 300, 130]
+    copies = _copies(lens, past, H, group, window)
+    pg, K, V, batch = _many(rng, H, D, P, lens, past, copies)
+    pg.batch = batch(pg.table)
+    for i, (n, p) in enumerate(zip(lens, past)):           # one channel of some tokens' values, early, in the middle of the new ones, last; a key
+        for t in {3, p + n // 2, p + n - 1}:
+            at = int(pg.ids[i, t // P])
+            pg.cache.v.view(torch.uint8)[at, 1, 5, t % P] = 0xff
+            V[i][t, 1, 5] = np.nan
+        at = int(pg.ids[i, p // P])
+        pg.cache.k.view(torch.uint8)[at, 0, p % P, 7] = 0x7f
+        K[i][p, 0, 7] = np.nan
+    _check(pg, K, V, bf16(rng, sum(lens), H * group, D), copies, lambda *a: ob.attention(offsets(lens), past, *a), window)
+
+
+def test_tiles_of_one_large_score_and_of_queries_that_are_zero_infinite_nan_or_tiny():
+    rng = np.random.default_rng(6)
+    H, D, P, lens, past = 1, 128, 64, [160, 60], [400, 0]
+    copies = _copies(lens, past, H, 2, 0)
+    pg, K, V, batch = _many(rng, H, D, P, lens, past, copies)
+    pg.batch = batch(pg.table)
+    q = bf16(rng, sum(lens), 2, D)
+    q[0] = 0.0
+    q[1, 0, 3], q[2, 1, 9] = float("nan"), float("inf")
+    q[3] = q[3] * 1e-30
+    q[4, 0, 1:] = q[4, 0, 1:] * 2.0 ** -18
+    q[5:20] = q[5:20] * 8                                  # scores that differ by dozens: the maximum moves, weights vanish
+
+    def formula(K, V, h, *a):
+        h[2, 1] = np.nan                                   # inf x finite, both signs
+        return ob.attention(offsets(lens), past, K, V, h, *a)
+
+    _check(pg, K, V, q, copies, formula)
