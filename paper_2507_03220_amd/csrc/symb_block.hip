@@ -218,7 +218,7 @@ struct KvPlan {
 // The kernels of an attention call: runs of `rows` rows of a segment for a key head.  All go over the tokens in chunks of 64.
 struct KvKernel {
     int rows;
-    int slots;                            // workgroups that run at once: two a CU, one with the registers of 17 rows and more
+    int slots;                            // workgroups that run at once: two a CU (of a head of 64 three fit; counted on, they gained nothing), one with the registers of 17 rows and more
     int worth;                            // chunks that a workgroup has to be spared for parts to pay
 };
 // Joining parts costs a launch and a pass over them, 5 to 8 us.  A chunk takes a workgroup's wavefront (one in four goes to each) 0.9 us with up to 16 rows, 1.6 and 2.5 with 32 and 48, and a
