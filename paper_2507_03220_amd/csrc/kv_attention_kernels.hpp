@@ -61,7 +61,8 @@ struct KvAttentionParams {
     int64_t q_stride, out_stride;
     int32_t num_pages, kv_heads, group, page_shift, window;
     int32_t part_rows;                    // of one key head
-    float scale, cap;                     // cap > 0: its value in log2 units, and scale / cap in `scale`; else scale in log2 units
+    float scale;                          // log2(e) times it
+    float cap, to_cap;                    // cap / scale, and kKvRoot scale / cap: the scores are capped before they are scaled
 };
 
 __device__ __forceinline__ int kv_token(int s, int m) { return 16 * (m >> 2) + 4 * s + (m & 3); }
@@ -130,13 +131,44 @@ __device__ __forceinline__ void kv_settle() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// A score in log2 units.
-template <bool CAP>
-__device__ __forceinline__ float kv_score(const KvAttentionParams& p, float s) {
-    if (!CAP) return s * p.scale;
-    // cap tanh(y) = cap (1 - 2 / (e^2y + 1)): at most cap 2^-23 off, which is what a score of that size is held to
-    const float y = s * p.scale;
-    return p.cap * (1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * 2.885390082f) + 1.f));
+// Scores s, not yet scaled, to cap tanh(s / cap).  With y = s / cap, cap (1 - 2 / (e^2y + 1)) is good to 2^-22 of the cap or so, which far below the cap may be more than the score itself: there it is the
+// series s (1 - y^2 / 3 + 2 y^4 / 15 - 17 y^6 / 315), whose next term is 2^-21 of s at y = 1/4.  Either way a score is off by 2^-20 of itself at most, whatever the cap.  Where no score of a
+// wavefront's chunk has come up to a quarter of the cap, which models choose well above their scores, the series is all there is, and no instruction of it is a transcendental one.
+// The series is formed in z = (r y)^2, r the 6th root of 17 / 315, as s + s z (z (2 / (15 r^4) - z) - 1 / (3 r^2)): two instructions with a literal each, and no constant in a register.
+// Measured: a prompt of 8192 tokens, 16 heads of 64, capped, 280 us (259 with the first formula alone, 171 without a cap); 32 on 16 heads of 128, 4 prompts of 8192 tokens in all, 253 (246); decode steps, bound
+// by memory, as before.
+constexpr float kKvSeries = 0.25f, kKvRoot = 0.6147375f;
+template <class V, int N>
+__device__ __forceinline__ void kv_cap(const KvAttentionParams& p, V (&s)[N]) {
+    constexpr int kEach = sizeof(V) / sizeof(float);
+    auto series = [&](float x) {
+        const float u = x * p.to_cap, z = u * u;
+        return __builtin_fmaf(x * z, __builtin_fmaf(z, 0.9336408f - z, -0.8820624f), x);
+    };
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) top = fmaxf(top, fabsf(s[i][e]));
+    if (__any(top * p.to_cap > kKvSeries * kKvRoot)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) {
+                float x = s[i][e];
+                asm volatile("" : "+v"(x));                        // (its series is formed here, not ahead of the branch: registers)
+                const float u = x * p.to_cap;
+                float far = p.cap * (1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(u * (2.885390082f / kKvRoot)) + 1.f)), near = series(x);
+                asm volatile("" : "+v"(far), "+v"(near));          // (both: the compiler would branch for every score)
+                s[i][e] = fabsf(u) > kKvSeries * kKvRoot ? far : near;
+                if (e & 1) __builtin_amdgcn_sched_barrier(0);      // (two at a time: registers)
+            }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) s[i][e] = series(s[i][e]);
+    }
 }
 
 // The page of a token, the same in all lanes, so through the scalar cache: page numbers then arrive beside the keys and values under way, not behind them.  Only pages of the tokens
@@ -191,8 +223,9 @@ __device__ __forceinline__ void kv_rows(const KvAttentionParams& p, const KvItem
     auto& join = shared.join;
     auto& stat = shared.stat;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-    // tokens that this lane's rows see; those that every row of the item sees, and those that some row does
-    int see_hi[R], see_lo[R];
+    // tokens that this lane's rows see (from the window's on: see_lo); those that every row of the item sees, and those that some row does
+    int see_hi[R];
+    auto see_lo = [&](int hi) { return p.window ? max(hi - p.window, 0) : 0; };
     const int last = min(it.r0 + 16 * R - 1, it.rows - 1);
     const int all_hi = it.past + it.r0 / p.group + 1, all_lo = p.window ? max(it.past + last / p.group + 1 - p.window, 0) : 0;
     const int any_hi = it.past + last / p.group + 1, any_lo = p.window ? max(all_hi - p.window, 0) : 0;
@@ -202,7 +235,6 @@ __device__ __forceinline__ void kv_rows(const KvAttentionParams& p, const KvItem
         const int row = it.r0 + 16 * r + n, pos = it.past + row / p.group;
         const bool valid = row < it.rows;
         see_hi[r] = valid ? pos + 1 : 0;
-        see_lo[r] = p.window ? max(pos + 1 - p.window, 0) : 0;
         kv_query<D>(q[r], p.q + (int64_t)(it.row0 + row / p.group) * p.q_stride + (h * p.group + row % p.group) * D, valid, g);
     }
     bool bad = false;
@@ -258,16 +290,12 @@ __device__ __forceinline__ void kv_rows(const KvAttentionParams& p, const KvItem
                 s[i] = kv_mfma(a, q[r].hi, floatx4{0, 0, 0, 0}, c.scale, q[r].hi_scale);
                 if constexpr (D == 128) s[i] = kv_mfma(a, q[r].lo, s[i], c.scale, q[r].lo_scale);
             }
-            if constexpr (CAP) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[i][e] = kv_score<true>(p, s[i][e]);
-            }
             kv_settle();
+            if constexpr (CAP) kv_cap(p, s);
             if (!whole) {
-                asm volatile("");                                  // (a branch: as a selection it would cost every chunk three instructions a score)
-                const int hi = see_hi[r] - t0 - 16 * g, lo = see_lo[r] - t0 - 16 * g;
+                int end = see_hi[r];
+                asm volatile("" : "+v"(end));                      // (a branch: as a selection it would cost every chunk three instructions a score, and the window's end a register)
+                const int hi = end - t0 - 16 * g, lo = see_lo(end) - t0 - 16 * g;
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -278,8 +306,7 @@ __device__ __forceinline__ void kv_rows(const KvAttentionParams& p, const KvItem
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) top = fmaxf(top, s[i][e]);
-            const float factor = CAP ? 1.f : p.scale;              // (without a cap the scores stay as they are: it goes into the exponent)
-            top = across_rows(top, Max()) * factor;
+            top = across_rows(top, Max()) * p.scale;               // (the scores stay as they are: their factor goes into the exponent)
             // m follows the row's maximum once that has outgrown it 2^kKvSlack-fold
             if (__any(top > m[r] + kKvSlack)) {
                 top = fmaxf(m[r], top);
@@ -294,7 +321,7 @@ __device__ __forceinline__ void kv_rows(const KvAttentionParams& p, const KvItem
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    s[i][e] = __builtin_amdgcn_exp2f(s[i][e] * factor + base);
+                    s[i][e] = __builtin_amdgcn_exp2f(s[i][e] * p.scale + base);
                     l[r] += s[i][e];
                 }
 #pragma unroll
@@ -315,9 +342,11 @@ __device__ __forceinline__ void kv_rows(const KvAttentionParams& p, const KvItem
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     intx8 seen, is;
+                    int end = see_hi[r];
+                    asm volatile("" : "+v"(end));
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        seen[i] = 0x38383838 & kv_keep_bytes(t0 + 16 * g + 4 * i, see_lo[r], see_hi[r]);           // (1)
+                        seen[i] = 0x38383838 & kv_keep_bytes(t0 + 16 * g + 4 * i, see_lo(end), end);               // (1)
                         seen[4 + i] = is[4 + i] = 0;
                     }
 #pragma unroll
@@ -464,8 +493,7 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 31, g = lane >> 5;
     const int w0 = it.r0 + 32 * wave, r = w0 + n, pos = it.past + r / p.group;
-    const bool valid = r < it.rows;
-    const int see_hi = pos + 1, see_lo = p.window ? max(pos + 1 - p.window, 0) : 0;
+    const int see_hi = pos + 1 - 8 * g, see_lo = (p.window ? max(pos + 1 - p.window, 0) : 0) - 8 * g;      // (as the lane counts a chunk's tokens: from 8g on)
     // The wavefront's rows come and go in vectors of 16 bytes, whole rows side by side, and through its own part of the shared memory (before the first chunk, behind the last).  As each lane
     // holds them, a row's pieces of 16 bytes would go one by one: 32 prompts of 256 tokens of 32 heads 73 us, so 65.
     constexpr int kMoveRows = 512 / D, kMoves = 32 / kMoveRows;
@@ -577,12 +605,12 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
     // NaN that `put` has cleared, to the rows that see it: ones in its places times ones where a row sees the token.
     auto give_nan = [&](int t0) {
         for (int q = 0; q < 4; ++q) {
-            const int t = t0 + 16 * q + 8 * g;
-            const int64_t block = (int64_t)kv_page(p, it.table, t0 + 16 * q, tile_lo, it.end, bad) * p.kv_heads + h;
+            const int from = t0 + 16 * q, t = from + 8 * g;
+            const int64_t block = (int64_t)kv_page(p, it.table, from, tile_lo, it.end, bad) * p.kv_heads + h;
             const int byte = p.v_scale[block];
             intx4 seen;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) seen[i] = (t + 2 * i >= see_lo && t + 2 * i < see_hi ? 0x3f80 : 0) | (t + 2 * i + 1 >= see_lo && t + 2 * i + 1 < see_hi ? 0x3f800000 : 0);
+            for (int i = 0; i < 4; ++i) seen[i] = (from + 2 * i >= see_lo && from + 2 * i < see_hi ? 0x3f80 : 0) | (from + 2 * i + 1 >= see_lo && from + 2 * i + 1 < see_hi ? 0x3f800000 : 0);
 #pragma unroll
             for (int j = 0; j < kTiles; ++j) {
                 const intx2 v = *(const intx2*)(p.v + ((block * D + 32 * j + n) << p.page_shift) + (t & in_page));
@@ -625,16 +653,11 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
                     s[u] = kv_mfma32(k, ql[w], s[u], kscale[u], q_scale - 4);
                 }
             }
-            if constexpr (CAP) {
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) s[u][e] = kv_score<true>(p, s[u][e]);
-            }
             kv_settle();
+            if constexpr (CAP) kv_cap(p, s);
             if (t0 < all_lo || t0 + kKvTileChunk > all_hi) {       // not every row sees all of it
                 asm volatile("");                                  // (a branch: as a selection it would cost every chunk)
-                const int hi = see_hi - t0 - 8 * g, lo = see_lo - t0 - 8 * g;
+                const int hi = see_hi - t0, lo = see_lo - t0;
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -648,8 +671,7 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
-            const float factor = CAP ? 1.f : p.scale;              // (without a cap the scores stay as they are: it goes into the exponent)
-            top = across_halves(top, Max()) * factor;
+            top = across_halves(top, Max()) * p.scale;             // (the scores stay as they are: their factor goes into the exponent)
             if (__any(top > m + kKvSlack)) {
                 top = fmaxf(m, top);
                 const float shrink = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top));
@@ -665,7 +687,7 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
                 float y[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    y[e] = __builtin_amdgcn_exp2f(s[q >> 1][8 * (q & 1) + e] * factor + base);
+                    y[e] = __builtin_amdgcn_exp2f(s[q >> 1][8 * (q & 1) + e] * p.scale + base);
                     l += y[e];
                 }
                 w[q] = kv_pack8(y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7]);
@@ -688,18 +710,23 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
     kv_settle();
     l = across_halves(l, Add());
     if (__any(bad)) m = NAN;
+    int at = tid;
+    asm volatile("" : "+v"(at));                                   // (the lane's place is formed again here, not kept over the loop: registers)
+    strip = (unsigned char*)&shared + (at >> 6) * 64 * D;
+    at &= 63;
+    const int own = at & 31, half = at >> 5;
     if (it.part >= 0) {
-        if (!valid) return;
-        const int64_t at = (int64_t)h * p.part_rows + it.part + r - it.r0;
-        if (g == 0) {
-            p.part_ml[at * 2] = m;
-            p.part_ml[at * 2 + 1] = l;
+        if (w0 + own >= it.rows) return;
+        const int64_t to = (int64_t)h * p.part_rows + it.part + w0 + own - it.r0;
+        if (half == 0) {
+            p.part_ml[to * 2] = m;
+            p.part_ml[to * 2 + 1] = l;
         }
 #pragma unroll
         for (int j = 0; j < kTiles; ++j)
 #pragma unroll
             for (int a = 0; a < 4; ++a)
-                *(floatx4*)(p.part_o + at * D + 32 * j + 8 * a + 4 * g) = floatx4{o[j][4 * a], o[j][4 * a + 1], o[j][4 * a + 2], o[j][4 * a + 3]};
+                *(floatx4*)(p.part_o + to * D + 32 * j + 8 * a + 4 * half) = floatx4{o[j][4 * a], o[j][4 * a + 1], o[j][4 * a + 2], o[j][4 * a + 3]};
         return;
     }
     const float inv = (m != m ? m : 1.f) / l;
@@ -707,13 +734,12 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
     for (int j = 0; j < kTiles; ++j)
 #pragma unroll
         for (int a = 0; a < 4; ++a)
-            *(intx2*)(strip + kv_strip<D>(n, 4 * j + a) + 8 * g) = intx2{(int)pack2_bf16(o[j][4 * a] * inv, o[j][4 * a + 1] * inv), (int)pack2_bf16(o[j][4 * a + 2] * inv, o[j][4 * a + 3] * inv)};
+            *(intx2*)(strip + kv_strip<D>(own, 4 * j + a) + 8 * half) = intx2{(int)pack2_bf16(o[j][4 * a] * inv, o[j][4 * a + 1] * inv), (int)pack2_bf16(o[j][4 * a + 2] * inv, o[j][4 * a + 3] * inv)};
     wave_sync();
-    int at = lane;
-    asm volatile("" : "+v"(at));                                   // (formed here, not kept over the loop: registers)
+    const int token_of = (w0 + own) / p.group;
 #pragma unroll
     for (int i = 0; i < kMoves; ++i) {
-        const int row = kMoveRows * i + at / (D / 8), token = __shfl(see_hi - 1 - it.past, row);
+        const int row = kMoveRows * i + at / (D / 8), token = __shfl(token_of, row);
         if (w0 + row < it.rows)
             *(intx4*)(p.out + (int64_t)(it.row0 + token) * p.out_stride + (h * p.group + w0 + row - token * p.group) * D + 8 * (at % (D / 8))) =
                 *(const intx4*)(strip + kv_strip<D>(row, at % (D / 8)));

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <new>
 #include <utility>
@@ -572,8 +573,11 @@ symb_status symb_kv_attention(symb_handle h, const symb_kv_batch* b, const symb_
         p.page_shift = page_shift(cache);
         p.window = window;
         p.part_rows = (int32_t)plan.part_rows;
-        p.scale = cap > 0.f ? scale / cap : scale * kLog2e;
-        p.cap = cap * kLog2e;
+        p.scale = scale * kLog2e;
+        if (cap > 0.f) {                  // (a quotient beyond fp32 is held at its end: scores of zero stay zero)
+            p.cap = std::min(cap / scale, FLT_MAX);
+            p.to_cap = std::min(kKvRoot * (scale / cap), FLT_MAX);
+        }
         const KvJoinParams jp{(const KvJoinItem*)(dev + o_join), p.part_o, p.part_ml, p.out, out_stride, p.kv_heads, p.group, p.part_rows};
         const KvItem* const items[3] = {(const KvItem*)(dev + o_items[0]), (const KvItem*)(dev + o_items[1]), (const KvItem*)(dev + o_items[2])};
         if (D == 128) st = cap > 0.f ? launch_attention<128, true>(h, p, plan, items, jp, s) : launch_attention<128, false>(h, p, plan, items, jp, s);
