@@ -121,7 +121,8 @@ symb_status symb_kv_workspace_bytes(const symb_kv_batch* b, const symb_kv_cache*
  * key head j / (q_heads / kv_heads); q_heads is a multiple of kv_heads.
  *   q, out [T][q_heads][head_dim] bf16 with row strides in elements (multiples of 8); out must not overlap q.
  *   scale > 0; cap >= 0, of any size (capping moves a score by 2^-20 of itself at most beside what the formula does); window >= 0.
- * What lies in hidden tokens, NaN included, never reaches a row.  Scores, maxima, sums and outputs are fp32, outputs rounded once; the weights exp(x - max) enter the
+ * What lies in hidden tokens, NaN and scales of any byte included, never reaches a row.  A value of 2^128 or more (a scale byte of 247 at least) is infinite or NaN to the rows that see it, all
+ * of a page whose scale byte is 0xff NaN.  Scores, maxima, sums and outputs are fp32, outputs rounded once; the weights exp(x - max) enter the
  * second product as bf16, 2^-9 of each at most (their sum takes them as they were).  Deterministic. */
 symb_status symb_kv_attention(symb_handle h, const symb_kv_batch* b, const symb_kv_cache* cache, const void* q, int64_t q_stride, int32_t q_heads,
                               void* out, int64_t out_stride, float scale, int32_t window, float cap, void* ws, size_t ws_bytes, void* stream);

@@ -204,11 +204,12 @@ __device__ __forceinline__ int kv_keep_bytes(int t, int lo, int hi) {      // of
     const unsigned above = a <= 0 ? ~0u : a < 4 ? ~0u << (8 * a) : 0u;
     return (int)(below & above);
 }
-// 0xff in the place of each E4M3 byte that is NaN, or (at a scale of 2^120) 256 or more: 2^128.
-__device__ __forceinline__ int kv_nan_bytes(int w, int scale_byte) {
-    const unsigned top = (((unsigned)w & 0x7f7f7f7fu) + (scale_byte >= 247 ? 0x08080808u : 0x01010101u)) & 0x80808080u;
-    return (int)((top >> 7) * 255u);
-}
+// 0xff in the place of each E4M3 byte that is NaN or, at its page's scale of 2^(byte - 127), 2^128 or more: as bf16 those widen to infinity.  From byte 247 on that begins at code (262 - byte) << 3;
+// byte 255 makes NaN of every code.  `step` takes the first of them to the sign bit.
+__device__ __forceinline__ unsigned kv_nan_step(int byte) { return 0x01010101u * (unsigned)(byte < 247 ? 1 : byte < 255 ? 8 * (byte - 246) : 128); }
+__device__ __forceinline__ int kv_nan_bytes(int w, unsigned step) { return (int)((((((unsigned)w & 0x7f7f7f7fu) + step) & 0x80808080u) >> 7) * 255u); }
+// The scale of what is left: a zero at scale 255 would be NaN again.
+__device__ __forceinline__ int kv_clean_scale(int byte) { return min(byte, 254); }
 // Four wavefronts share an item's tokens, chunk by chunk, each for all of its R x 16 rows, and join through shared memory.  Keys and values go straight from memory into
 // registers, the next chunk's keys and this one's values while this one's scores are formed: up to 16 KB on their way in every wavefront, and two wavefronts a SIMD for up to
 // 16 rows, one for more.
@@ -329,6 +330,7 @@ __device__ __forceinline__ void kv_rows(const KvAttentionParams& p, const KvItem
         }
         if (!whole) {
             int keep[4], found = 0;
+            unsigned step = kv_nan_step(vscale);
 #pragma unroll
             for (int i = 0; i < 4; ++i) keep[i] = kv_keep_bytes(t0 + 16 * g + 4 * i, any_lo, any_hi);
 #pragma unroll
@@ -336,12 +338,13 @@ __device__ __forceinline__ void kv_rows(const KvAttentionParams& p, const KvItem
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     v[j][i] &= keep[i];
-                    found |= kv_nan_bytes(v[j][i], vscale);
+                    found |= kv_nan_bytes(v[j][i], step);
                 }
             if (__any(found != 0)) {
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     intx8 seen, is;
+                    asm volatile("" : "+v"(step));                 // (found again where they are needed, not kept: registers)
                     int end = see_hi[r];
                     asm volatile("" : "+v"(end));
 #pragma unroll
@@ -352,18 +355,20 @@ __device__ __forceinline__ void kv_rows(const KvAttentionParams& p, const KvItem
 #pragma unroll
                     for (int j = 0; j < kTiles; ++j) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) is[i] = kv_nan_bytes(v[j][i], vscale) & 0x38383838;
+                        for (int i = 0; i < 4; ++i) is[i] = kv_nan_bytes(v[j][i], step) & 0x38383838;
                         const floatx4 cnt = kv_mfma(is, seen, floatx4{0, 0, 0, 0}, 127, 127);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[r][j][e] += cnt[e] != 0.f ? NAN : 0.f;
                         __builtin_amdgcn_sched_barrier(0);         // (one at a time: registers)
                     }
                 }
+                asm volatile("" : "+v"(step));
 #pragma unroll
                 for (int j = 0; j < kTiles; ++j)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) v[j][i] &= ~kv_nan_bytes(v[j][i], vscale);
+                    for (int i = 0; i < 4; ++i) v[j][i] &= ~kv_nan_bytes(v[j][i], step);
             }
+            vscale = kv_clean_scale(vscale);
         }
         const float scale = kv_scale(vscale);
 #pragma unroll
@@ -587,15 +592,16 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
             *(intx4*)(keys[buf] + k_lds + 32 * D * i) = kv[i];
             if (edge) {
                 int found = 0;
+                const unsigned step = kv_nan_step(next_vscale[u]);
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    const int v = vv[i][w] & kv_keep_bytes(t0 + 32 * u + 16 * vc + 4 * w, tile_lo, it.end), nan = kv_nan_bytes(v, next_vscale[u]);
+                    const int v = vv[i][w] & kv_keep_bytes(t0 + 32 * u + 16 * vc + 4 * w, tile_lo, it.end), nan = kv_nan_bytes(v, step);
                     found |= nan;
                     vv[i][w] = v & ~nan;
                 }
                 if (found) noted[buf] = t0;
             }
-            const float scale = kv_scale(next_vscale[u]);
+            const float scale = kv_scale(edge ? kv_clean_scale(next_vscale[u]) : next_vscale[u]);
 #pragma unroll
             for (int c = 0; c < 2; ++c) *(bf16x8*)(values[buf] + kv_lds(128, vd, 4 * u + 2 * vc + c)) = kv_widen(vv[i][2 * c], vv[i][2 * c + 1], scale);
         }
@@ -607,7 +613,7 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
         for (int q = 0; q < 4; ++q) {
             const int from = t0 + 16 * q, t = from + 8 * g;
             const int64_t block = (int64_t)kv_page(p, it.table, from, tile_lo, it.end, bad) * p.kv_heads + h;
-            const int byte = p.v_scale[block];
+            const unsigned step = kv_nan_step(p.v_scale[block]);
             intx4 seen;
 #pragma unroll
             for (int i = 0; i < 4; ++i) seen[i] = (from + 2 * i >= see_lo && from + 2 * i < see_hi ? 0x3f80 : 0) | (from + 2 * i + 1 >= see_lo && from + 2 * i + 1 < see_hi ? 0x3f800000 : 0);
@@ -617,7 +623,7 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
                 intx4 is;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int nan = kv_nan_bytes(v[i >> 1] & kv_keep_bytes(t + 4 * (i >> 1), tile_lo, it.end), byte) >> (16 * (i & 1));
+                    const int nan = kv_nan_bytes(v[i >> 1] & kv_keep_bytes(t + 4 * (i >> 1), tile_lo, it.end), step) >> (16 * (i & 1));
                     is[i] = (nan & 1 ? 0x3f80 : 0) | (nan & 0x100 ? 0x3f800000 : 0);
                 }
                 kv_floatx16 cnt;

@@ -9,12 +9,15 @@ from test_gpu_block_wide import _copies
 
 # rows of one key head: up to 16; 17 to 32 and 33 to 48 of enough segments; prompts that go 16 rows at a time; prompts in tiles of 128
 PATHS = {
-    "rows": dict(H=2, group=2, lens=[1, 5, 1], past=[700, 90, 0], many=False),
+    "rows": dict(H=2, group=2, lens=[1, 5, 1], past=[700, 126, 0], many=False),
     "runs": dict(H=2, group=2, lens=[60, 1, 40], past=[300, 130, 0], many=False),
     "rows32": dict(H=16, group=1, lens=[17, 30, 1], past=[500, 33, 90], many=True),
     "rows48": dict(H=16, group=1, lens=[40, 48], past=[300, 0], many=True),
     "tiles": dict(H=2, group=3, lens=[100, 43], past=[260, 64], many=True),
 }
+
+# of one segment of each: (segment, first token of a page that only its later rows see; window, end of a page that only its earlier rows see)
+EDGES = {"rows": (1, 128, 64, 64), "runs": (0, 320, 60, 256), "rows32": (0, 512, 60, 448), "rows48": (0, 320, 60, 256), "tiles": (0, 320, 60, 256)}
 
 
 class Path:
@@ -29,6 +32,19 @@ class Path:
         self.K, self.V = self.pg.fill(self.rng, std=std)
         self.table = self.pg.table.clone()
         self.T, self.heads, self.off = sum(self.lens), self.H * self.group, offsets(self.lens)
+
+    @classmethod
+    def with_edge(cls, name, D, P, seed, windowed):
+        """... with `page`, a page (of 32 or 64 tokens) of one segment that some of its rows see and others do not, its first token `first`, and `sees`, which of the batch's rows do."""
+        seg, first, window, end = EDGES[name]
+        self = cls(name, D, P, seed, window if windowed else 0)
+        self.seg, self.first = seg, end - P if windowed else first
+        self.page = int(self.pg.ids[seg, self.first // P])
+        pos = self.past[seg] + np.arange(self.lens[seg])
+        self.sees = np.zeros(self.T, bool)
+        self.sees[self.off[seg]:self.off[seg + 1]] = (pos >= self.first) & (not windowed or pos - window < self.first + P - 1)
+        assert 0 < self.sees.sum() < self.lens[seg]
+        return self
 
     def queries(self, std=1.0):
         return bf16(self.rng, self.T, self.heads, self.D, std=std)
