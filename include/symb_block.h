@@ -83,8 +83,8 @@ typedef struct {
     const int32_t* seg_offsets;    /* HOST, as in symb_batch */
     const int32_t* past;           /* HOST, num_segments entries: tokens in the cache before this call's (>= 0) */
     const int32_t* page_table;     /* DEVICE int32 [num_segments][table_stride].  Entries of pages that a call does not touch are not read.
-                                      A page number outside 0 .. num_pages-1 is never followed: its tokens are not stored, and a row
-                                      that should see them comes out NaN */
+                                      A page number outside 0 .. num_pages-1 is never followed: its tokens are not stored, and the rows
+                                      that see them, and no others, come out NaN */
     int32_t table_stride;          /* entries per segment: (past[i] + n_i) / page_tokens rounded up at least, for every segment with rows */
 } symb_kv_batch;
 

@@ -57,7 +57,7 @@ struct KvAttentionParams {
     const bf16* q;
     bf16* out;
     float* part_o;                        // [part rows][D], unnormalised
-    float* part_ml;                       // [part rows][2]: maximum (log2 units), sum
+    float* part_ml;                       // [part rows][2]: maximum (log2 units, never NaN), sum (NaN in a row that is)
     int64_t q_stride, out_stride;
     int32_t num_pages, kv_heads, group, page_shift, window;
     int32_t part_rows;                    // of one key head
@@ -172,17 +172,14 @@ __device__ __forceinline__ void kv_cap(const KvAttentionParams& p, V (&s)[N]) {
 }
 
 // The page of a token, the same in all lanes, so through the scalar cache: page numbers then arrive beside the keys and values under way, not behind them.  Only pages of the tokens
-// lo .. hi-1 are looked up (others are hidden: any page will do); a number outside the pool is reported, and page 0 read in its place.
+// lo .. hi-1 are looked up (others are hidden: any page will do); for a number outside the pool page 0 is read, with a key scale of 0xff: its tokens' scores
+// are NaN, so the rows that see them are, and the others are none the wiser.
 __device__ __forceinline__ int kv_look_up(const KvAttentionParams& p, int table, int token, int lo, int hi) {
     typedef const __attribute__((address_space(4))) int32_t* Table;
     return ((Table)(uintptr_t)p.page_table)[table + (max(min(token, hi - 1), lo) >> p.page_shift)];
 }
-__device__ __forceinline__ int kv_in_pool(const KvAttentionParams& p, int page, bool& bad) {
-    const bool in = (unsigned)page < (unsigned)p.num_pages;
-    bad |= !in;
-    return in ? page : 0;
-}
-__device__ __forceinline__ int kv_page(const KvAttentionParams& p, int table, int token, int lo, int hi, bool& bad) { return kv_in_pool(p, kv_look_up(p, table, token, lo, hi), bad); }
+__device__ __forceinline__ int kv_outside(const KvAttentionParams& p, int page) { return (unsigned)page < (unsigned)p.num_pages ? 0 : 0xff; }      // (to be or'd with the scale)
+__device__ __forceinline__ int kv_in_pool(int page, int outside) { return outside ? 0 : page; }
 
 __device__ __forceinline__ float kv_scale(int byte) { return as_float(byte << 23); }
 // Eight E4M3 values times a power of two as bf16.
@@ -238,7 +235,6 @@ __device__ __forceinline__ void kv_rows(const KvAttentionParams& p, const KvItem
         see_hi[r] = valid ? pos + 1 : 0;
         kv_query<D>(q[r], p.q + (int64_t)(it.row0 + row / p.group) * p.q_stride + (h * p.group + row % p.group) * D, valid, g);
     }
-    bool bad = false;
     floatx4 o[R][kTiles];
     float m[R], l[R];
 #pragma unroll
@@ -250,7 +246,7 @@ __device__ __forceinline__ void kv_rows(const KvAttentionParams& p, const KvItem
     }
     struct Keys {
         intx4 k[4][kWords];
-        int scale;
+        int scale, outside0, outside1;
     };
     const int in_page = (1 << p.page_shift) - 1;
     int page0, page1, next0, next1;                                // of a chunk's first and last 32 tokens, in the pool; numbers of the chunk whose keys are asked for next
@@ -259,8 +255,10 @@ __device__ __forceinline__ void kv_rows(const KvAttentionParams& p, const KvItem
         next1 = kv_look_up(p, it.table, t + 32, any_lo, it.end);
     };
     auto ask_keys = [&](Keys& c, int t0) {
-        page0 = kv_in_pool(p, next0, bad);
-        page1 = kv_in_pool(p, next1, bad);
+        c.outside0 = kv_outside(p, next0);
+        c.outside1 = kv_outside(p, next1);
+        page0 = kv_in_pool(next0, c.outside0);
+        page1 = kv_in_pool(next1, c.outside1);
         look_up(t0 + 4 * kKvChunk);
         const int64_t block = (int64_t)(n & 8 ? page1 : page0) * p.kv_heads + h;
         const unsigned char* k = p.k + ((block << p.page_shift) + ((t0 + kv_token(0, n)) & in_page)) * D + 16 * g;
@@ -281,6 +279,7 @@ __device__ __forceinline__ void kv_rows(const KvAttentionParams& p, const KvItem
     };
     auto work = [&](const Keys& c, int t0) {
         const bool whole = t0 >= all_lo && t0 + kKvChunk <= all_hi;                    // every row sees all of it
+        const int kscale = c.scale | (n & 8 ? c.outside1 : c.outside0);
         bf16x8 w[R][2];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -288,8 +287,8 @@ __device__ __forceinline__ void kv_rows(const KvAttentionParams& p, const KvItem
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const intx8 a = __builtin_shufflevector(c.k[i][0], c.k[i][kWords - 1], 0, 1, 2, 3, 4, 5, 6, 7);
-                s[i] = kv_mfma(a, q[r].hi, floatx4{0, 0, 0, 0}, c.scale, q[r].hi_scale);
-                if constexpr (D == 128) s[i] = kv_mfma(a, q[r].lo, s[i], c.scale, q[r].lo_scale);
+                s[i] = kv_mfma(a, q[r].hi, floatx4{0, 0, 0, 0}, kscale, q[r].hi_scale);
+                if constexpr (D == 128) s[i] = kv_mfma(a, q[r].lo, s[i], kscale, q[r].lo_scale);
             }
             kv_settle();
             if constexpr (CAP) kv_cap(p, s);
@@ -401,11 +400,9 @@ __device__ __forceinline__ void kv_rows(const KvAttentionParams& p, const KvItem
         t0 = t2;
     }
     // the four wavefronts' results: o 2^(m - M) added up, and so the sums
-    const bool any_bad = __any(bad);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         l[r] = across_rows(l[r], Add());
-        if (any_bad) m[r] = NAN;
         if (g == 0) {
             stat[r][wave][n][0] = m[r];
             stat[r][wave][n][1] = l[r];
@@ -415,16 +412,11 @@ __device__ __forceinline__ void kv_rows(const KvAttentionParams& p, const KvItem
     for (int r = 0; r < R; ++r) {
         __syncthreads();
         float M = -INFINITY, sum = 0.f;
-        bool nan = false;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            M = fmaxf(M, stat[r][k][n][0]);
-            nan |= stat[r][k][n][0] != stat[r][k][n][0];
-        }
+        for (int k = 0; k < 4; ++k) M = fmaxf(M, stat[r][k][n][0]);
         const float base = M == -INFINITY ? 0.f : M;
 #pragma unroll
         for (int k = 0; k < 4; ++k) sum += stat[r][k][n][1] * __builtin_amdgcn_exp2f(stat[r][k][n][0] - base);
-        if (nan) M = sum = NAN;
         // without parts the outputs leave here as they are: the division goes into the factor
         const float mine = __builtin_amdgcn_exp2f(m[r] - base) * (it.part >= 0 ? 1.f : 1.f / sum);
 #pragma unroll
@@ -513,19 +505,20 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
     const int tile_all_hi = it.past + it.r0 / p.group + 1, tile_all_lo = p.window ? max(it.past + min(it.r0 + kKvTileRows - 1, it.rows - 1) / p.group + 1 - p.window, 0) : 0;
     const int tile_lo = p.window ? max(it.past + it.r0 / p.group + 1 - p.window, 0) : 0;
 
-    bool bad = false;
     // Keys and values of a chunk, from memory to registers and from there to shared memory: pass i of the workgroup (head of 128), or half i of it (head of 64), moves
     // the tokens 32i .. 32i+31, so that a page's address is the same in a wavefront's lanes.
     const int in_page = (1 << p.page_shift) - 1, kt = tid / (D / 16), kc = tid % (D / 16), vd = D == 128 ? tid >> 1 : (tid & 127) >> 1, vc = tid & 1;
     const int k_off = (kt & in_page & 31) * D + 16 * kc, v_off = (vd << p.page_shift) + 16 * vc;
     const int k_lds = kv_lds(D, kt, kc);                       // (32 tokens on: a fixed distance)
     intx4 kv[kVecs], vv[kVecs];
-    int kscale[2], next_kscale[2], next_vscale[2];
+    int kscale[2], next_kscale[2], next_vscale[2], outside[2];
     auto ask = [&](int t0) {
         int64_t block[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            block[u] = (int64_t)kv_page(p, it.table, t0 + 32 * u, tile_lo, it.end, bad) * p.kv_heads + h;
+            const int page = kv_look_up(p, it.table, t0 + 32 * u, tile_lo, it.end);
+            outside[u] = kv_outside(p, page);
+            block[u] = (int64_t)kv_in_pool(page, outside[u]) * p.kv_heads + h;
             next_kscale[u] = p.k_scale[block[u]];
             next_vscale[u] = p.v_scale[block[u]];
         }
@@ -606,13 +599,14 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
             for (int c = 0; c < 2; ++c) *(bf16x8*)(values[buf] + kv_lds(128, vd, 4 * u + 2 * vc + c)) = kv_widen(vv[i][2 * c], vv[i][2 * c + 1], scale);
         }
 #pragma unroll
-        for (int u = 0; u < 2; ++u) kscale[u] = next_kscale[u];
+        for (int u = 0; u < 2; ++u) kscale[u] = next_kscale[u] | outside[u];
     };
     // NaN that `put` has cleared, to the rows that see it: ones in its places times ones where a row sees the token.
     auto give_nan = [&](int t0) {
         for (int q = 0; q < 4; ++q) {
             const int from = t0 + 16 * q, t = from + 8 * g;
-            const int64_t block = (int64_t)kv_page(p, it.table, from, tile_lo, it.end, bad) * p.kv_heads + h;
+            const int page = kv_look_up(p, it.table, from, tile_lo, it.end);
+            const int64_t block = (int64_t)kv_in_pool(page, kv_outside(p, page)) * p.kv_heads + h;
             const unsigned step = kv_nan_step(p.v_scale[block]);
             intx4 seen;
 #pragma unroll
@@ -715,7 +709,6 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
     }
     kv_settle();
     l = across_halves(l, Add());
-    if (__any(bad)) m = NAN;
     int at = tid;
     asm volatile("" : "+v"(at));                                   // (the lane's place is formed again here, not kept over the loop: registers)
     strip = (unsigned char*)&shared + (at >> 6) * 64 * D;
@@ -735,7 +728,7 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
                 *(floatx4*)(p.part_o + to * D + 32 * j + 8 * a + 4 * half) = floatx4{o[j][4 * a], o[j][4 * a + 1], o[j][4 * a + 2], o[j][4 * a + 3]};
         return;
     }
-    const float inv = (m != m ? m : 1.f) / l;
+    const float inv = 1.f / l;
 #pragma unroll
     for (int j = 0; j < kTiles; ++j)
 #pragma unroll
@@ -795,13 +788,9 @@ SYMB_KERNEL __launch_bounds__(256) void symb_kv_join_kernel(KvJoinParams p) {
     const int h = blockIdx.x % p.kv_heads, row = it.r0 + blockIdx.y, tid = threadIdx.x;
     if (row >= it.rows) return;
     const int64_t at = (int64_t)h * p.part_rows + it.part0 + blockIdx.y;
-    float M = -INFINITY, bad = 0.f;
-    for (int k = tid; k < it.parts; k += 256) {
-        const float m = p.part_ml[(at + (int64_t)it.stride * k) * 2];
-        if (m != m) bad = 1.f;
-        M = fmaxf(M, m);
-    }
-    M = across_wave(bad != 0.f ? INFINITY : M, Max());            // (no maximum is infinite without the row being NaN)
+    float M = -INFINITY;
+    for (int k = tid; k < it.parts; k += 256) M = fmaxf(M, p.part_ml[(at + (int64_t)it.stride * k) * 2]);
+    M = across_wave(M, Max());
     if ((tid & 63) == 0) top[tid >> 6] = M;
     __syncthreads();
     M = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
@@ -827,7 +816,6 @@ SYMB_KERNEL __launch_bounds__(256) void symb_kv_join_kernel(KvJoinParams p) {
         sum += sums[k];
         v += part[k][tid];
     }
-    if (M == INFINITY) sum = NAN;
     *(intx2*)(p.out + (int64_t)(it.row0 + row / p.group) * p.out_stride + (h * p.group + row % p.group) * D + d) =
         intx2{(int)pack2_bf16(v[0] / sum, v[1] / sum), (int)pack2_bf16(v[2] / sum, v[3] / sum)};
 }
@@ -841,12 +829,7 @@ SYMB_KERNEL __launch_bounds__(256) void symb_kv_join_rows_kernel(KvJoinParams p)
         const int row = it.r0 + r;
         const int64_t at = (int64_t)h * p.part_rows + it.part0 + r;
         float M = -INFINITY;
-        bool bad = false;
-        for (int k = 0; k < it.parts; ++k) {
-            const float m = p.part_ml[(at + (int64_t)it.stride * k) * 2];
-            bad |= m != m;
-            M = fmaxf(M, m);
-        }
+        for (int k = 0; k < it.parts; ++k) M = fmaxf(M, p.part_ml[(at + (int64_t)it.stride * k) * 2]);
         const float base = M == -INFINITY ? 0.f : M;
         float sum = 0.f;
         floatx4 v = floatx4{0, 0, 0, 0};
@@ -857,7 +840,6 @@ SYMB_KERNEL __launch_bounds__(256) void symb_kv_join_rows_kernel(KvJoinParams p)
             sum += p.part_ml[a * 2 + 1] * f;
             v += *(const floatx4*)(p.part_o + a * D + d) * f;
         }
-        if (bad) sum = NAN;
         *(intx2*)(p.out + (int64_t)(it.row0 + row / p.group) * p.out_stride + (h * p.group + row % p.group) * D + d) =
             intx2{(int)pack2_bf16(v[0] / sum, v[1] / sum), (int)pack2_bf16(v[2] / sum, v[3] / sum)};
     }
