@@ -28,11 +28,18 @@ def _workspace(n: int) -> torch.Tensor:
     return torch.empty(max(n, 256), device="cuda", dtype=torch.uint8)
 
 
+def _stream(stream: int):
+    return torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+
+
 def _on(stream: int):
     """Torch's own work (what it allocates, what it copies) in the order of `stream`."""
-    if stream == torch.cuda.current_stream().cuda_stream:
-        return contextlib.nullcontext()
-    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream())
+    return contextlib.nullcontext() if stream == torch.cuda.current_stream().cuda_stream else torch.cuda.stream(_stream(stream))
+
+
+def _also_on(t: torch.Tensor, stream: int) -> None:
+    """The memory of a tensor that was allocated in another stream's order is given on only when what `stream` has been given so far is done as well."""
+    t.record_stream(_stream(stream))
 
 
 def rotation_table(positions: int, dim: int, base: float = 10000.0) -> torch.Tensor:
@@ -42,7 +49,8 @@ def rotation_table(positions: int, dim: int, base: float = 10000.0) -> torch.Ten
 
 
 class NormedProjection:
-    """x -> adapter_i(W norm_i(x)) for the rows of every client i, and its backward pass.  `norms` and `adapters` hold each client's own parameters and where its gradients go."""
+    """x -> adapter_i(W norm_i(x)) for the rows of every client i, and its backward pass.  `norms` and `adapters` hold each client's own parameters and where its gradients go.
+    Its buffers are allocated in the order of the stream that uses them, and again when another one does: results are there in that stream's order, and stay until the next call of the same pass."""
 
     def __init__(self, handle, W: torch.Tensor, lens: Sequence[int], norms: Sequence[sb.Norm], adapters: Sequence[sb.Adapter], kind: int = sb.SYMB_NORM_LAYER,
                  eps: float = 1e-5, weight_base: float = 0.0):
@@ -50,19 +58,35 @@ class NormedProjection:
         d_out, d_in = W.shape
         off = _offsets(lens)
         self.norm, self.linear = sb.NormBatch(d_in, off, norms, kind, eps, weight_base), sb.Batch(d_in, d_out, off, adapters)
-        T = off[-1]
-        self.N, self.Y = (torch.empty(T, d, device="cuda", dtype=BF16) for d in (d_in, d_out))
-        self.dN, self.dX = (torch.empty(T, d_in, device="cuda", dtype=BF16) for _ in range(2))
-        self.ws = _workspace(max([sb.symb_norm_workspace_bytes(self.norm)] +
-                                 [sb.symb_workspace_bytes(self.linear, op) for op in (sb.SYMB_OP_FWD, sb.SYMB_OP_BWD_INPUT, sb.SYMB_OP_ADAPTER_GRAD)]))
+        self.T, self.d_in, self.d_out = off[-1], d_in, d_out
+        self.N = self.Y = self.dN = self.dX = self.ws = None
+        self._streams: Dict[str, int] = {}                             # of each buffer
+        self.ws_bytes = max([sb.symb_norm_workspace_bytes(self.norm)] +
+                            [sb.symb_workspace_bytes(self.linear, op) for op in (sb.SYMB_OP_FWD, sb.SYMB_OP_BWD_INPUT, sb.SYMB_OP_ADAPTER_GRAD)])
+
+    def _buffers(self, stream: int, **widths) -> None:
+        with _on(stream):
+            for name, d in widths.items():
+                if self._streams.get(name) != stream:
+                    setattr(self, name, torch.empty(self.T, d, device="cuda", dtype=BF16))
+                    self._streams[name] = stream
+            if self._streams.get("ws") != stream:
+                self.ws = _workspace(self.ws_bytes)
+                self._streams["ws"] = stream
 
     def forward(self, X: torch.Tensor, bias=None, stream: int = 0) -> torch.Tensor:
+        self._buffers(stream, N=self.d_in, Y=self.d_out)
         sb.symb_norm_fwd(self.h, self.norm, X, self.N, stream)
         sb.symb_base_linear_fwd(self.h, self.linear, self.N, self.W, bias, self.Y, None, self.ws, stream)
         return self.Y
 
     def backward(self, X: torch.Tensor, dY: torch.Tensor, flags: int = sb.SYMB_GRAD_OVERWRITE, stream: int = 0) -> torch.Tensor:
-        """dX; the adapters' and norms' gradients go to their own tensors.  Needs the normed rows of the forward pass on the same rows."""
+        """dX; the adapters' and norms' gradients go to their own tensors.  Needs the normed rows of the forward pass on the same rows, and their being there in the order of `stream`."""
+        if self.N is None:
+            raise RuntimeError("backward needs the normed rows of a forward pass")
+        self._buffers(stream, dN=self.d_in, dX=self.d_in)
+        if self._streams["N"] != stream:
+            _also_on(self.N, stream)
         sb.symb_adapter_grad(self.h, self.linear, self.N, dY, None, flags, self.ws, stream)
         sb.symb_base_linear_bwd_input(self.h, self.linear, dY, self.W, self.dN, sb.SYMB_BWD_FULL, self.ws, stream)
         sb.symb_norm_bwd(self.h, self.norm, X, self.dN, self.dX, flags, self.ws, stream)
