@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import contextlib
 from dataclasses import dataclass, field
-from typing import Dict, List, Sequence
+from typing import Dict, List, Optional, Sequence
 
 import torch
 
@@ -104,12 +104,18 @@ class Client:
 
 class AttentionBlock:
     """norm, query / key / value projections, cache append with rotation, attention, output projection: each for the whole batch, each client with its own norm, adapters and cache
-    pages.  The residual is the caller's."""
+    pages.  The residual is the caller's.  `scale`: what scores are multiplied with, head_dim ** -0.5 unless the model says otherwise; `biases`: bf16, by projection like W, those that it has."""
 
     def __init__(self, handle, W: Dict[str, torch.Tensor], heads: int, cache: sb.KvCache, rotation=None, kind: int = sb.SYMB_NORM_RMS, eps: float = 1e-6,
-                 weight_base: float = 0.0, window: int = 0, cap: float = 0.0):
+                 weight_base: float = 0.0, window: int = 0, cap: float = 0.0, scale: Optional[float] = None, biases: Optional[Dict[str, torch.Tensor]] = None):
+        if set(biases or {}) - set(W):
+            raise ValueError(f"biases of {sorted(biases)} for projections {sorted(W)}")
+        for p, b in (biases or {}).items():
+            if b.dtype is not BF16 or b.shape != W[p].shape[:1] or not b.is_contiguous():
+                raise ValueError(f"bias of {p}: dense [{W[p].shape[0]}] of bfloat16 expected, got {tuple(b.shape)} of {b.dtype}")
         self.h, self.W, self.heads, self.cache, self.rotation = handle, W, heads, cache, rotation
         self.kind, self.eps, self.weight_base, self.window, self.cap = kind, eps, weight_base, window, cap
+        self.scale, self.biases = cache.head_dim ** -0.5 if scale is None else scale, dict(biases or {})
         self.free = list(range(cache.num_pages - 1, -1, -1))           # pages that no client has
 
     def _reserve(self, c: Client, tokens: int) -> None:
@@ -148,12 +154,12 @@ class AttentionBlock:
         heads = {p: torch.empty(T, n, D, device="cuda", dtype=BF16) for p, n in rows.items()}
         sb.symb_norm_fwd(self.h, sb.NormBatch(width, off, [c.norm for c in clients], self.kind, self.eps, self.weight_base), X, N, stream)
         for p in rows:
-            sb.symb_base_linear_fwd(self.h, batch[p], N, self.W[p], None, heads[p], None, ws, stream)
+            sb.symb_base_linear_fwd(self.h, batch[p], N, self.W[p], self.biases.get(p), heads[p], None, ws, stream)
         q = heads["q"]
         sb.symb_kv_append(self.h, kv, self.cache, self.rotation, q, q, heads["k"], heads["v"], stream)
         attended = torch.empty_like(q)
-        sb.symb_kv_attention(self.h, kv, self.cache, q, attended, D ** -0.5, self.window, self.cap, ws, stream)
-        sb.symb_base_linear_fwd(self.h, batch["o"], attended, self.W["o"], None, out, None, ws, stream)
+        sb.symb_kv_attention(self.h, kv, self.cache, q, attended, self.scale, self.window, self.cap, ws, stream)
+        sb.symb_base_linear_fwd(self.h, batch["o"], attended, self.W["o"], self.biases.get("o"), out, None, ws, stream)
         for c, n in zip(clients, lens):
             c.past += n
         return out
