@@ -6,6 +6,10 @@
  * ordering and errors are symb.h's: bf16 activations, DEVICE tensors owned by the caller, 16-byte aligned, HOST descriptors copied during the
  * call, everything enqueued on `stream`, all checks before the first launch.  A batch without rows is legal and enqueues nothing, except
  * that symb_norm_bwd writes the zeros of SYMB_GRAD_OVERWRITE.
+ *
+ * A call's descriptors fill one slot of 2 MiB (symb.h): 36 bytes a segment for symb_norm_fwd; 32 a segment, 24 a gradient and 16 a chunk of rows (768 more than segments at most) for symb_norm_bwd; 16 for
+ * every page that a segment's new tokens go to (131072 of them); 32 for every work item of symb_kv_attention, of which a key head's rows (tokens times the query heads that share it) make at least one
+ * in 128.  More is SYMB_ERR_UNSUPPORTED, from the workspace queries too: one prompt of 170000 tokens with 48 query heads on a key head is about the longest; a longer one is given in several calls.
  */
 #ifndef SYMB_BLOCK_H
 #define SYMB_BLOCK_H

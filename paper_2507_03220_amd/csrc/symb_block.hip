@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
+#include <initializer_list>
 #include <new>
 #include <utility>
 #include <vector>
@@ -36,6 +37,13 @@ symb_status check_segments(symb_handle h, int32_t S, const int32_t* off) {
     for (int i = 0; i < S; ++i)
         if (off[i + 1] < off[i]) return fail(h, SYMB_ERR_BAD_SEGMENTS, "seg_offsets decrease at segment %d", i);
     return SYMB_OK;
+}
+
+// The size of a Blob of these lists: what the workspace queries refuse as the calls do.
+size_t blob_bytes(std::initializer_list<std::pair<size_t, size_t>> lists) {              // (entries, bytes of one)
+    size_t n = 0;
+    for (const auto& l : lists) n = align_up(n, 16) + std::max<size_t>(l.first, 1) * l.second;
+    return n;
 }
 
 // ---- norms -----------------------------------------------------------------------------------
@@ -123,6 +131,9 @@ symb_status plan_norm(symb_handle h, const symb_norm_batch* b, NormPlan& plan) {
         if (wanted) plan.groups.push_back(g);
         at = to;
     }
+    if (plan.groups.size() > 65535) return fail(h, SYMB_ERR_UNSUPPORTED, "%zu different weight gradients: 65535 at most", plan.groups.size());
+    const size_t need = blob_bytes({{(size_t)S, sizeof(NormDesc)}, {plan.chunks.size(), sizeof(NormChunk)}, {plan.groups.size(), sizeof(NormGroup)}});
+    if (need > kSlotBytes) return fail(h, SYMB_ERR_UNSUPPORTED, "batch descriptors need %zu bytes, capacity is %zu", need, kSlotBytes);
     return SYMB_OK;
 }
 size_t norm_part_bytes(const NormPlan& plan, int width) { return align_up((size_t)plan.parts * width * sizeof(float), 256); }
@@ -255,8 +266,7 @@ int64_t plan_quota(const std::vector<int32_t>& chunks, int kv_heads, const KvKer
     return most - low < k.worth ? most : low;
 }
 
-KvPlan plan_attention(const symb_kv_batch* b, const symb_kv_cache* c, int q_heads, int window) {
-    KvPlan plan;
+symb_status plan_attention(symb_handle h, const symb_kv_batch* b, const symb_kv_cache* c, int q_heads, int window, KvPlan& plan) {
     const int group = q_heads / c->kv_heads;
     std::vector<KvItem> runs;
     std::vector<int32_t> chunks;
@@ -318,7 +328,12 @@ KvPlan plan_attention(const symb_kv_batch* b, const symb_kv_cache* c, int q_head
             plan.tiles = (int)items.size();
         }
     }
-    return plan;
+    size_t all = plan.joins.size();
+    for (const auto& list : plan.items) all += list.size();
+    if ((int64_t)all * c->kv_heads > INT32_MAX || plan.part_rows > INT32_MAX) return fail(h, SYMB_ERR_UNSUPPORTED, "%zu work items of %d key heads", all, c->kv_heads);
+    const size_t need = blob_bytes({{plan.items[0].size(), sizeof(KvItem)}, {plan.items[1].size(), sizeof(KvItem)}, {plan.items[2].size(), sizeof(KvItem)}, {plan.joins.size(), sizeof(KvJoinItem)}});
+    if (need > kSlotBytes) return fail(h, SYMB_ERR_UNSUPPORTED, "%zu work items need %zu bytes of descriptors, capacity is %zu", all, need, kSlotBytes);
+    return SYMB_OK;
 }
 size_t part_ml_bytes(const KvPlan& plan, int kv_heads) { return align_up((size_t)plan.part_rows * kv_heads * 2 * sizeof(float), 256); }
 size_t part_bytes(const KvPlan& plan, const symb_kv_cache* c) {
@@ -329,9 +344,13 @@ symb_status check_attention(symb_handle h, const symb_kv_batch* b, const symb_kv
     if (st != SYMB_OK) return st;
     if (q_heads <= 0 || q_heads % c->kv_heads) return fail(h, SYMB_ERR_INVALID_ARG, "q_heads must be a positive multiple of kv_heads");
     if (window < 0) return fail(h, SYMB_ERR_INVALID_ARG, "window is negative");
-    for (int i = 0; i < b->num_segments; ++i)
-        if ((int64_t)(b->seg_offsets[i + 1] - b->seg_offsets[i]) * (q_heads / c->kv_heads) > INT32_MAX - 1024)
-            return fail(h, SYMB_ERR_UNSUPPORTED, "segment %d has too many rows", i);
+    int64_t least = 0;                                            // work items, before any list of them is made
+    for (int i = 0; i < b->num_segments; ++i) {
+        const int64_t rows = (int64_t)(b->seg_offsets[i + 1] - b->seg_offsets[i]) * (q_heads / c->kv_heads);
+        if (rows > INT32_MAX - 1024) return fail(h, SYMB_ERR_UNSUPPORTED, "segment %d has too many rows", i);
+        least += (rows + kKvTileRows - 1) / kKvTileRows;
+    }
+    if (least * (int64_t)sizeof(KvItem) > (int64_t)kSlotBytes) return fail(h, SYMB_ERR_UNSUPPORTED, "%lld work items at least, %zu fit the descriptors", (long long)least, kSlotBytes / sizeof(KvItem));
     return SYMB_OK;
 }
 
@@ -415,7 +434,6 @@ symb_status symb_norm_bwd(symb_handle h, const symb_norm_batch* b, const void* X
         if (misaligned16(X) || misaligned16(dY) || misaligned16(dX) || misaligned16(ws)) return fail(h, SYMB_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
         const size_t part = norm_part_bytes(plan, b->width);
         if (2 * part > ws_bytes || (part && !ws)) return fail(h, SYMB_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : 0, 2 * part);
-        if (plan.groups.size() > 65535) return fail(h, SYMB_ERR_UNSUPPORTED, "%zu different weight gradients: 65535 at most", plan.groups.size());
         hipStream_t s = (hipStream_t)stream;
         const std::vector<NormDesc> nd = norm_descs(b);
         Blob blob;
@@ -466,6 +484,11 @@ symb_status symb_kv_append(symb_handle h, const symb_kv_batch* b, const symb_kv_
         if ((st = check_rows(h, v, v_stride, (int64_t)cache->kv_heads * D, "v")) != SYMB_OK) return st;
         if (q && (st = check_rows(h, q, q_stride, (int64_t)q_heads * D, "q")) != SYMB_OK) return st;
         if (q && (st = check_rows(h, q_out, q_out_stride, (int64_t)q_heads * D, "q_out")) != SYMB_OK) return st;
+        size_t count = 0;
+        for (int i = 0; i < S; ++i)
+            if (b->seg_offsets[i + 1] > b->seg_offsets[i])
+                count += (size_t)(((int64_t)b->past[i] + b->seg_offsets[i + 1] - b->seg_offsets[i] - 1) / P - b->past[i] / P + 1);
+        if (count * sizeof(KvPage) > kSlotBytes) return fail(h, SYMB_ERR_UNSUPPORTED, "new tokens in %zu pages, %zu fit the descriptors", count, kSlotBytes / sizeof(KvPage));
         std::vector<KvPage> pages;
         int rows = 0;
         for (int i = 0; i < S; ++i)
@@ -519,9 +542,11 @@ symb_status symb_kv_append(symb_handle h, const symb_kv_batch* b, const symb_kv_
 symb_status symb_kv_workspace_bytes(const symb_kv_batch* b, const symb_kv_cache* cache, int32_t q_heads, int32_t window, size_t* out) {
     return guarded(nullptr, [&]() -> symb_status {
         if (!out) return fail(nullptr, SYMB_ERR_INVALID_ARG, "out is null");
-        const symb_status st = check_attention(nullptr, b, cache, q_heads, window);
+        symb_status st = check_attention(nullptr, b, cache, q_heads, window);
         if (st != SYMB_OK) return st;
-        *out = part_bytes(plan_attention(b, cache, q_heads, window), cache);
+        KvPlan plan;
+        if ((st = plan_attention(nullptr, b, cache, q_heads, window, plan)) != SYMB_OK) return st;
+        *out = part_bytes(plan, cache);
         return SYMB_OK;
     });
 }
@@ -540,13 +565,11 @@ symb_status symb_kv_attention(symb_handle h, const symb_kv_batch* b, const symb_
         const int D = cache->head_dim;
         if ((st = check_rows(h, q, q_stride, (int64_t)q_heads * D, "q")) != SYMB_OK) return st;
         if ((st = check_rows(h, out, out_stride, (int64_t)q_heads * D, "out")) != SYMB_OK) return st;
-        const KvPlan plan = plan_attention(b, cache, q_heads, window);
+        KvPlan plan;
+        if ((st = plan_attention(h, b, cache, q_heads, window, plan)) != SYMB_OK) return st;
         const size_t need = part_bytes(plan, cache);
         if (need && (!ws || ws_bytes < need)) return fail(h, SYMB_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : 0, need);
         if (need && misaligned16(ws)) return fail(h, SYMB_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
-        size_t work = plan.joins.size();
-        for (const auto& r : plan.items) work += r.size();
-        if ((int64_t)work * cache->kv_heads > INT32_MAX || plan.part_rows > INT32_MAX) return fail(h, SYMB_ERR_UNSUPPORTED, "%zu work items of %d key heads", work, cache->kv_heads);
         hipStream_t s = (hipStream_t)stream;
         Blob blob;
         size_t o_items[3];
