@@ -216,7 +216,7 @@ def _head_rows(t, what: str, shape) -> int:
     apart, head, element = t.stride() if t.dim() == 3 else (0, 0, 0)
     if t.dtype is not _dtype("bfloat16") or t.shape != shape or element != 1 or (head != shape[2] and shape[1] > 1):
         raise ValueError(f"{what}: {list(shape)} of bfloat16 with whole rows expected, got {tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
-    return apart if shape[0] > 1 else max(apart, shape[1] * shape[2])
+    return apart if shape[0] > 1 else shape[1] * shape[2]      # (of a single row it says nothing)
 
 
 @dataclass
