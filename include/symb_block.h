@@ -56,7 +56,7 @@ symb_status symb_norm_workspace_bytes(const symb_norm_batch* b, size_t* out);
 symb_status symb_norm_fwd(symb_handle h, const symb_norm_batch* b, const void* X, void* Y, void* stream);
 
 /* X, dY, dX [T][width] bf16, dense rows.  dX may be dY or X.  flags: SYMB_GRAD_OVERWRITE or SYMB_GRAD_ACCUMULATE for dweight and dbias; an
- * empty segment writes zeros or leaves them.  Deterministic: sums are formed in a fixed order. */
+ * empty segment writes zeros or leaves them.  Deterministic: sums are formed in a fixed order (in chunks of rows that the batch as a whole decides on; dX hangs on its own row alone). */
 symb_status symb_norm_bwd(symb_handle h, const symb_norm_batch* b, const void* X, const void* dY, void* dX, uint32_t flags, void* ws,
                           size_t ws_bytes, void* stream);
 
@@ -111,7 +111,7 @@ typedef struct {
  * For each touched page and head: the smallest power of two that brings the largest finite new value to 448 at most, and no smaller than the
  * page's scale if it holds earlier tokens of the segment (slots before the first new one; these are held again where the scale
  * grows).  Values are turned in fp32 and rounded once, to nearest even; infinities and NaN become NaN and leave the scale alone.  Slots behind the last
- * new token keep their bytes.  Segments of one call must not share a page that one of them writes. */
+ * new token keep their bytes.  A page that is given zeros alone gets the smallest scale, 2^-126.  Segments of one call must not share a page that one of them writes. */
 symb_status symb_kv_append(symb_handle h, const symb_kv_batch* b, const symb_kv_cache* cache, const symb_rotation* rotation, const void* q,
                            int64_t q_stride, int32_t q_heads, void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride, const void* v,
                            int64_t v_stride, void* stream);
@@ -124,10 +124,14 @@ symb_status symb_kv_workspace_bytes(const symb_kv_batch* b, const symb_kv_cache*
  * over the tokens s of the row's segment with  position - window < s <= position  (window 0: all up to its position).  Query head j reads
  * key head j / (q_heads / kv_heads); q_heads is a multiple of kv_heads.
  *   q, out [T][q_heads][head_dim] bf16 with row strides in elements (multiples of 8); out must not overlap q.
- *   scale > 0; cap >= 0, of any size (capping moves a score by 2^-20 of itself at most beside what the formula does); window >= 0.
+ *   scale > 0; cap >= 0, of any size (capping is good to 2^-19 of a score); window >= 0.
  * What lies in hidden tokens, NaN and scales of any byte included, never reaches a row.  A value of 2^128 or more (a scale byte of 247 at least) is infinite or NaN to the rows that see it, all
- * of a page whose scale byte is 0xff NaN.  Scores, maxima, sums and outputs are fp32, outputs rounded once; the weights exp(x - max) enter the
- * second product as bf16, 2^-9 of each at most (their sum takes them as they were).  Deterministic. */
+ * of a page whose scale byte is 0xff NaN.
+ * What is rounded: a row's query enters the scores as two E4M3 terms, exact for elements from 2^-13 of its largest on, off by 2^-21 of the largest (taken as 2^-93 at least) at most below; of a score's products those some
+ * 2^-15 below the largest are dropped; the weights exp(x - max) enter the second product as bf16, 2^-9 of each at most (their sum takes them as they were).  Scores, maxima, sums and outputs are
+ * otherwise fp32, outputs rounded once.
+ * The same batch gives the same bits.  The same segment in another batch may not: its rows' kernel and the split of its tokens are chosen for the batch as a whole.
+ * Under capture, `past` and the work lists made of it become part of the graph: a replay attends from the same positions (and symb_kv_append appends at them). */
 symb_status symb_kv_attention(symb_handle h, const symb_kv_batch* b, const symb_kv_cache* cache, const void* q, int64_t q_stride, int32_t q_heads,
                               void* out, int64_t out_stride, float scale, int32_t window, float cap, void* ws, size_t ws_bytes, void* stream);
 

@@ -5,7 +5,7 @@
 // computed in one pass over the tokens: m, the sum and the unnormalised output are kept in fp32 and scaled when m grows.
 //
 // Scores: v_mfma_scale_f32_*_f8f6f4 takes the keys' bytes as they lie and their page's E8M0 scale beside them, so no key is widened.  A bf16 query has eight significant bits,
-// two E4M3 terms: q = (hi + lo / 16) 2^e exactly for elements within 2^-14 of the row's largest (others to 2^-18 of it), one product each, which at twice
+// two E4M3 terms: q = (hi + lo / 16) 2^e exactly for elements from 2^-13 of the row's largest on (others to 2^-21 of it), one product each, which at twice
 // bf16's rate is what a bf16 product would cost.  Inside one instruction the matrix unit drops what lies more than about 2^-15 below its largest product: measured
 // relative errors of 1e-5 to 5e-5 of a sum, not growing with the number of instructions (the accumulator is full fp32).
 // Outputs: weights as bf16 (2^-9 of each; their sum is taken before they are rounded), values widened to bf16, exactly, scale included (v_cvt_scalef32_pk_bf16_fp8: two
@@ -15,8 +15,8 @@
 // The scores are formed as K Q^T, tokens down the rows of the result: a lane then holds tokens of ONE query row, in the order in which the
 // instruction wants them as the right operand of V^T P^T.  No score crosses lanes but for the row's maximum and sum, and none goes through shared memory.
 //
-// Measured: a prompt of 8192 tokens, 32 query on 16 key heads of 128, 525 to 545 us or 1.0 PFLOP/s where a large bf16 product reaches 1.3: matrix instructions 44 % of the time, vector
-// instructions (softmax, and values on their way to shared memory) 47 %, and two wavefronts of a SIMD overlap the two only in part.  Decode steps are bound by memory: 48 clients with up to
+// Measured: a prompt of 8192 tokens, 32 query on 16 key heads of 128, 533 to 540 us or 1.0 PFLOP/s where a large bf16 product reaches 1.3: matrix unit busy 45 % of the cycles, vector
+// instructions (softmax, and values on their way to shared memory) 48 %, and two wavefronts of a SIMD overlap the two only in part.  Decode steps are bound by memory: 48 clients with up to
 // 4096 tokens in the window, 538 MB, 98 us or 5.5 TB/s.  With 48 query heads on one key head (16 clients, contexts to 131072, 196 MB and 18.7 GFLOP) 53 us, 3.7 TB/s: one wavefront a SIMD.
 #pragma once
 #include <type_traits>
@@ -131,11 +131,11 @@ __device__ __forceinline__ void kv_settle() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// Scores s, not yet scaled, to cap tanh(s / cap).  With y = s / cap, cap (1 - 2 / (e^2y + 1)) is good to 2^-22 of the cap or so, which far below the cap may be more than the score itself: there it is the
-// series s (1 - y^2 / 3 + 2 y^4 / 15 - 17 y^6 / 315), whose next term is 2^-21 of s at y = 1/4.  Either way a score is off by 2^-20 of itself at most, whatever the cap.  Where no score of a
+// Scores s, not yet scaled, to cap tanh(s / cap).  With y = s / cap, cap (1 - 2 / (e^2y + 1)) is good to 2^-21 of the cap or so, which far below the cap may be more than the score itself: there it is the
+// series s (1 - y^2 / 3 + 2 y^4 / 15 - 17 y^6 / 315), whose next term is 2^-21 of s at y = 1/4.  Either way a score is off by 2^-19 of itself at most, whatever the cap.  Where no score of a
 // wavefront's chunk has come up to a quarter of the cap, which models choose well above their scores, the series is all there is, and no instruction of it is a transcendental one.
 // The series is formed in z = (r y)^2, r the 6th root of 17 / 315, as s + s z (z (2 / (15 r^4) - z) - 1 / (3 r^2)): two instructions with a literal each, and no constant in a register.
-// Measured: a prompt of 8192 tokens, 16 heads of 64, capped, 280 us (259 with the first formula alone, 171 without a cap); 32 on 16 heads of 128, 4 prompts of 8192 tokens in all, 253 (246); decode steps, bound
+// Measured: a prompt of 8192 tokens, 16 heads of 64, capped, 285 us (260 with the first formula alone, 171 without a cap); 32 on 16 heads of 128, 4 prompts of 8192 tokens in all, 253 (244); decode steps, bound
 // by memory, as before.
 constexpr float kKvSeries = 0.25f, kKvRoot = 0.6147375f;
 template <class V, int N>
@@ -745,7 +745,7 @@ __device__ __forceinline__ void kv_tile(const KvAttentionParams& p, const KvItem
     }
 }
 
-// Tiles, and items of up to 16 rows behind them, in one launch: both have two wavefronts a SIMD (head of 64: three; 16 heads of 8192 tokens 163 us, 196 with two), and a batch of prompts and decode steps is done when the longer of the two is.
+// Tiles, and items of up to 16 rows behind them, in one launch: both have two wavefronts a SIMD (head of 64: three; 16 heads of 8192 tokens 171 us, 196 with two), and a batch of prompts and decode steps is done when the longer of the two is.
 template <int D, bool CAP>
 SYMB_KERNEL __launch_bounds__(256, D == 64 ? 3 : 2) void symb_kv_attention_kernel(KvAttentionParams p) {
     __shared__ union __attribute__((aligned(16))) {
