@@ -1,6 +1,6 @@
 """ctypes binding of libsymb.so: argument marshalling only.
 
-Every function here has the name of the C entry point it calls (include/symb.h, include/symb_block.h) and
+Every function here has the name of the C entry point it calls (include/symb.h, include/symb_block.h, include/symb_loss.h) and
 does nothing but turn torch tensors into device pointers and host lists into C arrays.
 All arithmetic runs in the HIP kernels; there is no CPU or PyTorch fallback: if the
 library is missing, `lib()` raises.
@@ -29,6 +29,8 @@ SYMB_WEIGHT_LINEAR, SYMB_WEIGHT_CONV1D = 0, 1
 SYMB_NORM_LAYER, SYMB_NORM_RMS = 0, 1
 SYMB_NORM_MAX_WIDTH = 16384
 SYMB_ROTATE_HALVES, SYMB_ROTATE_ADJACENT = 0, 1
+SYMB_LOSS_MEAN, SYMB_LOSS_SUM = 0, 1
+SYMB_LOSS_MAX_WIDTH, SYMB_LOSS_MAX_VOCAB, SYMB_LOSS_MAX_ENTRIES = 32768, 1 << 22, 1024
 
 EXPORTS = ("symb_create", "symb_destroy", "symb_validate_batch", "symb_debug_row_segment_map",
            "symb_plan_row_tiles", "symb_workspace_bytes", "symb_base_linear_fwd",
@@ -40,7 +42,8 @@ EXPORTS = ("symb_create", "symb_destroy", "symb_validate_batch", "symb_debug_row
            "symb_batcher_next_due", "symb_batcher_take",
            "symb_debug_gemm_timing_enable", "symb_debug_gemm_timing_read", "symb_debug_descriptor_stats",
            "symb_debug_set_option", "symb_debug_xcd_rule", "symb_base_linear_fwd_static",
-           "symb_norm_workspace_bytes", "symb_norm_fwd", "symb_norm_bwd", "symb_kv_append", "symb_kv_workspace_bytes", "symb_kv_attention")
+           "symb_norm_workspace_bytes", "symb_norm_fwd", "symb_norm_bwd", "symb_kv_append", "symb_kv_workspace_bytes", "symb_kv_attention",
+           "symb_loss_workspace_bytes", "symb_cross_entropy", "symb_distillation")
 
 
 class symb_adapter(C.Structure):
@@ -79,6 +82,15 @@ class symb_kv_batch(C.Structure):
 
 class symb_rotation(C.Structure):
     _fields_ = [("table", C.c_void_p), ("positions", C.c_int32), ("dim", C.c_int32), ("pairs", C.c_int32)]
+
+
+class symb_loss(C.Structure):
+    _fields_ = [("scale", C.c_float), ("temperature", C.c_float)]
+
+
+class symb_loss_batch(C.Structure):
+    _fields_ = [("width", C.c_int32), ("vocab", C.c_int32), ("num_segments", C.c_int32), ("seg_offsets", C.POINTER(C.c_int32)),
+                ("losses", C.POINTER(symb_loss)), ("reduction", C.c_int32), ("cap", C.c_float)]
 
 
 class SymbError(RuntimeError):
@@ -131,6 +143,10 @@ def lib() -> C.CDLL:
         l.symb_kv_append.argtypes = [vp, kp, cp, rp, vp, i64, i32, vp, i64, vp, i64, vp, i64, vp]
         l.symb_kv_workspace_bytes.argtypes = [kp, cp, i32, i32, C.POINTER(sz)]
         l.symb_kv_attention.argtypes = [vp, kp, cp, vp, i64, i32, vp, i64, C.c_float, i32, C.c_float, vp, sz, vp]
+        lp = C.POINTER(symb_loss_batch)
+        l.symb_loss_workspace_bytes.argtypes = [lp, i32, i32, C.POINTER(sz)]
+        l.symb_cross_entropy.argtypes = [vp, lp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        l.symb_distillation.argtypes = [vp, lp, vp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
         l.symb_status_string.argtypes = [C.c_int]
         l.symb_status_string.restype = C.c_char_p
         l.symb_last_error.argtypes = [vp]
@@ -299,6 +315,30 @@ class Rotation:
     def __init__(self, table, pairs: int = SYMB_ROTATE_HALVES):
         self.table = _dense(table, "table", "float32", 2)
         self.c = symb_rotation(table.data_ptr(), table.shape[0], table.shape[1], int(pairs))
+        self._ref = C.byref(self.c)
+
+    def ref(self):
+        return self._ref
+
+
+@dataclass
+class Loss:
+    """One segment's loss: the gradient's scale, and the temperature of symb_distillation."""
+    scale: float = 1.0
+    temperature: float = 1.0
+
+
+class LossBatch:
+    """Owns the C arrays of one symb_loss_batch."""
+
+    def __init__(self, width: int, vocab: int, seg_offsets: Sequence[int], losses: Sequence[Loss], reduction: int = SYMB_LOSS_MEAN, cap: float = 0.0):
+        self.S = len(losses)
+        if len(seg_offsets) != self.S + 1:
+            raise ValueError("seg_offsets must have num_segments + 1 entries")
+        self.width, self.vocab, self.T = int(width), int(vocab), int(seg_offsets[-1])
+        self._off = _int32s(seg_offsets)
+        self._losses = (symb_loss * max(self.S, 1))(*[(float(x.scale), float(x.temperature)) for x in losses])
+        self.c = symb_loss_batch(self.width, self.vocab, self.S, self._off, self._losses, int(reduction), float(cap))
         self._ref = C.byref(self.c)
 
     def ref(self):
@@ -523,3 +563,37 @@ def symb_kv_attention(handle, batch: KvBatch, cache: KvCache, q, out, scale: flo
     wp, wb = _ws_args(ws)
     _check((_lib or lib()).symb_kv_attention(handle, batch._ref, cache._ref, q.data_ptr(), _head_rows(q, "q", shape), heads, out.data_ptr(), _head_rows(out, "out", shape),
                                              scale, window, cap, wp, wb, stream or None), handle)
+
+
+# ---- include/symb_loss.h -----------------------------------------------------------------------
+def symb_loss_workspace_bytes(batch: LossBatch, entries: int = 0, gradient: bool = True) -> int:
+    out = C.c_size_t(0)
+    _check(lib().symb_loss_workspace_bytes(batch.ref(), int(entries), 1 if gradient else 0, C.byref(out)))
+    return int(out.value)
+
+
+def _expect(t, what: str, dtype: str, shape) -> Optional[int]:
+    """Address of a dense tensor of that type and shape; None for None."""
+    if t is None:
+        return None
+    if t.dtype is not _dtype(dtype) or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what}: dense {list(shape)} of {dtype} expected, got {tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
+    return t.data_ptr()
+
+
+def symb_cross_entropy(handle, batch: LossBatch, X, W, labels, loss=None, row_loss=None, dX=None, ws=None, stream: int = 0) -> None:
+    """X, dX [T][width], W [vocab][width] bf16; labels [T] int32; loss [segments], row_loss [T] fp32."""
+    rows, wp, wb = (batch.T, batch.width), *_ws_args(ws)
+    _check((_lib or lib()).symb_cross_entropy(handle, batch._ref, _expect(X, "X", "bfloat16", rows), _expect(W, "W", "bfloat16", (batch.vocab, batch.width)),
+                                              _expect(labels, "labels", "int32", (batch.T,)), _expect(loss, "loss", "float32", (batch.S,)),
+                                              _expect(row_loss, "row_loss", "float32", (batch.T,)), _expect(dX, "dX", "bfloat16", rows), wp, wb, stream or None), handle)
+
+
+def symb_distillation(handle, batch: LossBatch, X, W, ids, logits, loss=None, row_loss=None, dX=None, ws=None, stream: int = 0) -> None:
+    """ids [T][entries] int32 and logits [T][entries] fp32 of the teacher; the rest as symb_cross_entropy."""
+    if ids.dim() != 2:
+        raise ValueError(f"ids: [{batch.T}][entries] expected, got {tuple(ids.shape)}")
+    rows, taught, (wp, wb) = (batch.T, batch.width), (batch.T, ids.shape[1]), _ws_args(ws)
+    _check((_lib or lib()).symb_distillation(handle, batch._ref, _expect(X, "X", "bfloat16", rows), _expect(W, "W", "bfloat16", (batch.vocab, batch.width)),
+                                             _expect(ids, "ids", "int32", taught), _expect(logits, "logits", "float32", taught), taught[1], _expect(loss, "loss", "float32", (batch.S,)),
+                                             _expect(row_loss, "row_loss", "float32", (batch.T,)), _expect(dX, "dX", "bfloat16", rows), wp, wb, stream or None), handle)

@@ -8,11 +8,12 @@ from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB = os.path.join(HERE, "libsymb.so")
-SOURCES = [os.path.join(HERE, "csrc", "symb_api.hip"), os.path.join(HERE, "csrc", "symb_batcher.hip"), os.path.join(HERE, "csrc", "symb_block.hip")]
+SOURCES = [os.path.join(HERE, "csrc", "symb_api.hip"), os.path.join(HERE, "csrc", "symb_batcher.hip"), os.path.join(HERE, "csrc", "symb_block.hip"),
+           os.path.join(HERE, "csrc", "symb_loss.hip")]
 DEPS = SOURCES + [os.path.join(HERE, "csrc", f) for f in
                   ("gemm16_kernel.hpp", "gemm16_asm.hpp", "adapter_kernels.hpp", "small_kernels.hpp", "narrow_kernel.hpp", "shortk_kernel.hpp", "symb_device.hpp", "symb_ring.hpp",
-                   "symb_context.hpp", "block_device.hpp", "norm_kernels.hpp", "kv_append_kernel.hpp", "kv_attention_kernels.hpp")] + \
-    [os.path.join(os.path.dirname(HERE), "include", f) for f in ("symb.h", "symb_batcher.h", "symb_block.h")]
+                   "symb_context.hpp", "block_device.hpp", "norm_kernels.hpp", "kv_append_kernel.hpp", "kv_attention_kernels.hpp", "loss_kernels.hpp")] + \
+    [os.path.join(os.path.dirname(HERE), "include", f) for f in ("symb.h", "symb_batcher.h", "symb_block.h", "symb_loss.h")]
 
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-shared", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall"]

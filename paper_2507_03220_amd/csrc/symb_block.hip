@@ -7,7 +7,6 @@
 #include <cfloat>
 #include <cmath>
 #include <initializer_list>
-#include <new>
 #include <utility>
 #include <vector>
 
@@ -19,32 +18,6 @@
 using namespace symb;
 
 namespace {
-
-// Nothing throws across the C boundary: the work lists are the only allocations.
-template <class F>
-symb_status guarded(symb_handle h, F&& f) {
-    try {
-        return f();
-    } catch (const std::bad_alloc&) {
-        return fail(h, SYMB_ERR_UNSUPPORTED, "out of host memory for the batch's work lists");
-    }
-}
-
-symb_status check_segments(symb_handle h, int32_t S, const int32_t* off) {
-    if (S < 0) return fail(h, SYMB_ERR_INVALID_ARG, "num_segments is negative");
-    if (!off) return fail(h, SYMB_ERR_INVALID_ARG, "seg_offsets is null");
-    if (off[0] != 0) return fail(h, SYMB_ERR_BAD_SEGMENTS, "seg_offsets[0] must be 0");
-    for (int i = 0; i < S; ++i)
-        if (off[i + 1] < off[i]) return fail(h, SYMB_ERR_BAD_SEGMENTS, "seg_offsets decrease at segment %d", i);
-    return SYMB_OK;
-}
-
-// The size of a Blob of these lists: what the workspace queries refuse as the calls do.
-size_t blob_bytes(std::initializer_list<std::pair<size_t, size_t>> lists) {              // (entries, bytes of one)
-    size_t n = 0;
-    for (const auto& l : lists) n = align_up(n, 16) + std::max<size_t>(l.first, 1) * l.second;
-    return n;
-}
 
 // ---- norms -----------------------------------------------------------------------------------
 symb_status check_norm(symb_handle h, const symb_norm_batch* b) {

@@ -1,0 +1,255 @@
+// Host side of include/symb_loss.h: argument checks, the plan of a call and its launches.
+#include "../../include/symb_loss.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <vector>
+
+#include "loss_kernels.hpp"
+#include "symb_context.hpp"
+
+using namespace symb;
+
+namespace {
+
+symb_status check_loss(symb_handle h, const symb_loss_batch* b, int32_t entries) {
+    if (!b) return fail(h, SYMB_ERR_INVALID_ARG, "batch is null");
+    if (b->width <= 0 || b->width % 8) return fail(h, SYMB_ERR_INVALID_ARG, "width must be a positive multiple of 8");
+    if (b->width > SYMB_LOSS_MAX_WIDTH) return fail(h, SYMB_ERR_UNSUPPORTED, "width %d exceeds SYMB_LOSS_MAX_WIDTH", b->width);
+    if (b->vocab <= 0) return fail(h, SYMB_ERR_INVALID_ARG, "vocab must be positive");
+    if (b->vocab > SYMB_LOSS_MAX_VOCAB) return fail(h, SYMB_ERR_UNSUPPORTED, "vocab %d exceeds SYMB_LOSS_MAX_VOCAB", b->vocab);
+    if (b->reduction != SYMB_LOSS_MEAN && b->reduction != SYMB_LOSS_SUM) return fail(h, SYMB_ERR_INVALID_ARG, "unknown reduction %d", b->reduction);
+    if (!(b->cap >= 0.f) || !std::isfinite(b->cap)) return fail(h, SYMB_ERR_INVALID_ARG, "cap must be finite and not negative");
+    const symb_status st = check_segments(h, b->num_segments, b->seg_offsets);
+    if (st != SYMB_OK) return st;
+    if (b->num_segments && !b->losses) return fail(h, SYMB_ERR_INVALID_ARG, "losses is null");
+    for (int i = 0; i < b->num_segments; ++i) {
+        if (!std::isfinite(b->losses[i].scale)) return fail(h, SYMB_ERR_INVALID_ARG, "segment %d: scale must be finite", i);
+        if (entries && (!(b->losses[i].temperature > 0.f) || !std::isfinite(b->losses[i].temperature)))
+            return fail(h, SYMB_ERR_INVALID_ARG, "segment %d: temperature must be positive and finite", i);
+    }
+    if (entries < 0) return fail(h, SYMB_ERR_INVALID_ARG, "entries is negative");
+    if (entries > SYMB_LOSS_MAX_ENTRIES) return fail(h, SYMB_ERR_UNSUPPORTED, "%d entries: SYMB_LOSS_MAX_ENTRIES at most", entries);
+    const int64_t T = b->seg_offsets[b->num_segments];
+    if (T * b->width >= ((int64_t)1 << 31)) return fail(h, SYMB_ERR_UNSUPPORTED, "%lld rows of %d: fewer than 2^31 elements at once", (long long)T, b->width);
+    const size_t need = blob_bytes({{(size_t)b->num_segments + 1, sizeof(int32_t)}, {(size_t)b->num_segments, sizeof(LossDesc)}});
+    if (need > kSlotBytes) return fail(h, SYMB_ERR_UNSUPPORTED, "batch descriptors need %zu bytes, capacity is %zu", need, kSlotBytes);
+    return SYMB_OK;
+}
+
+// A call's chunks of rows, tiles, and the places of its workspace.
+struct LossPlan {
+    int chunk = 0, score_blk = 8, grad_blk = 8, pitch = 0, column_parts = 0;
+    int64_t part_tiles = 0;
+    size_t rows = 0, flags = 0, count = 0, gain = 0, scores = 0, slopes = 0, shares = 0, row_ab = 0, row_base = 0, row_loss = 0, stats = 0, row_gain = 0, held = 0, parts = 0, bytes = 0;
+};
+// What a call may hold: weights of a chunk of rows, and, where the losses alone are wanted, their sums.
+constexpr int64_t kHeldBytes = (int64_t)2 << 30, kStatBytes = (int64_t)256 << 20;
+
+int64_t tiles_of(int64_t rows, int64_t columns, int edge) { return ((rows + edge - 1) / edge) * ((columns + edge - 1) / edge); }
+
+// Microseconds of the product with W of so many rows, in tiles of 32 blk.
+double score_us(int rows, const symb_loss_batch* b, int blk) {
+    const int64_t tiles = tiles_of(rows, b->vocab, 32 * blk), slots = blk == 8 ? 256 : 512;
+    return (double)((tiles + slots - 1) / slots) * ((b->width + 63) / 64 * (blk == 8 ? 1.2 : 0.7) + (blk == 8 ? 10 : 6));
+}
+template <int BLK>
+double grad_us(int rows, const symb_loss_batch* b, int& n) {
+    using G = LossGrad<BLK>;
+    n = loss_grad_parts<BLK>(rows, b->width, b->vocab, INT64_MAX);
+    return 1e-3 * (double)loss_grad_ns(tiles_of(rows, b->width, 32 * BLK), b->vocab / 64, n, G::kSlots, G::kStageNs, G::kPartNs);
+}
+
+LossPlan plan_loss(const symb_loss_batch* b, int32_t entries, bool gradient) {
+    LossPlan plan;
+    const int64_t T = b->seg_offsets[b->num_segments], K = std::max(entries, 1);
+    const int rows = (int)((T + 255) / 256 * 256);
+    plan.pitch = (b->vocab + 63) / 64 * 64;
+    const int64_t row_bytes = gradient ? (int64_t)plan.pitch * 2 : ((int64_t)(b->vocab + 255) / 256) * 4 * (int64_t)sizeof(float2);
+    const int most = (int)std::min<int64_t>(rows, std::max<int64_t>((gradient ? kHeldBytes : kStatBytes) / row_bytes / 256 * 256, 256));
+    // of the chunks that fit, the one whose whole chunks take least in all
+    int n8 = 1, n4 = 1;
+    double least = 1e300;
+    plan.chunk = most;
+    for (int c = 256; c <= most; c += 256) {
+        const int whole = rows / c, rest = rows % c;
+        auto us = [&](int r) { return r ? std::min(score_us(r, b, 8), score_us(r, b, 4)) + (gradient ? std::min(grad_us<8>(r, b, n8), grad_us<4>(r, b, n4)) : 0.0) + 15.0 : 0.0; };
+        const double all = whole * us(c) + us(rest);
+        if (all < least) least = all, plan.chunk = c;
+    }
+    const int first = (int)std::min<int64_t>(T, plan.chunk);
+    plan.score_blk = score_us(first, b, 8) < score_us(first, b, 4) ? 8 : 4;
+    if (gradient) {
+        plan.grad_blk = grad_us<8>(first, b, n8) < grad_us<4>(first, b, n4) ? 8 : 4;
+        const int edge = 32 * plan.grad_blk;
+        plan.part_tiles = std::max<int64_t>(tiles_of(first, b->width, edge) * (plan.grad_blk == 8 ? n8 : n4), std::min<int64_t>(512, tiles_of(1, b->width, edge) * std::max(b->vocab / 256, 1)));
+    }
+    plan.column_parts = (b->vocab + 32 * plan.score_blk - 1) / (32 * plan.score_blk) * 2;
+    size_t at = 0;
+    auto take = [&](size_t n) {
+        const size_t o = at;
+        at += align_up(n, 256);
+        return o;
+    };
+    plan.rows = take(T * sizeof(int32_t));
+    plan.flags = take(entries ? T * sizeof(int32_t) : 0);
+    plan.count = take(sizeof(int32_t));
+    plan.gain = take(b->num_segments * sizeof(float));
+    plan.scores = take(T * K * sizeof(float));
+    plan.slopes = take(T * K * sizeof(float));
+    plan.shares = take(entries ? T * K * sizeof(float) : 0);
+    plan.row_ab = take(T * sizeof(float2));
+    plan.row_base = take(entries ? T * sizeof(float) : 0);
+    plan.row_loss = take(T * sizeof(float));
+    plan.stats = take((size_t)plan.column_parts * plan.chunk * sizeof(float2));
+    plan.row_gain = take(gradient ? plan.chunk * sizeof(float) : 0);
+    plan.held = take(gradient ? (size_t)plan.chunk * plan.pitch * 2 : 0);
+    plan.parts = take((size_t)plan.part_tiles * (32 * plan.grad_blk) * (32 * plan.grad_blk) * sizeof(float));
+    plan.bytes = T ? at : 0;
+    return plan;
+}
+
+// A kernel of the tiles of gemm16_asm.hpp: its LDS once per context (the attribute belongs to the device the kernel is loaded on).
+template <int BLK, class F>
+symb_status launch_tiles(symb_handle h, F kernel, int64_t tiles, const LossParams& p, hipStream_t s) {
+    const void* k = reinterpret_cast<const void*>(kernel);
+    constexpr int smem = Gemm16Tile<BLK, BLK>::SMEM;
+    if (std::find(h->lds_attr_set.begin(), h->lds_attr_set.end(), k) == h->lds_attr_set.end()) {
+        SYMB_HIP(h, hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, smem));
+        h->lds_attr_set.push_back(k);
+    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(256), smem, s, p);
+    SYMB_HIP(h, hipGetLastError());
+    return SYMB_OK;
+}
+template <int BLK>
+symb_status launch_scores(symb_handle h, const LossParams& p, int rows, hipStream_t s) {
+    const int64_t tiles = tiles_of(rows, p.V, 32 * BLK);
+    if (p.dX) return p.cap > 0.f ? launch_tiles<BLK>(h, symb_loss_scores_kernel<BLK, true, true>, tiles, p, s) : launch_tiles<BLK>(h, symb_loss_scores_kernel<BLK, true, false>, tiles, p, s);
+    return p.cap > 0.f ? launch_tiles<BLK>(h, symb_loss_scores_kernel<BLK, false, true>, tiles, p, s) : launch_tiles<BLK>(h, symb_loss_scores_kernel<BLK, false, false>, tiles, p, s);
+}
+template <int BLK>
+symb_status launch_grad(symb_handle h, const LossParams& p, int rows, hipStream_t s) {
+    const symb_status st = launch_tiles<BLK>(h, symb_loss_grad_kernel<BLK>, p.part_tiles, p, s);
+    if (st != SYMB_OK) return st;
+    hipLaunchKernelGGL(symb_loss_reduce_kernel<BLK>, dim3((unsigned)(tiles_of(rows, p.width, 32 * BLK) * 4 * BLK)), dim3(256), 0, s, p);
+    SYMB_HIP(h, hipGetLastError());
+    return SYMB_OK;
+}
+
+symb_status run_loss(symb_handle h, const symb_loss_batch* b, const void* X, const void* W, const int32_t* labels, const int32_t* ids, const float* logits, int32_t entries, float* loss,
+                     float* row_loss, void* dX, void* ws, size_t ws_bytes, void* stream) {
+    symb_status st = check_handle(h);
+    if (st != SYMB_OK) return st;
+    CallGuard guard(h);
+    if ((st = check_loss(h, b, entries)) != SYMB_OK) return st;
+    const int S = b->num_segments, T = b->seg_offsets[S];
+    if (!S) return SYMB_OK;
+    for (const void* ptr : {(const void*)loss, (const void*)row_loss, (const void*)labels, (const void*)ids, (const void*)logits})
+        if ((uintptr_t)ptr & 3) return fail(h, SYMB_ERR_INVALID_ARG, "device pointers must be 4-byte aligned");
+    if (T && (!X || !W || (entries ? !ids || !logits : !labels))) return fail(h, SYMB_ERR_INVALID_ARG, entries ? "X, W, ids and logits are required" : "X, W and labels are required");
+    if (!loss && !row_loss && !dX) return fail(h, SYMB_ERR_INVALID_ARG, "neither losses nor a gradient are asked for");
+    if (misaligned16(X) || misaligned16(W) || misaligned16(dX) || misaligned16(ws)) return fail(h, SYMB_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+    const LossPlan plan = plan_loss(b, entries, dX != nullptr);
+    if (plan.bytes && (!ws || ws_bytes < plan.bytes)) return fail(h, SYMB_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : 0, plan.bytes);
+    if (!T && !loss) return SYMB_OK;
+    hipStream_t s = (hipStream_t)stream;
+    std::vector<LossDesc> ld(S);
+    for (int i = 0; i < S; ++i) ld[i] = LossDesc{b->losses[i].scale, b->losses[i].temperature};
+    Blob blob;
+    const size_t o_off = blob.add(b->seg_offsets, (size_t)S + 1), o_ld = blob.add(ld.data(), ld.size());
+    unsigned char* dev = nullptr;
+    if ((st = upload(h, blob, s, &dev)) != SYMB_OK) return st;
+    unsigned char* const w = (unsigned char*)ws;
+    LossParams p{};
+    p.X = (const bf16*)X;
+    p.W = (const bf16*)W;
+    p.dX = (bf16*)dX;
+    p.own_flags = (int32_t*)(w + plan.flags);
+    p.flags = entries ? p.own_flags : labels;
+    p.ids = ids;
+    p.teacher = logits;
+    p.loss = loss;
+    p.row_loss = row_loss ? row_loss : (float*)(w + plan.row_loss);
+    p.off = (const int32_t*)(dev + o_off);
+    p.losses = (const LossDesc*)(dev + o_ld);
+    p.rows = (int32_t*)(w + plan.rows);
+    p.count = (int32_t*)(w + plan.count);
+    p.gain = (float*)(w + plan.gain);
+    p.scores = (float*)(w + plan.scores);
+    p.slopes = (float*)(w + plan.slopes);
+    p.shares = (float*)(w + plan.shares);
+    p.row_ab = (float2*)(w + plan.row_ab);
+    p.row_base = (float*)(w + plan.row_base);
+    p.stats = (float2*)(w + plan.stats);
+    p.row_gain = (float*)(w + plan.row_gain);
+    p.held = (bf16*)(w + plan.held);
+    p.parts = (float*)(w + plan.parts);
+    p.part_tiles = plan.part_tiles;
+    p.T = T;
+    p.S = S;
+    p.V = b->vocab;
+    p.pitch = plan.pitch;
+    p.width = b->width;
+    p.K = std::max(entries, 1);
+    p.chunk = plan.chunk;
+    p.group_m = 8;
+    p.mean = b->reduction == SYMB_LOSS_MEAN;
+    p.cap = b->cap;
+    p.to_cap = b->cap > 0.f ? 1.f / b->cap : 0.f;
+    if (T) {
+        if (entries) {
+            hipLaunchKernelGGL(symb_loss_teacher_kernel, dim3((T + 3) / 4), dim3(256), 0, s, p);
+            SYMB_HIP(h, hipGetLastError());
+        }
+        hipLaunchKernelGGL(symb_loss_rows_kernel, dim3((T + 255) / 256 + S), dim3(256), 0, s, p);
+        SYMB_HIP(h, hipGetLastError());
+        hipLaunchKernelGGL(symb_loss_entries_kernel, dim3(T), dim3(256), 0, s, p);
+        SYMB_HIP(h, hipGetLastError());
+    }
+    for (int64_t at = 0; at < T; at += plan.chunk) {
+        p.chunk0 = (int32_t)at;
+        const int rows = (int)std::min<int64_t>(T - at, plan.chunk);
+        if ((st = plan.score_blk == 8 ? launch_scores<8>(h, p, rows, s) : launch_scores<4>(h, p, rows, s)) != SYMB_OK) return st;
+        hipLaunchKernelGGL(symb_loss_join_kernel, dim3((rows + kJoinRows - 1) / kJoinRows), dim3(kJoinRows * kJoinSets), 0, s, p, plan.column_parts, 16 * plan.score_blk);
+        SYMB_HIP(h, hipGetLastError());
+        if (dX && (st = plan.grad_blk == 8 ? launch_grad<8>(h, p, rows, s) : launch_grad<4>(h, p, rows, s)) != SYMB_OK) return st;
+    }
+    if (loss) {
+        hipLaunchKernelGGL(symb_loss_segments_kernel, dim3(S), dim3(256), 0, s, p);
+        SYMB_HIP(h, hipGetLastError());
+    }
+    guard.completed = true;
+    return seal_slot(h);
+}
+
+}  // namespace
+
+extern "C" {
+
+symb_status symb_loss_workspace_bytes(const symb_loss_batch* b, int32_t entries, int32_t gradient, size_t* out) {
+    return guarded(nullptr, [&]() -> symb_status {
+        if (!out) return fail(nullptr, SYMB_ERR_INVALID_ARG, "out is null");
+        const symb_status st = check_loss(nullptr, b, entries);
+        if (st != SYMB_OK) return st;
+        *out = plan_loss(b, entries, gradient != 0).bytes;
+        return SYMB_OK;
+    });
+}
+
+symb_status symb_cross_entropy(symb_handle h, const symb_loss_batch* b, const void* X, const void* W, const int32_t* labels, float* loss, float* row_loss, void* dX, void* ws, size_t ws_bytes,
+                               void* stream) {
+    return guarded(h, [&]() -> symb_status { return run_loss(h, b, X, W, labels, nullptr, nullptr, 0, loss, row_loss, dX, ws, ws_bytes, stream); });
+}
+
+symb_status symb_distillation(symb_handle h, const symb_loss_batch* b, const void* X, const void* W, const int32_t* ids, const float* logits, int32_t entries, float* loss, float* row_loss,
+                              void* dX, void* ws, size_t ws_bytes, void* stream) {
+    return guarded(h, [&]() -> symb_status {
+        if (entries < 1) return fail(h, SYMB_ERR_INVALID_ARG, "entries must be positive");
+        return run_loss(h, b, X, W, nullptr, ids, logits, entries, loss, row_loss, dX, ws, ws_bytes, stream);
+    });
+}
+
+}  // extern "C"
