@@ -20,6 +20,10 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 struct LossDesc {
     float scale, temperature;
 };
+struct LossRow {                          // of a row that takes part: its weights are 2^(a z - b), and its segment
+    float a, b;
+    int32_t seg, entries;                 // entries: of the teacher, in the order of their ids
+};
 struct LossParams {
     const bf16* X;
     const bf16* W;
@@ -35,19 +39,22 @@ struct LossParams {
     int32_t* rows;                        // [T] the rows that take part, in order
     int32_t* count;                       // how many they are
     float* gain;                          // [S] scale, over the segment's rows that take part if the loss is a mean
-    float* scores;                        // [T][K] a z_j - b of a row's entries
-    float* slopes;                        // [T][K] z'
-    float* shares;                        // [T][K] q
-    float2* row_ab;                       // [T] a and b
-    float* row_base;                      // [T] sum_j q_j (log q_j - (a z_j - b) ln 2)
+    LossRow* info;                        // [T]
+    float* slopes;                        // [T] z' of the label
+    int32_t* sorted;                      // [T][K] a row's ids in their order, absent ones left out,
+    float* shares;                        // [T][K] their q,
+    float* scores;                        // [T][K] and their s, from the first product
+    uint16_t* starts;                     // [T][column tiles + 1] how many of them lie before each of its tiles
     float2* stats;                        // [column parts][chunk] shift and sum of a row's weights
     float* row_gain;                      // [chunk] what a row's product is multiplied with
     bf16* held;                           // [chunk][pitch] weights
     float* parts;                         // partial tiles of the second product
+    int32_t* part_count;                  // in how many parts each tile comes
     int64_t part_tiles;                   // room for that many
     int32_t T, S, V, pitch, width, K;
     int32_t chunk0, chunk;                // the chunk's first row (of those that take part) and its length at most
-    int32_t group_m, mean;
+    int32_t tile_cols;                    // columns of a tile of the first product
+    int32_t group_m, mean, grad_blk;
     float cap, to_cap;                    // 1 / cap
 };
 
@@ -63,34 +70,44 @@ __device__ __forceinline__ float loss_capped(float s, float cap, float to_cap, f
     return is_near ? near : far;
 }
 
-// ---- which rows take part -----------------------------------------------------------------------------------------------------------
-// A row with a teacher: flag 0, and the softmax of its entries (absent ones: share 0).  One wavefront a row.
-SYMB_KERNEL __launch_bounds__(256) void symb_loss_teacher_kernel(LossParams p) {
-    const int lane = threadIdx.x & 63, t = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    if (t >= p.T) return;
-    const int32_t* ids = p.ids + (int64_t)t * p.K;
-    const float* l = p.teacher + (int64_t)t * p.K;
-    float* q = p.shares + (int64_t)t * p.K;
-    const float to_t = 1.f / p.losses[seg_of_row(p.off, 0, p.S - 1, t)].temperature;
-    bool any = false;
-    float most = -__builtin_inff();
-    for (int j = lane; j < p.K; j += 64)
-        if (ids[j] >= 0) {
-            any = true;
-            most = fmaxf(most, l[j]);
+// tanh(y) for |y| <= kLossNear: y times a polynomial in y^2, 2^-22 of it at most (the coefficients: least largest relative error, from exchanged extrema).
+constexpr float kLossNear = 1.22f;
+__device__ __forceinline__ float loss_tanh(float y) {
+    const float u = y * y;
+    float r = -1.9576128e-4f;
+    r = fmaf(r, u, 1.6539543e-3f);
+    r = fmaf(r, u, -6.9249099e-3f);
+    r = fmaf(r, u, 2.0681336e-2f);
+    r = fmaf(r, u, -5.3551411e-2f);
+    r = fmaf(r, u, 1.3325926e-1f);
+    r = fmaf(r, u, -3.3332821e-1f);
+    r = fmaf(r, u, 0.99999994f);
+    return y * r;
+}
+
+// ---- which rows take part, and their own scores -------------------------------------------------------------------------------------
+// s = x . W_id over a wavefront; NaN for a number outside the vocabulary, which is never followed.
+__device__ __forceinline__ float loss_score(const LossParams& p, int t, int id) {
+    if (id >= p.V) return __builtin_nanf("");
+    const bf16 *x = p.X + (int64_t)t * p.width, *w = p.W + (int64_t)id * p.width;
+    float s[2] = {0.f, 0.f};
+#pragma unroll 4
+    for (int c = threadIdx.x & 63; c < p.width >> 3; c += 64) {
+        const intx4 u = *(const intx4*)(x + c * 8), v = *(const intx4*)(w + c * 8);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            s[0] = fmaf(bf16_lo((unsigned)u[i]), bf16_lo((unsigned)v[i]), s[0]);
+            s[1] = fmaf(bf16_hi((unsigned)u[i]), bf16_hi((unsigned)v[i]), s[1]);
         }
-    const bool part = __ballot(any) != 0;
-    if (lane == 0) p.own_flags[t] = part ? 0 : -1;
-    if (!part) return;
-    most = across_wave(most, Max());
-    float sum = 0.f;
-    for (int j = lane; j < p.K; j += 64) {
-        const float e = ids[j] >= 0 ? expf((l[j] - most) * to_t) : 0.f;
-        q[j] = e;
-        sum += e;
     }
-    sum = across_wave(sum, Add());
-    for (int j = lane; j < p.K; j += 64) q[j] /= sum;
+    return across_wave(s[0] + s[1], Add());
+}
+// A row that takes no part: zeros.
+__device__ __forceinline__ void loss_no_row(const LossParams& p, int t) {
+    const int lane = threadIdx.x & 63;
+    if (lane == 0) p.row_loss[t] = 0.f;
+    if (p.dX)
+        for (int c = lane; c < p.width >> 3; c += 64) *(intx4*)(p.dX + (int64_t)t * p.width + c * 8) = intx4{0, 0, 0, 0};
 }
 
 // Sum of `v` over the workgroup's 256 threads.
@@ -103,10 +120,9 @@ __device__ __forceinline__ int loss_count(int v, int* lds) {
     __syncthreads();
     return v;
 }
-// The first workgroups list the rows of 256 each (every one counts those before its own); one a segment counts its rows.
-SYMB_KERNEL __launch_bounds__(256) void symb_loss_rows_kernel(LossParams p) {
-    __shared__ int lds[4];
-    const int lists = (p.T + 255) / 256, b = blockIdx.x;
+// Workgroup `b` lists the rows of 256 that take part (and counts those before them itself); behind the lists, one a segment counts its rows.
+__device__ __forceinline__ void loss_list(const LossParams& p, int b, int* lds) {
+    const int lists = (p.T + 255) / 256;
     if (b < lists) {
         int before = 0;
         for (int t = threadIdx.x; t < b * 256; t += 256) before += p.flags[t] >= 0;
@@ -130,63 +146,94 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_rows_kernel(LossParams p) {
     if (threadIdx.x == 0) p.gain[i] = p.mean ? p.losses[i].scale / (float)max(n, 1) : p.losses[i].scale;
 }
 
-// ---- the scores of a row's own entries ----------------------------------------------------------------------------------------------
-// One workgroup a row: its entries' dot products, a wavefront each in turn; a and b; rows that take no part get their zeros.
-SYMB_KERNEL __launch_bounds__(256) void symb_loss_entries_kernel(LossParams p) {
-    __shared__ float best[4];
-    const int t = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), nvec = p.width >> 3;
-    const int flag = p.flags[t];
-    if (flag < 0) {
-        if (threadIdx.x == 0) p.row_loss[t] = 0.f;
-        if (p.dX)
-            for (int c = threadIdx.x; c < nvec; c += 256) *(intx4*)(p.dX + (int64_t)t * p.width + c * 8) = intx4{0, 0, 0, 0};
-        return;
+// Labels: the lists, and a wavefront for each row's own score.
+SYMB_KERNEL __launch_bounds__(256) void symb_loss_labels_kernel(LossParams p) {
+    __shared__ int lds[4];
+    const int lists = (p.T + 255) / 256 + p.S;
+    if ((int)blockIdx.x < lists) return loss_list(p, blockIdx.x, lds);
+    const int t = (blockIdx.x - lists) * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    if (t >= p.T) return;
+    const int label = p.flags[t];
+    if (label < 0) return loss_no_row(p, t);
+    float s = loss_score(p, t, label), slope = 1.f;
+    if (p.cap > 0.f) s = loss_capped(s, p.cap, p.to_cap, slope);
+    if ((threadIdx.x & 63) == 0) {
+        p.info[t] = LossRow{kLog2e, s * kLog2e, seg_of_row(p.off, 0, p.S - 1, t), 1};
+        p.slopes[t] = slope;
     }
-    const bf16* x = p.X + (int64_t)t * p.width;
-    const float a = p.ids ? kLog2e / p.losses[seg_of_row(p.off, 0, p.S - 1, t)].temperature : kLog2e;
+}
+SYMB_KERNEL __launch_bounds__(256) void symb_loss_rows_kernel(LossParams p) {
+    __shared__ int lds[4];
+    loss_list(p, blockIdx.x, lds);
+}
+
+// Teachers: a row's entries in the order of their ids, with their shares, the tiles of the vocabulary that they lie in, and the score of the one with the largest share.  A wavefront a row.
+SYMB_KERNEL __launch_bounds__(256) void symb_loss_teacher_kernel(LossParams p) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), t = blockIdx.x * 4 + wave;
+    if (t >= p.T) return;
+    const int K = p.K, pad = (K + 63) / 64 * 64;
+    int* const list = (int*)smem + wave * 2 * pad;        // ids as they come (absent ones behind all others), then in order
+    int* const order = list + pad;
+    const int32_t* ids = p.ids + (int64_t)t * K;
+    const float* l = p.teacher + (int64_t)t * K;
     float most = -__builtin_inff();
-    for (int j = wave; j < p.K; j += 4) {
-        const int id = p.ids ? p.ids[(int64_t)t * p.K + j] : flag;
-        if (id < 0) continue;
-        float s = 0.f;
-        if (id < p.V) {
-            const bf16* w = p.W + (int64_t)id * p.width;
-            for (int c = lane; c < nvec; c += 64) {
-                const intx4 u = *(const intx4*)(x + c * 8), v = *(const intx4*)(w + c * 8);
+    int n = 0;
+    bool outside = false;
+    for (int j = lane; j < pad; j += 64) {
+        const int id = j < K ? ids[j] : -1;
+        list[j] = id < 0 ? 0x7fffffff : min(id, 0x7ffffffe);
+        if (id >= 0) most = fmaxf(most, l[j]);
+        outside |= id >= p.V;
+        n += __popcll(__ballot(id >= 0));
+    }
+    if (lane == 0) p.own_flags[t] = n ? 0 : -1;
+    if (!n) return loss_no_row(p, t);
+    const int seg = seg_of_row(p.off, 0, p.S - 1, t);
+    const float T = p.losses[seg].temperature, to_t = 1.f / T;
+    most = across_wave(most, Max());
+    // (a NaN among the logits makes the sum, and with it all shares, NaN)
+    float sum = 0.f, best = -1.f;
+    for (int j = lane; j < K; j += 64) sum += ids[j] >= 0 ? expf((l[j] - most) * to_t) : 0.f;
+    const float to_sum = 1.f / across_wave(sum, Add());
+    int best_id = 0x7fffffff;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+    for (int j = lane; j < K; j += 64) {
+        const int id = list[j];
+        if (id == 0x7fffffff) continue;
+        int at = 0;                                       // entries before this one, in the order of ids and then as they come
+        for (int k = 0; k < pad; k += 4) {
+            const intx4 o = *(const intx4*)(list + k);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    s = fmaf(bf16_lo((unsigned)u[i]), bf16_lo((unsigned)v[i]), s);
-                    s = fmaf(bf16_hi((unsigned)u[i]), bf16_hi((unsigned)v[i]), s);
-                }
-            }
-            s = across_wave(s, Add());
-        } else s = __builtin_nanf("");               // (a number outside the vocabulary is never followed)
-        float slope = 1.f;
-        if (p.cap > 0.f) s = loss_capped(s, p.cap, p.to_cap, slope);
-        const float z = s * a;
-        if (lane == 0) {
-            p.scores[(int64_t)t * p.K + j] = z;
-            p.slopes[(int64_t)t * p.K + j] = slope;
+            for (int i = 0; i < 4; ++i) at += o[i] < id || (o[i] == id && k + i < j);
         }
-        most = z != z || most != most ? __builtin_nanf("") : fmaxf(most, z);
+        const float q = expf((l[j] - most) * to_t) * to_sum;
+        order[at] = id;
+        p.sorted[(int64_t)t * K + at] = id;
+        p.shares[(int64_t)t * K + at] = q;
+        if (q > best || (q == best && id < best_id)) best = q, best_id = id;
     }
-    if (lane == 0) best[wave] = most;
-    __syncthreads();
-    float b = best[0];
+    // the best entry's score
+    const float top = across_wave(best, Max());
+    int mine = best == top ? best_id : 0x7fffffff;
 #pragma unroll
-    for (int w = 1; w < 4; ++w) b = b != b || best[w] != best[w] ? __builtin_nanf("") : fmaxf(b, best[w]);
-    if (threadIdx.x == 0) p.row_ab[t] = make_float2(a, b);
-    if (!p.ids || wave) return;
-    float base = 0.f;
-    for (int j = lane; j < p.K; j += 64) {
-        const int64_t at = (int64_t)t * p.K + j;
-        if (p.ids[at] < 0) continue;
-        const float z = p.scores[at] - b, q = p.shares[at];
-        p.scores[at] = z;
-        if (!(q == 0.f)) base += q * (logf(q) - z * kLn2);
+    for (int m = 32; m; m >>= 1) mine = min(mine, __shfl_xor(mine, m));
+    outside = __any(outside || mine == 0x7fffffff);       // (all shares NaN: none is the largest)
+    float s = __builtin_nanf(""), slope;
+    if (!outside) {
+        s = loss_score(p, t, mine);
+        if (p.cap > 0.f) s = loss_capped(s, p.cap, p.to_cap, slope);
     }
-    base = across_wave(base, Add());
-    if (lane == 0) p.row_base[t] = base;
+    const float a = kLog2e * to_t;
+    if (lane == 0) p.info[t] = LossRow{a, s * a, seg, n};
+    // starts[c]: entries in the tiles before c
+    const int tiles = (p.V + p.tile_cols - 1) / p.tile_cols;
+    uint16_t* const starts = p.starts + (int64_t)t * (tiles + 1);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+    for (int k = lane; k <= n; k += 64) {
+        const int from = k ? min(order[k - 1], p.V - 1) / p.tile_cols + 1 : 0, to = k < n ? min(order[k], p.V - 1) / p.tile_cols : tiles;
+        for (int c = from; c <= to; ++c) starts[c] = (uint16_t)k;
+    }
 }
 
 // ---- products -------------------------------------------------------------------------------------------------------------------------
@@ -312,8 +359,35 @@ __device__ __forceinline__ void loss_place(int lin, int m_tiles, int n_tiles, in
     tn = lin % width / rows;
 }
 
-// X W^T of a chunk, a tile a workgroup: its rows' sums of weights, and the weights themselves where the gradient wants them.
-template <int BLK, bool GRAD, bool CAP>
+// Element (j, e) of a lane's scores: half of what is left at every step.  (With masks that the compiler cannot see through: it makes selected values loads from a selected address, and the scores
+// an array in scratch memory.)
+template <int BLK>
+__device__ __forceinline__ float loss_pick(const float (&w)[BLK][4], int j, int e) {
+    auto mask = [](int bit) __attribute__((always_inline)) {
+        int m = bit ? -1 : 0;
+        asm volatile("" : "+v"(m));
+        return m;
+    };
+    auto pick = [](int m, int yes, int no) __attribute__((always_inline)) { return (yes & m) | (no & ~m); };
+    const int e0 = mask(e & 1), e1 = mask(e & 2), j0 = mask(j & 1), j1 = mask(j & 2), j2 = mask(j & 4);
+    int v[BLK];
+    static_for<0, BLK>([&](auto K) __attribute__((always_inline)) {
+        constexpr int k = decltype(K)::value;
+        v[k] = pick(e1, pick(e0, as_int(w[k][3]), as_int(w[k][2])), pick(e0, as_int(w[k][1]), as_int(w[k][0])));
+    });
+    if constexpr (BLK == 8) static_for<0, 4>([&](auto K) __attribute__((always_inline)) { v[decltype(K)::value] = pick(j2, v[decltype(K)::value + 4], v[decltype(K)::value]); });
+    return as_float(pick(j1, pick(j0, v[3], v[2]), pick(j0, v[1], v[0])));
+}
+// A tile row's entries of its teacher, behind the staged tile in LDS.
+struct LossHits {
+    int64_t at;                           // of the first one in `sorted`, `scores`
+    int32_t n;
+    int32_t id[4];                        // the first of them
+    int32_t pad;
+};
+
+// X W^T of a chunk, a tile a workgroup: its rows' sums of weights, the scores of their teachers' entries, and the weights themselves where the gradient wants them.
+template <int BLK, bool GRAD, bool CAP, bool TEACHER>
 SYMB_KERNEL __launch_bounds__(256) void symb_loss_scores_kernel(const LossParams p) {
     using TT = Gemm16Tile<BLK, BLK>;
     constexpr int BM = TT::BM, BN = TT::BN, CP = TT::C_PITCH;
@@ -336,14 +410,29 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_scores_kernel(const LossParams
 #pragma unroll
     for (int i = 0; i < BLK; ++i) {
         const int t = list[min(m0 + wm0 + 16 * i + l15, rows - 1)];
-        const float2 ab = p.row_ab[t];
-        a[i] = ab.x;
-        b[i] = ab.y;
-        label[i] = p.ids ? -1 : p.flags[t] - (n0 + wn0 + 4 * lg);              // of block j, element e: 16 j + e
+        a[i] = p.info[t].a;
+        b[i] = p.info[t].b;
+        if constexpr (!TEACHER) label[i] = p.flags[t] - (n0 + wn0 + 4 * lg);   // of block j, element e: 16 j + e
+    }
+    LossHits hits{};
+    if (TEACHER && tid < BM && m0 + tid < rows) {
+        const int t = list[m0 + tid];
+        const uint16_t* const start = p.starts + (int64_t)t * (n_tiles + 1) + tn;
+        const int at = start[0];
+        hits.n = start[1] - at;
+        hits.at = (int64_t)t * p.K + at;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) hits.id[k] = p.sorted[(int64_t)t * p.K + min(at + k, p.K - 1)];
     }
     auto a_at = [&](int row) __attribute__((always_inline)) { return (unsigned)(list[min(m0 + row, rows - 1)] - first) * (unsigned)p.width; };
     loss_tile<BLK, false>(smem, p.X + (size_t)first * p.width, a_at, p.W + (size_t)n0 * p.width, p.width, p.V - n0, 0, p.width / 64, true, p.width);
 
+    LossHits* const row_hits = reinterpret_cast<LossHits*>(smem + TT::C_BYTES);
+    static_assert(TT::C_BYTES % 16 == 0 && TT::C_BYTES + BM * (int)sizeof(LossHits) <= TT::SMEM, "");
+    if constexpr (TEACHER) {
+        if (tid < BM) row_hits[tid] = hits;
+        __syncthreads();
+    }
     const unsigned c_lane = (unsigned)((wm0 + l15) * CP + (wn0 + lg * 4) * 2);
     const int left = p.V - (n0 + wn0 + 4 * lg);                                // columns of this lane: 16 j + e < left
     const bool edge = n0 + BN > p.V;
@@ -351,50 +440,104 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_scores_kernel(const LossParams
     static_for<0, BLK>([&](auto I) __attribute__((always_inline)) {
         constexpr int i = decltype(I)::value;
         float w[BLK][4], slope[CAP ? BLK : 1][4];
-        float sum = 0.f, shift = 0.f;
-        static_for<0, BLK>([&](auto J) __attribute__((always_inline)) {
-            constexpr int j = decltype(J)::value;
-            acc16_read4<4 * (BLK * i + j)>(w[j][0], w[j][1], w[j][2], w[j][3]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if constexpr (CAP) w[j][e] = loss_capped(w[j][e], p.cap, p.to_cap, slope[j][e]);
-                w[j][e] = fmaf(w[j][e], a[i], -b[i]);
-                if (edge && 16 * j + e >= left) w[j][e] = -__builtin_inff();
-            }
-        });
-        auto weights = [&]() __attribute__((always_inline)) {
-            sum = 0.f;
+        auto scores = [&]() __attribute__((always_inline)) {
+            static_for<0, BLK>([&](auto J) __attribute__((always_inline)) {
+                constexpr int j = decltype(J)::value;
+                acc16_read4<4 * (BLK * i + j)>(w[j][0], w[j][1], w[j][2], w[j][3]);
+            });
+        };
+        // a z - b, the general way
+        auto exponents = [&]() __attribute__((always_inline)) {
 #pragma unroll
             for (int j = 0; j < BLK; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float v = __builtin_amdgcn_exp2f(w[j][e] - shift);
-                    sum += 16 * j + e == label[i] ? 0.f : v;
+                    if constexpr (CAP) w[j][e] = loss_capped(w[j][e], p.cap, p.to_cap, slope[j][e]);
+                    w[j][e] = fmaf(w[j][e], a[i], -b[i]);
                 }
-            sum = across_rows(sum, Add());
         };
-        weights();
-        if (__any(!(sum < 0x1p64f))) {                                         // scores far above the row's own entries (or NaN)
-            float most = w[0][0];
+        float sum;
+        auto weights = [&](float shift) __attribute__((always_inline)) {
+            float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int j = 0; j < BLK; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) most = fmaxf(most, w[j][e]);
+                for (int e = 0; e < 4; ++e) w[j][e] = __builtin_amdgcn_exp2f(w[j][e] - shift);
+            if (edge)
+#pragma unroll
+                for (int j = 0; j < BLK; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[j][e] = 16 * j + e < left ? w[j][e] : 0.f;
+            if (!TEACHER && __any((unsigned)label[i] < 16u * BLK)) {
+#pragma unroll
+                for (int j = 0; j < BLK; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[e] += 16 * j + e == label[i] ? 0.f : w[j][e];
+            } else {
+#pragma unroll
+                for (int j = 0; j < BLK; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[e] += w[j][e];
+            }
+            sum = across_rows((s[0] + s[1]) + (s[2] + s[3]), Add());
+        };
+        scores();
+        if constexpr (TEACHER) {
+            const LossHits& hit = row_hits[wm0 + 16 * i + l15];
+            const int n = hit.n;
+#pragma unroll 1
+            for (int k = 0; __any(k < n); ++k) {
+                int c = -1;
+                if (k < n) c = (k < 4 ? hit.id[k] : p.sorted[hit.at + k]) - (n0 + wn0);
+                const bool mine = (unsigned)c < (unsigned)TT::WN && (c >> 2 & 3) == lg;
+                if (!__any(mine)) continue;
+                const float s = loss_pick<BLK>(w, c >> 4, c & 3);
+                if (mine) p.scores[hit.at + k] = s;
+            }
+        }
+        if constexpr (CAP) {
+            float top = 0.f;
+#pragma unroll
+            for (int j = 0; j < BLK; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(w[j][e]));
+            if (__any(!(top <= kLossNear * p.cap))) exponents();
+            else {
+                const float to_exp = a[i] * p.cap;
+#pragma unroll
+                for (int j = 0; j < BLK; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float y = w[j][e] * p.to_cap, th = loss_tanh(y);
+                        slope[j][e] = fmaf(-th, th, 1.f);
+                        w[j][e] = fmaf(th, to_exp, -b[i]);
+                    }
+            }
+        } else exponents();
+        float shift = 0.f;
+        weights(0.f);
+        if (__any(!(sum < 0x1p64f))) {                                         // scores far above the row's own entries (or NaN)
+            const bool far = !(sum < 0x1p64f);
+            scores();
+            exponents();
+            float most = -__builtin_inff();
+#pragma unroll
+            for (int j = 0; j < BLK; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (!edge || 16 * j + e < left) most = fmaxf(most, w[j][e]);
             most = across_rows(most, Max());
-            shift = sum < 0x1p64f ? 0.f : most;
-            weights();
+            shift = far ? most : 0.f;
+            weights(shift);
         }
         if (lg == 0) stats[16 * i + l15] = make_float2(shift, sum);            // (rows behind the last one have room)
         if constexpr (GRAD) {
 #pragma unroll
             for (int j = 0; j < BLK; ++j) {
-                float v[4];
+                if constexpr (CAP)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    v[e] = __builtin_amdgcn_exp2f(w[j][e] - shift);
-                    if constexpr (CAP) v[e] *= slope[j][e];
-                }
-                *reinterpret_cast<uint2*>(smem + c_lane + i * 16 * CP + j * 32) = make_uint2(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]));
+                    for (int e = 0; e < 4; ++e) w[j][e] *= slope[j][e];
+                *reinterpret_cast<uint2*>(smem + c_lane + i * 16 * CP + j * 32) = make_uint2(pack2_bf16(w[j][0], w[j][1]), pack2_bf16(w[j][2], w[j][3]));
             }
         }
     });
@@ -411,107 +554,159 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_scores_kernel(const LossParams
     }
 }
 
-// ---- sums, losses, and the entries of q ---------------------------------------------------------------------------------------------
-constexpr int kJoinRows = 16, kJoinSets = 32;
-// 16 rows a workgroup of 512: the column parts' sums in a fixed order, the rows' losses, and their entries of p - q into the held weights.  `parts`: column parts of `cols` columns.
-SYMB_KERNEL __launch_bounds__(kJoinRows* kJoinSets) void symb_loss_join_kernel(const LossParams p, int parts, int cols) {
-    __shared__ float2 lds[kJoinSets][kJoinRows];
-    __shared__ float row_most[kJoinRows], row_sum[kJoinRows];
-    const int rows = loss_chunk_rows(p), m0 = blockIdx.x * kJoinRows;
-    if (m0 >= rows) return;
-    const int r = threadIdx.x % kJoinRows, set = threadIdx.x / kJoinRows, m = m0 + r;
-    // pairs (most, sum): the sum counts in units of 2^most
-    auto join = [](float2 x, float2 y) {
-        const float top = fmaxf(x.x, y.x);
-        return make_float2(top, (x.x == top ? x.y : x.y * exp2f(x.x - top)) + (y.x == top ? y.y : y.y * exp2f(y.x - top)));
-    };
-    float2 s = make_float2(0.f, 0.f);
-    if (m < rows)
-#pragma unroll 4
-        for (int c = set; c < parts; c += kJoinSets) s = join(s, p.stats[(size_t)c * p.chunk + m]);
-    lds[set][r] = s;
-    __syncthreads();
-    if (set == 0 && m < rows) {
-        for (int k = 1; k < kJoinSets; ++k) s = join(s, lds[k][r]);
-        const int t = p.rows[p.chunk0 + m], seg = seg_of_row(p.off, 0, p.S - 1, t);
-        float loss, l = s.y;
-        if (!p.ids) {
-            loss = s.x == 0.f ? log1pf(s.y) : s.x * kLn2 + logf(s.y + exp2f(-s.x));
-            l += exp2f(-s.x);
-            if (p.dX) p.row_gain[m] = p.gain[seg] / l;
-        } else {
-            const float T = p.losses[seg].temperature;
-            loss = T * T * (p.row_base[t] + s.x * kLn2 + logf(l));
-            if (p.dX) p.row_gain[m] = p.gain[seg] * T / l;
-        }
-        if (!(fabsf(p.row_ab[t].y) < __builtin_inff())) {              // (infinite scores among its entries)
-            loss = __builtin_nanf("");
-            if (p.dX) p.row_gain[m] = loss;
-        }
-        p.row_loss[t] = loss;
-        row_most[r] = s.x;
-        row_sum[r] = s.y;
-    }
-    if (!p.dX) return;
-    __syncthreads();
-    // columns that were held in other units than the row's
-    for (int k = 0; k < kJoinRows && m0 + k < rows; ++k) {
-        const float most = row_most[k];
-        if (!(most > 0.f)) continue;
-        bf16* const held = p.held + (size_t)(m0 + k) * p.pitch;
-        for (int c = threadIdx.x; c < p.pitch; c += kJoinRows * kJoinSets) {
-            const float shift = c < p.V ? p.stats[(size_t)(c / cols) * p.chunk + m0 + k].x : most;
-            if (shift != most) held[c] = (bf16)((float)held[c] * exp2f(shift - most));
-        }
-    }
-    __syncthreads();
-    for (int k = threadIdx.x; k < kJoinRows * p.K; k += kJoinRows * kJoinSets) {
-        const int row = k / p.K, j = k - row * p.K;
-        if (m0 + row >= rows) continue;
-        const int t = p.rows[p.chunk0 + m0 + row];
-        const int64_t at = (int64_t)t * p.K;
-        const float most = row_most[row], l = row_sum[row];
-        bf16* const held = p.held + (size_t)(m0 + row) * p.pitch;
-        if (!p.ids) {
-            const int id = p.flags[t];
-            if (id < p.V) held[id] = (bf16)(-l * p.slopes[at]);
-            continue;
-        }
-        const int id = p.ids[at + j];
-        if (id < 0 || id >= p.V) continue;
-        float q = 0.f;                                // (a token that the row names twice: both entries write the same)
-        for (int o = 0; o < p.K; ++o) q += p.ids[at + o] == id ? p.shares[at + o] : 0.f;
-        held[id] = (bf16)((exp2f(p.scores[at + j] - most) - q * l) * p.slopes[at + j]);
-    }
-}
-
-// ---- the gradient's product -----------------------------------------------------------------------------------------------------------
 // Parts that the second product's inner dimension (the vocabulary) is cut into: as few rounds of workgroups as possible, weighed against the partial tiles' way through memory.
-// Whole numbers: the kernels that ask for it have to agree.  room: partial tiles that fit the workspace.
 template <int BLK>
 struct LossGrad {
     static constexpr int kSlots = BLK == 8 ? 256 : 512;                        // workgroups at once
     static constexpr int kStageNs = BLK == 8 ? 1200 : 700, kPartNs = BLK == 8 ? 30000 : 15000;
-    static constexpr int kMostParts = 128;
 };
-__host__ __device__ constexpr int64_t loss_grad_ns(int64_t tiles, int stages, int n, int slots, int stage_ns, int part_ns) {
-    return (tiles * n + slots - 1) / slots * ((int64_t)((stages + n - 1) / n) * stage_ns + part_ns);
-}
+constexpr int kLossParts = 128;
 template <int BLK>
-__host__ __device__ inline int loss_grad_parts(int rows, int width, int V, int64_t room) {
+__host__ __device__ constexpr int64_t loss_grad_ns(int64_t tiles, int stages, int n) {
     using G = LossGrad<BLK>;
+    return (tiles * n + G::kSlots - 1) / G::kSlots * ((int64_t)((stages + n - 1) / n) * G::kStageNs + G::kPartNs);
+}
+// room: partial tiles that fit the workspace.
+__host__ __device__ constexpr bool loss_grad_fits(int64_t tiles, int stages, int n, int64_t room) { return n == 1 || (tiles * n <= room && stages / n >= 4); }
+
+// ---- sums, losses, and the entries of q ---------------------------------------------------------------------------------------------
+constexpr int kJoinRows = 16, kJoinSets = 32;
+// Pairs (unit, sum): the sum counts in 2^unit.
+__device__ __forceinline__ float loss_in(float2 s, float unit) { return s.x == unit ? s.y : s.y * exp2f(s.x - unit); }
+// 16 rows a workgroup of 512: the column parts' sums in a fixed order, the rows' losses, and their entries of p - q into the held weights.  `parts`: column parts of `cols` columns;
+// finish: the segments' losses as well (one workgroup has all rows).  Beside that, for how many parts the gradient's product comes in.
+template <int BLK>
+__device__ __forceinline__ int loss_grad_parts(const LossParams& p, int rows) {
     constexpr int BM = 32 * BLK;
-    const int64_t tiles = (int64_t)((rows + BM - 1) / BM) * ((width + BM - 1) / BM);
-    const int stages = V / 64;
-    int best = 1;
-    int64_t least = loss_grad_ns(tiles, stages, 1, G::kSlots, G::kStageNs, G::kPartNs);
-    for (int n = 2; n <= G::kMostParts && tiles * n <= room && stages / n >= 4; ++n) {
-        const int64_t ns = loss_grad_ns(tiles, stages, n, G::kSlots, G::kStageNs, G::kPartNs);
-        if (ns * 200 < least * 199) least = ns, best = n;
+    const int64_t tiles = (int64_t)((rows + BM - 1) / BM) * ((p.width + BM - 1) / BM);
+    const int stages = p.V / 64;
+    float best = 3e38f;                                   // (nanoseconds)
+    int n = 1;
+    for (int k = 1 + (int)(threadIdx.x & 63); k <= kLossParts; k += 64) {
+        const float ns = loss_grad_fits(tiles, stages, k, p.part_tiles) ? (float)loss_grad_ns<BLK>(tiles, stages, k) * (1.f + 1e-4f * k) : 3e38f;
+        if (ns < best) best = ns, n = k;
     }
-    return best;
+#pragma unroll
+    for (int m = 32; m; m >>= 1) {
+        const float other = __shfl_xor(best, m);
+        const int k = __shfl_xor(n, m);
+        if (other < best || (other == best && k < n)) best = other, n = k;
+    }
+    return n;
+}
+SYMB_KERNEL __launch_bounds__(kJoinRows* kJoinSets) void symb_loss_join_kernel(const LossParams p, int parts, int cols, bool finish) {
+    __shared__ float2 lds[kJoinSets / 4][kJoinRows];
+    __shared__ float row_unit[kJoinRows], row_sum[kJoinRows], row_gain[kJoinRows];
+    __shared__ int row_t[kJoinRows];
+    __shared__ LossRow row_info[kJoinRows];
+    const int r = threadIdx.x % kJoinRows, set = threadIdx.x / kJoinRows, m0 = blockIdx.x * kJoinRows, m = m0 + r, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int rows = loss_chunk_rows(p);
+    if (m0 >= rows && !finish) return;
+    if (p.dX && blockIdx.x == 0 && wave == kJoinSets / 4 - 1) {
+        const int n = p.grad_blk == 8 ? loss_grad_parts<8>(p, rows) : loss_grad_parts<4>(p, rows);
+        if (lane == 0) *p.part_count = n;
+    }
+    int t = 0;
+    LossRow info{};
+    float gain = 0.f;
+    if (set == 0 && m < rows) {
+        t = p.rows[p.chunk0 + m];
+        info = p.info[t];
+        gain = p.gain[info.seg];
+    }
+    float2 s = make_float2(0.f, 0.f);
+    if (m < rows) {
+        const float2* at = p.stats + (size_t)set * p.chunk + m;
+        const size_t step = (size_t)kJoinSets * p.chunk;
+        constexpr int AHEAD = 8;
+        for (int c = set; c < parts; c += AHEAD * kJoinSets, at += AHEAD * step) {
+            float2 v[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) v[k] = c + k * kJoinSets < parts ? at[k * step] : make_float2(0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                if (v[k].x == s.x) s.y += v[k].y;
+                else {
+                    const float unit = fmaxf(s.x, v[k].x);
+                    s = make_float2(unit, loss_in(s, unit) + loss_in(v[k], unit));
+                }
+            }
+        }
+    }
+    const float top = across_rows(s.x, Max()), part = across_rows(loss_in(s, top), Add());
+    if (lane < kJoinRows) lds[wave][r] = make_float2(top, part);
+    __syncthreads();
+    if (set == 0 && m < rows) {
+        float unit = 0.f, l = 0.f;
+#pragma unroll
+        for (int k = 0; k < kJoinSets / 4; ++k) unit = fmaxf(unit, lds[k][r].x);
+#pragma unroll
+        for (int k = 0; k < kJoinSets / 4; ++k) l += loss_in(lds[k][r], unit);
+        row_unit[r] = unit;
+        row_sum[r] = l;
+        row_t[r] = t;
+        row_info[r] = info;
+        if (!(fabsf(info.b) < __builtin_inff())) gain = l = __builtin_nanf("");          // (infinite scores among its entries)
+        if (!p.ids) {
+            p.row_loss[t] = unit == 0.f ? log1pf(l) : unit * kLn2 + logf(l + exp2f(-unit));
+            l += exp2f(-unit);
+        } else gain *= kLog2e / info.a;
+        if (p.dX) p.row_gain[m] = gain / l;
+        row_gain[r] = l;
+    }
+    __syncthreads();
+    if (p.dX) {
+        // columns that were held in other units than the row's
+        for (int k = 0; k < kJoinRows && m0 + k < rows; ++k) {
+            const float unit = row_unit[k];
+            if (!(unit > 0.f)) continue;
+            bf16* const held = p.held + (size_t)(m0 + k) * p.pitch;
+            for (int c = threadIdx.x; c < p.pitch; c += kJoinRows * kJoinSets) {
+                const float shift = c < p.V ? p.stats[(size_t)(c / cols) * p.chunk + m0 + k].x : unit;
+                if (shift != unit) held[c] = (bf16)((float)held[c] * exp2f(shift - unit));
+            }
+        }
+        __syncthreads();
+        if (!p.ids && set == 0 && m < rows) {
+            const int id = p.flags[t];
+            if (id < p.V) p.held[(size_t)m * p.pitch + id] = (bf16)(-row_sum[r] * p.slopes[t]);
+        }
+    }
+    if (p.ids)
+        for (int k = wave; k < kJoinRows && m0 + k < rows; k += kJoinRows * kJoinSets / 64) {
+            const LossRow row = row_info[k];
+            const float unit = row_unit[k], l = row_gain[k], T = kLog2e / row.a;
+            const int64_t at = (int64_t)row_t[k] * p.K;
+            bf16* const held = p.held + (size_t)(m0 + k) * p.pitch;
+            float base = 0.f;
+            for (int j = lane; j < row.entries; j += 64) {
+                const int id = p.sorted[at + j];
+                if (id >= p.V) continue;                   // (the row is NaN already)
+                float q = p.shares[at + j], z = p.scores[at + j], slope = 1.f;
+                if (p.cap > 0.f) z = loss_capped(z, p.cap, p.to_cap, slope);
+                z = fmaf(z, row.a, -row.b);
+                if (!(q == 0.f)) base += q * (logf(q) - z * kLn2);
+                if (!p.dX || (j && p.sorted[at + j - 1] == id)) continue;
+                for (int o = j + 1; o < row.entries && p.sorted[at + o] == id; ++o) q += p.shares[at + o];     // (a token that the row names twice)
+                held[id] = (bf16)((exp2f(z - unit) - q * l) * slope);
+            }
+            base = across_wave(base, Add());
+            if (lane == 0) p.row_loss[row_t[k]] = T * T * (base + unit * kLn2 + logf(l));
+        }
+    if (!finish) return;
+    __syncthreads();
+    for (int i = threadIdx.x; i < p.S; i += kJoinRows * kJoinSets) {
+        float sum = 0.f;
+        int n = 0;
+        for (int k = p.off[i]; k < p.off[i + 1]; ++k) {
+            sum += p.row_loss[k];
+            n += p.flags[k] >= 0;
+        }
+        p.loss[i] = p.mean ? sum / (float)max(n, 1) : sum;
+    }
 }
 
+// ---- the gradient's product -----------------------------------------------------------------------------------------------------------
 template <int BLK>
 SYMB_KERNEL __launch_bounds__(256) void symb_loss_grad_kernel(const LossParams p) {
     using TT = Gemm16Tile<BLK, BLK>;
@@ -520,7 +715,7 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_grad_kernel(const LossParams p
     const int rows = loss_chunk_rows(p);
     if (rows <= 0) return;
     const int m_tiles = (rows + BM - 1) / BM, n_tiles = (p.width + BN - 1) / BN, tiles = m_tiles * n_tiles;
-    const int n = loss_grad_parts<BLK>(rows, p.width, p.V, p.part_tiles), total = tiles * n, per_xcd = (total + 7) >> 3;
+    const int n = *p.part_count, total = tiles * n, per_xcd = (total + 7) >> 3;
     const int lin = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= per_xcd || lin >= total) return;
     const int part = lin / tiles;
@@ -537,28 +732,35 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_grad_kernel(const LossParams p
     else asm volatile(SYMB_GEMM16S_STORE_PARTIAL : : "v"(lane_off), "s"(mine) : "memory", SYMB_GEMM16S_VCLOBBERS);
 }
 
-// The parts of a tile added in order, times the row's gain, to the rows they belong to.  A workgroup takes one wavefront's 16 rows of a tile.
-template <int BLK>
+// The parts of a tile added in a fixed order, times the row's gain, to the rows they belong to.  A workgroup takes blocks of 16 x 16 of one wavefront's rows: four of them, or, of products in many
+// parts, one whose parts its wavefronts share out.
+template <int BLK, bool MANY>
 SYMB_KERNEL __launch_bounds__(256) void symb_loss_reduce_kernel(const LossParams p) {
-    constexpr int BM = 32 * BLK;
+    constexpr int BM = 32 * BLK, GROUPS = MANY ? BLK : BLK / 4;
+    __shared__ floatx4 lds[4][64];
     const int rows = loss_chunk_rows(p);
     if (rows <= 0) return;
     const int n_tiles = (p.width + BM - 1) / BM, m_tiles = (rows + BM - 1) / BM, tiles = m_tiles * n_tiles;
-    const int tile = blockIdx.x / (4 * BLK), wave = blockIdx.x / BLK % 4, i = blockIdx.x % BLK;
-    const int m = tile / n_tiles * BM + (wave >> 1) * (BM / 2) + 16 * i + (threadIdx.x & 15);
-    if (tile >= tiles || m >= rows) return;
-    const int n = loss_grad_parts<BLK>(rows, p.width, p.V, p.part_tiles);
-    const float gain = p.row_gain[m];
-    bf16* const out = p.dX + (size_t)p.rows[p.chunk0 + m] * p.width;
-    for (int j = threadIdx.x >> 6; j < BLK; j += 4) {
-        const int col = tile % n_tiles * BM + (wave & 1) * (BM / 2) + 16 * j + 4 * (threadIdx.x >> 4 & 3);
-        if (col >= p.width) continue;
-        const float* src = p.parts + (size_t)tile * (BM * BM) + (size_t)(wave * BLK * BLK + BLK * i + j) * 256 + (threadIdx.x & 63) * 4;
-        floatx4 s = *(const floatx4*)src;
-#pragma unroll 4
-        for (int k = 1; k < n; ++k) s += *(const floatx4*)(src + (size_t)k * tiles * (BM * BM));
-        *(uint2*)(out + col) = make_uint2(pack2_bf16(s[0] * gain, s[1] * gain), pack2_bf16(s[2] * gain, s[3] * gain));
+    const int lane = threadIdx.x & 63, own = threadIdx.x >> 6, j = blockIdx.x % GROUPS * (MANY ? 1 : 4) + (MANY ? 0 : own);
+    const int i = blockIdx.x / GROUPS % BLK, wave = blockIdx.x / (GROUPS * BLK) % 4, tile = blockIdx.x / (GROUPS * BLK * 4);
+    if (tile >= tiles) return;
+    const int m = tile / n_tiles * BM + (wave >> 1) * (BM / 2) + 16 * i + (lane & 15), col = tile % n_tiles * BM + (wave & 1) * (BM / 2) + 16 * j + 4 * (lane >> 4);
+    const int n = *p.part_count;
+    const float* src = p.parts + (size_t)tile * (BM * BM) + (size_t)(wave * BLK * BLK + BLK * i + j) * 256 + lane * 4;
+    floatx4 s = floatx4{0, 0, 0, 0};
+#pragma unroll 8
+    for (int k = MANY ? own : 0; k < n; k += MANY ? 4 : 1) s += *(const floatx4*)(src + (size_t)k * tiles * (BM * BM));
+    if constexpr (MANY) {
+        lds[own][lane] = s;
+        __syncthreads();
+        if (own) return;
+        s += lds[1][lane];
+        s += lds[2][lane];
+        s += lds[3][lane];
     }
+    if (m >= rows || col >= p.width) return;
+    const float gain = p.row_gain[m];
+    *(uint2*)(p.dX + (size_t)p.rows[p.chunk0 + m] * p.width + col) = make_uint2(pack2_bf16(s[0] * gain, s[1] * gain), pack2_bf16(s[2] * gain, s[3] * gain));
 }
 
 // A segment's loss: its rows' in a fixed order.

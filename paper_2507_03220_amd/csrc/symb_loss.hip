@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 #include <vector>
 
 #include "loss_kernels.hpp"
@@ -43,7 +44,8 @@ symb_status check_loss(symb_handle h, const symb_loss_batch* b, int32_t entries)
 struct LossPlan {
     int chunk = 0, score_blk = 8, grad_blk = 8, pitch = 0, column_parts = 0;
     int64_t part_tiles = 0;
-    size_t rows = 0, flags = 0, count = 0, gain = 0, scores = 0, slopes = 0, shares = 0, row_ab = 0, row_base = 0, row_loss = 0, stats = 0, row_gain = 0, held = 0, parts = 0, bytes = 0;
+    bool many_parts = false;              // the second product's tiles come in many parts
+    size_t rows = 0, flags = 0, count = 0, gain = 0, info = 0, slopes = 0, sorted = 0, shares = 0, scores = 0, starts = 0, row_loss = 0, stats = 0, row_gain = 0, held = 0, parts = 0, bytes = 0;
 };
 // What a call may hold: weights of a chunk of rows, and, where the losses alone are wanted, their sums.
 constexpr int64_t kHeldBytes = (int64_t)2 << 30, kStatBytes = (int64_t)256 << 20;
@@ -57,14 +59,18 @@ double score_us(int rows, const symb_loss_batch* b, int blk) {
 }
 template <int BLK>
 double grad_us(int rows, const symb_loss_batch* b, int& n) {
-    using G = LossGrad<BLK>;
-    n = loss_grad_parts<BLK>(rows, b->width, b->vocab, INT64_MAX);
-    return 1e-3 * (double)loss_grad_ns(tiles_of(rows, b->width, 32 * BLK), b->vocab / 64, n, G::kSlots, G::kStageNs, G::kPartNs);
+    const int64_t tiles = tiles_of(rows, b->width, 32 * BLK);
+    int64_t least = INT64_MAX;
+    for (int k = 1; k <= kLossParts && loss_grad_fits(tiles, b->vocab / 64, k, INT64_MAX); ++k) {
+        const int64_t ns = loss_grad_ns<BLK>(tiles, b->vocab / 64, k);
+        if (ns + ns / 10000 * k < least) least = ns + ns / 10000 * k, n = k;
+    }
+    return 1e-3 * (double)least;
 }
 
 LossPlan plan_loss(const symb_loss_batch* b, int32_t entries, bool gradient) {
     LossPlan plan;
-    const int64_t T = b->seg_offsets[b->num_segments], K = std::max(entries, 1);
+    const int64_t T = b->seg_offsets[b->num_segments], listed = T * entries;
     const int rows = (int)((T + 255) / 256 * 256);
     plan.pitch = (b->vocab + 63) / 64 * 64;
     const int64_t row_bytes = gradient ? (int64_t)plan.pitch * 2 : ((int64_t)(b->vocab + 255) / 256) * 4 * (int64_t)sizeof(float2);
@@ -84,6 +90,7 @@ LossPlan plan_loss(const symb_loss_batch* b, int32_t entries, bool gradient) {
     if (gradient) {
         plan.grad_blk = grad_us<8>(first, b, n8) < grad_us<4>(first, b, n4) ? 8 : 4;
         const int edge = 32 * plan.grad_blk;
+        plan.many_parts = (plan.grad_blk == 8 ? n8 : n4) >= 8;
         plan.part_tiles = std::max<int64_t>(tiles_of(first, b->width, edge) * (plan.grad_blk == 8 ? n8 : n4), std::min<int64_t>(512, tiles_of(1, b->width, edge) * std::max(b->vocab / 256, 1)));
     }
     plan.column_parts = (b->vocab + 32 * plan.score_blk - 1) / (32 * plan.score_blk) * 2;
@@ -95,13 +102,14 @@ LossPlan plan_loss(const symb_loss_batch* b, int32_t entries, bool gradient) {
     };
     plan.rows = take(T * sizeof(int32_t));
     plan.flags = take(entries ? T * sizeof(int32_t) : 0);
-    plan.count = take(sizeof(int32_t));
+    plan.count = take(2 * sizeof(int32_t));
     plan.gain = take(b->num_segments * sizeof(float));
-    plan.scores = take(T * K * sizeof(float));
-    plan.slopes = take(T * K * sizeof(float));
-    plan.shares = take(entries ? T * K * sizeof(float) : 0);
-    plan.row_ab = take(T * sizeof(float2));
-    plan.row_base = take(entries ? T * sizeof(float) : 0);
+    plan.info = take(T * sizeof(LossRow));
+    plan.slopes = take(entries ? 0 : T * sizeof(float));
+    plan.sorted = take(listed * sizeof(int32_t));
+    plan.shares = take(listed * sizeof(float));
+    plan.scores = take(listed * sizeof(float));
+    plan.starts = take(entries ? T * (plan.column_parts / 2 + 1) * sizeof(uint16_t) : 0);
     plan.row_loss = take(T * sizeof(float));
     plan.stats = take((size_t)plan.column_parts * plan.chunk * sizeof(float2));
     plan.row_gain = take(gradient ? plan.chunk * sizeof(float) : 0);
@@ -127,14 +135,20 @@ symb_status launch_tiles(symb_handle h, F kernel, int64_t tiles, const LossParam
 template <int BLK>
 symb_status launch_scores(symb_handle h, const LossParams& p, int rows, hipStream_t s) {
     const int64_t tiles = tiles_of(rows, p.V, 32 * BLK);
-    if (p.dX) return p.cap > 0.f ? launch_tiles<BLK>(h, symb_loss_scores_kernel<BLK, true, true>, tiles, p, s) : launch_tiles<BLK>(h, symb_loss_scores_kernel<BLK, true, false>, tiles, p, s);
-    return p.cap > 0.f ? launch_tiles<BLK>(h, symb_loss_scores_kernel<BLK, false, true>, tiles, p, s) : launch_tiles<BLK>(h, symb_loss_scores_kernel<BLK, false, false>, tiles, p, s);
+    auto by_teacher = [&](auto grad, auto cap) {
+        constexpr bool G = decltype(grad)::value, C = decltype(cap)::value;
+        return p.ids ? launch_tiles<BLK>(h, symb_loss_scores_kernel<BLK, G, C, true>, tiles, p, s) : launch_tiles<BLK>(h, symb_loss_scores_kernel<BLK, G, C, false>, tiles, p, s);
+    };
+    auto by_cap = [&](auto grad) { return p.cap > 0.f ? by_teacher(grad, std::true_type{}) : by_teacher(grad, std::false_type{}); };
+    return p.dX ? by_cap(std::true_type{}) : by_cap(std::false_type{});
 }
 template <int BLK>
-symb_status launch_grad(symb_handle h, const LossParams& p, int rows, hipStream_t s) {
+symb_status launch_grad(symb_handle h, const LossParams& p, int rows, bool many_parts, hipStream_t s) {
     const symb_status st = launch_tiles<BLK>(h, symb_loss_grad_kernel<BLK>, p.part_tiles, p, s);
     if (st != SYMB_OK) return st;
-    hipLaunchKernelGGL(symb_loss_reduce_kernel<BLK>, dim3((unsigned)(tiles_of(rows, p.width, 32 * BLK) * 4 * BLK)), dim3(256), 0, s, p);
+    const unsigned blocks = (unsigned)(tiles_of(rows, p.width, 32 * BLK) * 4 * BLK * BLK);
+    if (many_parts) hipLaunchKernelGGL((symb_loss_reduce_kernel<BLK, true>), dim3(blocks), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((symb_loss_reduce_kernel<BLK, false>), dim3(blocks / 4), dim3(256), 0, s, p);
     SYMB_HIP(h, hipGetLastError());
     return SYMB_OK;
 }
@@ -177,12 +191,14 @@ symb_status run_loss(symb_handle h, const symb_loss_batch* b, const void* X, con
     p.losses = (const LossDesc*)(dev + o_ld);
     p.rows = (int32_t*)(w + plan.rows);
     p.count = (int32_t*)(w + plan.count);
+    p.part_count = p.count + 1;
     p.gain = (float*)(w + plan.gain);
-    p.scores = (float*)(w + plan.scores);
+    p.info = (LossRow*)(w + plan.info);
     p.slopes = (float*)(w + plan.slopes);
+    p.sorted = (int32_t*)(w + plan.sorted);
     p.shares = (float*)(w + plan.shares);
-    p.row_ab = (float2*)(w + plan.row_ab);
-    p.row_base = (float*)(w + plan.row_base);
+    p.scores = (float*)(w + plan.scores);
+    p.starts = (uint16_t*)(w + plan.starts);
     p.stats = (float2*)(w + plan.stats);
     p.row_gain = (float*)(w + plan.row_gain);
     p.held = (bf16*)(w + plan.held);
@@ -193,31 +209,34 @@ symb_status run_loss(symb_handle h, const symb_loss_batch* b, const void* X, con
     p.V = b->vocab;
     p.pitch = plan.pitch;
     p.width = b->width;
-    p.K = std::max(entries, 1);
+    p.K = entries;
+    p.tile_cols = 32 * plan.score_blk;
     p.chunk = plan.chunk;
     p.group_m = 8;
+    p.grad_blk = plan.grad_blk;
     p.mean = b->reduction == SYMB_LOSS_MEAN;
     p.cap = b->cap;
     p.to_cap = b->cap > 0.f ? 1.f / b->cap : 0.f;
-    if (T) {
-        if (entries) {
-            hipLaunchKernelGGL(symb_loss_teacher_kernel, dim3((T + 3) / 4), dim3(256), 0, s, p);
-            SYMB_HIP(h, hipGetLastError());
-        }
-        hipLaunchKernelGGL(symb_loss_rows_kernel, dim3((T + 255) / 256 + S), dim3(256), 0, s, p);
+    const unsigned lists = (unsigned)((T + 255) / 256 + S), fours = (unsigned)((T + 3) / 4);
+    if (entries && T) {
+        hipLaunchKernelGGL(symb_loss_teacher_kernel, dim3(fours), dim3(256), 4 * 2 * align_up(entries, 64) * sizeof(int32_t), s, p);
         SYMB_HIP(h, hipGetLastError());
-        hipLaunchKernelGGL(symb_loss_entries_kernel, dim3(T), dim3(256), 0, s, p);
+        hipLaunchKernelGGL(symb_loss_rows_kernel, dim3(lists), dim3(256), 0, s, p);
+        SYMB_HIP(h, hipGetLastError());
+    } else if (T) {
+        hipLaunchKernelGGL(symb_loss_labels_kernel, dim3(lists + fours), dim3(256), 0, s, p);
         SYMB_HIP(h, hipGetLastError());
     }
+    const bool finish = loss && T && T <= kJoinRows;
     for (int64_t at = 0; at < T; at += plan.chunk) {
         p.chunk0 = (int32_t)at;
         const int rows = (int)std::min<int64_t>(T - at, plan.chunk);
         if ((st = plan.score_blk == 8 ? launch_scores<8>(h, p, rows, s) : launch_scores<4>(h, p, rows, s)) != SYMB_OK) return st;
-        hipLaunchKernelGGL(symb_loss_join_kernel, dim3((rows + kJoinRows - 1) / kJoinRows), dim3(kJoinRows * kJoinSets), 0, s, p, plan.column_parts, 16 * plan.score_blk);
+        hipLaunchKernelGGL(symb_loss_join_kernel, dim3((rows + kJoinRows - 1) / kJoinRows), dim3(kJoinRows * kJoinSets), 0, s, p, plan.column_parts, 16 * plan.score_blk, finish);
         SYMB_HIP(h, hipGetLastError());
-        if (dX && (st = plan.grad_blk == 8 ? launch_grad<8>(h, p, rows, s) : launch_grad<4>(h, p, rows, s)) != SYMB_OK) return st;
+        if (dX && (st = plan.grad_blk == 8 ? launch_grad<8>(h, p, rows, plan.many_parts, s) : launch_grad<4>(h, p, rows, plan.many_parts, s)) != SYMB_OK) return st;
     }
-    if (loss) {
+    if (loss && !finish) {
         hipLaunchKernelGGL(symb_loss_segments_kernel, dim3(S), dim3(256), 0, s, p);
         SYMB_HIP(h, hipGetLastError());
     }
