@@ -558,13 +558,16 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_scores_kernel(const LossParams
 template <int BLK>
 struct LossGrad {
     static constexpr int kSlots = BLK == 8 ? 256 : 512;                        // workgroups at once
-    static constexpr int kStageNs = BLK == 8 ? 1200 : 700, kPartNs = BLK == 8 ? 30000 : 15000;
+    static constexpr int kPartNs = BLK == 8 ? 116 : 40;                        // a partial tile, written and read
 };
-constexpr int kLossParts = 128;
+constexpr int kLossParts = 128, kLossRoundNs = 5000;
+// A stage of a tile of 256 x 256; of 128 x 128, of two workgroups that share a CU and of one that has it alone.
+constexpr int kLossStageNs = 1400, kLossStage4Ns = 1100, kLossLoneNs = 720;
 template <int BLK>
 __host__ __device__ constexpr int64_t loss_grad_ns(int64_t tiles, int stages, int n) {
     using G = LossGrad<BLK>;
-    return (tiles * n + G::kSlots - 1) / G::kSlots * ((int64_t)((stages + n - 1) / n) * G::kStageNs + G::kPartNs);
+    const int stage = BLK == 8 ? kLossStageNs : tiles * n <= G::kSlots / 2 ? kLossLoneNs : kLossStage4Ns;
+    return (tiles * n + G::kSlots - 1) / G::kSlots * ((int64_t)((stages + n - 1) / n) * stage + kLossRoundNs) + tiles * n * G::kPartNs;
 }
 // room: partial tiles that fit the workspace.
 __host__ __device__ constexpr bool loss_grad_fits(int64_t tiles, int stages, int n, int64_t room) { return n == 1 || (tiles * n <= room && stages / n >= 4); }
@@ -732,12 +735,37 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_grad_kernel(const LossParams p
     else asm volatile(SYMB_GEMM16S_STORE_PARTIAL : : "v"(lane_off), "s"(mine) : "memory", SYMB_GEMM16S_VCLOBBERS);
 }
 
+// A segment's loss: its rows' in a fixed order.
+__device__ __forceinline__ void loss_segment(const LossParams& p, int i, floatx4* room) {
+    float* const lds = (float*)room;
+    int* const counts = (int*)(room + 1);
+    float s = 0.f;
+    int n = 0;
+    for (int t = p.off[i] + threadIdx.x; t < p.off[i + 1]; t += 256) {
+        s += p.row_loss[t];
+        n += p.flags[t] >= 0;
+    }
+    s = across_wave(s, Add());
+    n = loss_count(n, counts);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s = lds[0] + lds[1] + lds[2] + lds[3];
+        p.loss[i] = p.mean ? s / (float)max(n, 1) : s;
+    }
+}
+SYMB_KERNEL __launch_bounds__(256) void symb_loss_segments_kernel(LossParams p) {
+    __shared__ floatx4 lds[2];
+    loss_segment(p, blockIdx.x, lds);
+}
+
 // The parts of a tile added in a fixed order, times the row's gain, to the rows they belong to.  A workgroup takes blocks of 16 x 16 of one wavefront's rows: four of them, or, of products in many
-// parts, one whose parts its wavefronts share out.
+// parts, one whose parts its wavefronts share out.  Workgroups from number `blocks` on: the segments' losses.
 template <int BLK, bool MANY>
-SYMB_KERNEL __launch_bounds__(256) void symb_loss_reduce_kernel(const LossParams p) {
+SYMB_KERNEL __launch_bounds__(256) void symb_loss_reduce_kernel(const LossParams p, int blocks) {
     constexpr int BM = 32 * BLK, GROUPS = MANY ? BLK : BLK / 4;
     __shared__ floatx4 lds[4][64];
+    if ((int)blockIdx.x >= blocks) return loss_segment(p, blockIdx.x - blocks, lds[0]);
     const int rows = loss_chunk_rows(p);
     if (rows <= 0) return;
     const int n_tiles = (p.width + BM - 1) / BM, m_tiles = (rows + BM - 1) / BM, tiles = m_tiles * n_tiles;
@@ -761,27 +789,6 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_reduce_kernel(const LossParams
     if (m >= rows || col >= p.width) return;
     const float gain = p.row_gain[m];
     *(uint2*)(p.dX + (size_t)p.rows[p.chunk0 + m] * p.width + col) = make_uint2(pack2_bf16(s[0] * gain, s[1] * gain), pack2_bf16(s[2] * gain, s[3] * gain));
-}
-
-// A segment's loss: its rows' in a fixed order.
-SYMB_KERNEL __launch_bounds__(256) void symb_loss_segments_kernel(LossParams p) {
-    __shared__ float lds[4];
-    __shared__ int counts[4];
-    const int i = blockIdx.x;
-    float s = 0.f;
-    int n = 0;
-    for (int t = p.off[i] + threadIdx.x; t < p.off[i + 1]; t += 256) {
-        s += p.row_loss[t];
-        n += p.flags[t] >= 0;
-    }
-    s = across_wave(s, Add());
-    n = loss_count(n, counts);
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        s = lds[0] + lds[1] + lds[2] + lds[3];
-        p.loss[i] = p.mean ? s / (float)max(n, 1) : s;
-    }
 }
 
 }  // namespace symb

@@ -55,7 +55,8 @@ int64_t tiles_of(int64_t rows, int64_t columns, int edge) { return ((rows + edge
 // Microseconds of the product with W of so many rows, in tiles of 32 blk.
 double score_us(int rows, const symb_loss_batch* b, int blk) {
     const int64_t tiles = tiles_of(rows, b->vocab, 32 * blk), slots = blk == 8 ? 256 : 512;
-    return (double)((tiles + slots - 1) / slots) * ((b->width + 63) / 64 * (blk == 8 ? 1.2 : 0.7) + (blk == 8 ? 10 : 6));
+    const int stage = blk == 8 ? kLossStageNs : tiles <= slots / 2 ? kLossLoneNs : kLossStage4Ns;
+    return 1e-3 * (double)((tiles + slots - 1) / slots) * ((b->width + 63) / 64 * stage + (blk == 8 ? 8000 : 6000));
 }
 template <int BLK>
 double grad_us(int rows, const symb_loss_batch* b, int& n) {
@@ -79,7 +80,8 @@ LossPlan plan_loss(const symb_loss_batch* b, int32_t entries, bool gradient) {
     int n8 = 1, n4 = 1;
     double least = 1e300;
     plan.chunk = most;
-    for (int c = 256; c <= most; c += 256) {
+    const int step = std::max(256, most / 64 / 256 * 256);
+    for (int c = step; c <= most; c += step) {
         const int whole = rows / c, rest = rows % c;
         auto us = [&](int r) { return r ? std::min(score_us(r, b, 8), score_us(r, b, 4)) + (gradient ? std::min(grad_us<8>(r, b, n8), grad_us<4>(r, b, n4)) : 0.0) + 15.0 : 0.0; };
         const double all = whole * us(c) + us(rest);
@@ -143,12 +145,12 @@ symb_status launch_scores(symb_handle h, const LossParams& p, int rows, hipStrea
     return p.dX ? by_cap(std::true_type{}) : by_cap(std::false_type{});
 }
 template <int BLK>
-symb_status launch_grad(symb_handle h, const LossParams& p, int rows, bool many_parts, hipStream_t s) {
+symb_status launch_grad(symb_handle h, const LossParams& p, int rows, bool many_parts, bool segments, hipStream_t s) {
     const symb_status st = launch_tiles<BLK>(h, symb_loss_grad_kernel<BLK>, p.part_tiles, p, s);
     if (st != SYMB_OK) return st;
-    const unsigned blocks = (unsigned)(tiles_of(rows, p.width, 32 * BLK) * 4 * BLK * BLK);
-    if (many_parts) hipLaunchKernelGGL((symb_loss_reduce_kernel<BLK, true>), dim3(blocks), dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((symb_loss_reduce_kernel<BLK, false>), dim3(blocks / 4), dim3(256), 0, s, p);
+    const unsigned blocks = (unsigned)(tiles_of(rows, p.width, 32 * BLK) * 4 * BLK * BLK / (many_parts ? 1 : 4)), more = segments ? p.S : 0;
+    if (many_parts) hipLaunchKernelGGL((symb_loss_reduce_kernel<BLK, true>), dim3(blocks + more), dim3(256), 0, s, p, (int)blocks);
+    else hipLaunchKernelGGL((symb_loss_reduce_kernel<BLK, false>), dim3(blocks + more), dim3(256), 0, s, p, (int)blocks);
     SYMB_HIP(h, hipGetLastError());
     return SYMB_OK;
 }
@@ -234,9 +236,10 @@ symb_status run_loss(symb_handle h, const symb_loss_batch* b, const void* X, con
         if ((st = plan.score_blk == 8 ? launch_scores<8>(h, p, rows, s) : launch_scores<4>(h, p, rows, s)) != SYMB_OK) return st;
         hipLaunchKernelGGL(symb_loss_join_kernel, dim3((rows + kJoinRows - 1) / kJoinRows), dim3(kJoinRows * kJoinSets), 0, s, p, plan.column_parts, 16 * plan.score_blk, finish);
         SYMB_HIP(h, hipGetLastError());
-        if (dX && (st = plan.grad_blk == 8 ? launch_grad<8>(h, p, rows, plan.many_parts, s) : launch_grad<4>(h, p, rows, plan.many_parts, s)) != SYMB_OK) return st;
+        const bool segments = loss && !finish && at + rows == T;
+        if (dX && (st = plan.grad_blk == 8 ? launch_grad<8>(h, p, rows, plan.many_parts, segments, s) : launch_grad<4>(h, p, rows, plan.many_parts, segments, s)) != SYMB_OK) return st;
     }
-    if (loss && !finish) {
+    if (loss && !finish && !(dX && T)) {
         hipLaunchKernelGGL(symb_loss_segments_kernel, dim3(S), dim3(256), 0, s, p);
         SYMB_HIP(h, hipGetLastError());
     }
