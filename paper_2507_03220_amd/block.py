@@ -166,8 +166,9 @@ class AttentionBlock:
 
 
 def main() -> None:
-    """Four clients with LoRA adapters of their own on a Llama2-7B-shaped block: prompts, 32 decode steps, and a fine-tuning step through a normed projection."""
+    """Four clients with LoRA adapters of their own on a Llama2-7B-shaped block: prompts, 32 decode steps, and a fine-tuning step through a normed projection, from the losses of its outputs back."""
     import time
+    from .head import LossHead
     g = torch.Generator(device="cuda").manual_seed(0)
     normal = lambda *s, std=1.0, mean=0.0: (torch.randn(*s, device="cuda", generator=g) * std + mean).to(BF16)  # noqa: E731
     h, width, heads, H, D, r = sb.symb_create(torch.cuda.current_device()), 4096, 32, 32, 128, 16
@@ -194,8 +195,17 @@ def main() -> None:
     timed("32 decode steps of 4 clients", lambda: [block.forward(normal(4, width), [1] * 4, clients, stream) for _ in range(32)])
     norms = [sb.Norm(c.norm.weight, None, torch.empty(width, device="cuda")) for c in clients]
     step = NormedProjection(h, W["q"], lens, norms, [lora("q", grads=True) for _ in lens], sb.SYMB_NORM_RMS, 1e-6)
-    X, dY = normal(sum(lens), width), normal(sum(lens), heads * D)
-    timed("fine-tuning step through norm and projection", lambda: (step.forward(X, None, stream), step.backward(X, dY, stream=stream)))
+    vocab, X = 32000, normal(sum(lens), width)
+    head = LossHead(h, normal(vocab, heads * D, std=(heads * D) ** -0.5), lens, [sb.Norm(normal(heads * D, std=0.1, mean=1.0)) for _ in lens], [sb.Loss() for _ in lens])
+    labels = torch.randint(0, vocab, (sum(lens),), device="cuda", generator=g, dtype=torch.int32)
+    labels[:lens[0] // 2] = -1                                         # (the first client's prompt)
+
+    def tune():
+        losses, dY = head.cross_entropy(step.forward(X, None, stream), labels, stream=stream)
+        step.backward(X, dY, stream=stream)
+        return losses
+    timed("fine-tuning step through norm, projection and losses", tune)
+    print("losses", ["%.3f" % x for x in tune().tolist()])
     sb.symb_destroy(h)
 
 

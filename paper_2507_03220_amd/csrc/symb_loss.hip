@@ -74,7 +74,8 @@ LossPlan plan_loss(const symb_loss_batch* b, int32_t entries, bool gradient) {
     const int64_t T = b->seg_offsets[b->num_segments], listed = T * entries;
     const int rows = (int)((T + 255) / 256 * 256);
     plan.pitch = (b->vocab + 63) / 64 * 64;
-    const int64_t row_bytes = gradient ? (int64_t)plan.pitch * 2 : ((int64_t)(b->vocab + 255) / 256) * 4 * (int64_t)sizeof(float2);
+    // (a row's weights, or, of a small vocabulary, its fp32 product)
+    const int64_t row_bytes = gradient ? std::max<int64_t>(plan.pitch * 2, (b->width + 255) / 256 * 1024) : ((int64_t)(b->vocab + 255) / 256) * 4 * (int64_t)sizeof(float2);
     const int most = (int)std::min<int64_t>(rows, std::max<int64_t>((gradient ? kHeldBytes : kStatBytes) / row_bytes / 256 * 256, 256));
     // of the chunks that fit, the one whose whole chunks take least in all
     int n8 = 1, n4 = 1;

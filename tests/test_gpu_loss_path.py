@@ -1,0 +1,245 @@
+"""The losses as they are used: behind each client's last norm and before the backward pass (paper_2507_03220_amd/head.py), on several streams, in graphs, on several handles, in place, and over
+more rows than a call's workspace holds at once."""
+import numpy as np
+import pytest
+import torch
+
+import gpu_harness as gh
+from block_harness import bf16, close, host, offsets, stream
+from loss_harness import NAN, Case
+from oracle import block as ob
+from oracle import loss as ol
+from paper_2507_03220_amd import binding as sb
+from paper_2507_03220_amd import block as blk
+from paper_2507_03220_amd import head as hd
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("teacher", [False, True])
+def test_a_fine_tuning_step_from_the_losses_back(teacher):
+    """Norm and projection, last norm, losses, and back: every step against its own definition on what it was given, with the bounds of the step's own tests."""
+    rng = np.random.default_rng(1)
+    width, mid, vocab, lens = 128, 256, 1000, [70, 3, 0, 129]
+    off, T = offsets(lens), 202
+    W, V, X = bf16(rng, mid, width, std=width ** -0.5), bf16(rng, vocab, mid, std=2 * mid ** -0.5), bf16(rng, T, width)
+    first = [sb.Norm(bf16(rng, width, std=0.1, mean=1.0), None, torch.empty(width, device="cuda")) for _ in lens]
+    last = [sb.Norm(bf16(rng, mid, std=0.1, mean=1.0), None, torch.full((mid,), NAN, device="cuda")) for _ in lens]
+    ads = [sb.Adapter(sb.SYMB_ADAPTER_LORA, 8, 1.5, bf16(rng, 8, width, std=width ** -0.5), bf16(rng, mid, 8, std=0.3), torch.empty(8, width, device="cuda"), torch.empty(mid, 8, device="cuda"))
+           for _ in lens]
+    scales, temps = [1.0, 0.5, 2.0, 1.5], [1.0, 2.0, 1.0, 1.5]
+    step = blk.NormedProjection(gh.handle(), W, lens, first, ads, sb.SYMB_NORM_RMS, 1e-6)
+    head = hd.LossHead(gh.handle(), V, lens, last, [sb.Loss(a, t) for a, t in zip(scales, temps)], cap=10.0)
+    Y = step.forward(X, None, stream())
+    if teacher:
+        ids, logits = rng.integers(-1, vocab, (T, 7)).astype(np.int32), rng.standard_normal((T, 7)).astype(np.float32)
+        given = torch.from_numpy(ids).cuda(), torch.from_numpy(logits).cuda()
+        run = lambda **kw: head.distillation(Y, *given, stream=stream(), **kw)  # noqa: E731
+        want = lambda N: ol.distillation(off, N, host(V), ids, logits, scales, temps, True, 10.0)  # noqa: E731
+    else:
+        labels = rng.integers(0, vocab, T).astype(np.int32)
+        labels[:30] = -1
+        given = torch.from_numpy(labels).cuda()
+        run = lambda **kw: head.cross_entropy(Y, given, stream=stream(), **kw)  # noqa: E731
+        want = lambda N: ol.cross_entropy(off, N, host(V), labels, scales, True, 10.0)  # noqa: E731
+    loss, dY = run()
+    step.backward(X, dY, stream=stream())
+    torch.cuda.synchronize()
+    w = [host(n.weight) for n in last]
+    N = ob.norm_fwd(off, host(Y), w, [None] * 4, False, 1e-6, 0.0)
+    close(head.N, N, 1.01 * 2.0 ** -8 * np.abs(N) + 2e-5, "normed rows")
+    want_loss, want_rows, dN, mass, both = want(host(head.N))
+    # scores of 256 products, capped: 2^-14 of their magnitudes (2 * 256 * 2^-24 of up to 64 or so), and the exponents' 2^-20
+    e = 2 * mid * 2.0 ** -24 * 64 + 2.0 ** -18
+    np.testing.assert_allclose(host(head.row_loss), want_rows, rtol=2.0 ** -20, atol=8 * e)
+    np.testing.assert_allclose(host(loss), want_loss, rtol=2.0 ** -20, atol=8 * e)
+    # the losses' gradient went in place through the norm's backward pass: that pass of what the losses' gradient may have been
+    dX, dw, _ = ob.norm_bwd(off, host(Y), dN, w, False, 1e-6, 0.0)
+    off_by = 1.02 * 2.0 ** -8 * (np.abs(dN) + mass) + 2.2 * e * both
+    rstd = 1 / np.sqrt((host(Y) ** 2).mean(1, keepdims=True) + 1e-6)
+    weight = np.concatenate([np.tile(np.abs(w[i]), (n, 1)) for i, n in enumerate(lens)])
+    z = np.abs(host(Y)) * rstd
+    # dx = r (g - z mean(g z)), g = dy w: each term of dy's error at its largest
+    room = rstd * (off_by * weight + z * (off_by * weight * z).mean(1, keepdims=True))
+    close(dY, dX, room + 1.02 * 2.0 ** -8 * np.abs(dX) + 1e-5, "gradient of the rows")
+    for i, n in enumerate(last):
+        rows = slice(off[i], off[i + 1])
+        close(n.dweight, dw[i], (off_by * z)[rows].sum(0) + 1e-5, f"norm gradient of client {i}")
+    # again on another stream, adding up
+    before = [n.dweight.clone() for n in last]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = head.cross_entropy(Y, given, flags=sb.SYMB_GRAD_ACCUMULATE, stream=side.cuda_stream) if not teacher else \
+            head.distillation(Y, *given, flags=sb.SYMB_GRAD_ACCUMULATE, stream=side.cuda_stream)
+    side.synchronize()
+    assert torch.equal(again[0], loss) and torch.equal(again[1], dY)
+    for n, b in zip(last, before):
+        np.testing.assert_allclose(host(n.dweight), 2 * host(b), rtol=1e-6, atol=1e-7)
+    only, none = run(gradient=False)
+    torch.cuda.synchronize()
+    assert none is None
+    np.testing.assert_allclose(host(only), host(again[0]), rtol=2.0 ** -20)
+
+
+def _call(h, c, batch, X, given, loss, row, dX, ws, st):
+    (sb.symb_distillation if c.K else sb.symb_cross_entropy)(h, batch, X, c.W, *given, loss, row, dX, ws, st)
+
+
+def test_in_a_graph():
+    """Captured with other work, replayed on new inputs with eager calls between; the last replay on labels of which none takes part."""
+    h = sb.symb_create(0)                                  # (captured calls want a handle of their own)
+    cases = [Case(31, [40, 300], 128, 900, prompt=0.2), Case(32, [9], 64, 400, 5)]
+    outs = []
+    for c in cases:
+        batch, given = c.batch(), c.taught()
+        ws = torch.empty(sb.symb_loss_workspace_bytes(batch, c.K), device="cuda", dtype=torch.uint8)
+        X = c.X.clone()
+        outs.append((c, batch, given, ws, X, torch.empty(c.S, device="cuda"), torch.empty(c.T, device="cuda"), torch.empty_like(X)))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for c, batch, given, ws, X, loss, row, dX in outs:
+            _call(h, c, batch, X, given, loss, row, dX, ws, side.cuda_stream)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        for c, batch, given, ws, X, loss, row, dX in outs:
+            _call(h, c, batch, X, given, loss, row, dX, ws, torch.cuda.current_stream().cuda_stream)
+    for turn in range(4):
+        want = []
+        for c, batch, given, ws, X, loss, row, dX in outs:
+            X.copy_(c.X.roll(turn, 1))
+            if turn == 3:
+                given[0].fill_(-1)
+            elif turn and c.K == 0:                        # other rows take part
+                given[0].copy_(given[0].roll(1))
+                X.nan_to_num_(0.5)
+            for t in (loss, row, dX):
+                t.fill_(NAN)
+            mine = [torch.empty_like(t) for t in (loss, row, dX)]
+            _call(gh.handle(), c, batch, X, given, *mine, torch.empty_like(ws), stream())
+            want.append(mine)
+        graph.replay()
+        torch.cuda.synchronize()
+        for (c, _, _, _, _, *got), mine in zip(outs, want):
+            assert all(torch.equal(a, b) for a, b in zip(got, mine)), turn
+            assert not torch.isnan(got[2]).any()
+            assert turn != 3 or not (got[0].any() or got[1].any() or got[2].any())
+    del graph
+    sb.symb_destroy(h)
+
+
+def test_two_at_once():
+    """On two streams with workspaces of their own; each gets the bits that it has alone."""
+    cases = [Case(33, [500], 256, 8000), Case(34, [300, 200], 192, 5000, 12)]
+    alone = [c.run() for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    outs = []
+    for c in cases:
+        batch = c.batch()
+        outs.append((c, batch, c.taught(), torch.empty(c.S, device="cuda"), torch.empty(c.T, device="cuda"), torch.empty_like(c.X),
+                     torch.empty(sb.symb_loss_workspace_bytes(batch, c.K), device="cuda", dtype=torch.uint8)))
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for s, (c, batch, given, loss, row, dX, ws) in zip(streams, outs):
+            _call(gh.handle(), c, batch, c.X, given, loss, row, dX, ws, s.cuda_stream)
+    torch.cuda.synchronize()
+    for got, want in zip(outs, alone):
+        assert all(torch.equal(a, b) for a, b in zip(got[3:6], want))
+
+
+def _reference(c):
+    """Losses of the rows and the gradient in 64 bits on the GPU, some rows at a time."""
+    W, T = c.W.double(), torch.tensor(c.temperatures, device="cuda", dtype=torch.float64).repeat_interleave(torch.tensor(c.lens, device="cuda"))
+    n = [max(int((~c.out[a:b]).sum()), 1) if c.mean else 1 for a, b in zip(c.off[:-1], c.off[1:])]
+    gain = torch.tensor([s / k for s, k in zip(c.scales, n)], device="cuda", dtype=torch.float64).repeat_interleave(torch.tensor(c.lens, device="cuda"))
+    row, dX = torch.zeros(c.T, device="cuda", dtype=torch.float64), torch.zeros(c.T, c.width, device="cuda", dtype=torch.float64)
+    given = c.taught()
+    for part in torch.arange(c.T, device="cuda")[torch.from_numpy(~c.out).cuda()].split(2048):
+        z = c.X[part].double() @ W.t().contiguous()
+        slope = 1.0
+        if c.cap:
+            z = torch.tanh(z / c.cap)
+            slope = 1 - z * z
+            z = z * c.cap
+        if c.K:
+            z /= T[part, None]
+            there = given[0][part] >= 0
+            q = torch.softmax((given[1][part].double() / T[part, None]).masked_fill(~there, -float("inf")), 1)
+            at, t = given[0][part].long().clamp(min=0), T[part]
+        else:
+            q, at, t = torch.ones(len(part), 1, device="cuda", dtype=torch.float64), given[0][part].long()[:, None], torch.ones(len(part), device="cuda", dtype=torch.float64)
+        logp = torch.log_softmax(z, 1)
+        row[part] = t * t * (q * (torch.where(q > 0, q, 1.0).log() - logp.gather(1, at))).sum(1)
+        dX[part] = ((logp.exp_().scatter_add_(1, at, -q) * slope) @ W) * (t * gain[part])[:, None]
+    return row, dX
+
+
+# more rows than the weights of one chunk have room for; wide and narrow tiles of both products, whole and ragged, with what is left of either inner dimension behind the last whole stage
+@pytest.mark.parametrize("lens,width,vocab,entries,prompt,cap", [
+    ([30000, 9001], 16, 30011, 0, 0.1, 0.0), ([2500, 1, 2595], 64, 256001, 0, 0.0, 5.0), ([5000], 72, 256000, 3, 0.5, 0.0), ([1500, 47], 4104, 9001, 0, 0.0, 5.0), ([2048], 1032, 33000, 5, 0.0, 0.0),
+    ([1100], 2056, 20017, 40, 0.3, 8.0), ([512], 2048, 20011, 0, 0.0, 0.0), ([500, 12], 2048, 20011, 20, 0.0, 5.0), ([4000], 2040, 9000, 0, 0.6, 0.0), ([2000, 1001], 1096, 8129, 9, 0.0, 0.0)])
+def test_many_rows(lens, width, vocab, entries, prompt, cap):
+    c = Case(35 + vocab, lens, width, vocab, entries, prompt=prompt, cap=cap)
+    loss, row, dX = c.run()
+    want_row, want = _reference(c)
+    # the bounds of loss_harness.py in the 2-norm, where roundings of many terms are independent: half a step (2^-8 at most, 2^-9 in the mean square) of the output and of each weight
+    assert ((row.double() - want_row).abs() <= 1e-4 * want_row.abs() + 1e-4).all()
+    # (a label's weight of almost one and the others' sum are the two halves of a row's gradient: each off by 2^-9 of itself)
+    err = (dX.double() - want).norm(dim=1) / want.norm(dim=1).clamp(min=1e-30)
+    assert float(err.max()) < 2.0 ** -7, float(err.max())
+    assert float((dX.double() - want).norm() / want.norm()) < 2.0 ** -8
+    n = [max(int((~c.out[a:b]).sum()), 1) for a, b in zip(c.off[:-1], c.off[1:])]
+    np.testing.assert_allclose(host(loss), [float(want_row[a:b].sum()) / k for a, b, k in zip(c.off[:-1], c.off[1:], n)], rtol=1e-4)
+    assert not dX[torch.from_numpy(c.out).cuda()].any()
+
+
+@pytest.mark.parametrize("entries", [0, 6])
+def test_against_differences(entries):
+    """A step along the sign of a row's gradient changes its loss as the gradient says."""
+    c = Case(40, [50], 128, 700, entries, mean=False, temperatures=[1.5], cap=6.0)
+    c.scales = [1.0]
+    _, _, dX = c.run()
+    X, e = c.X, c.score_error()
+    up, down = ((X.float() + s * 2.0 ** -5 * torch.sign(dX.float())).to(torch.bfloat16) for s in (1, -1))
+    a, b = c.run(X=up, gradient=False)[1], c.run(X=down, gradient=False)[1]
+    moved = host(up) - host(down)
+    ends = []
+    for c.X in (up, down):
+        ends.append(c.want()[1])
+    c.X = X
+    want, mass, both = c.want()[2:]
+    # what is behind the first order, in 64 bits; the gradient's own roundings along the step; the losses' at both ends
+    behind = np.abs(ends[0] - ends[1] - (moved * want).sum(1))
+    assert (behind < 0.2 * np.abs(ends[0] - ends[1])).mean() > 0.9
+    grad = (np.abs(moved) * (1.02 * 2.0 ** -8 * (np.abs(want) + mass) + 2.2 * e[:, None] * both)).sum(1)
+    T = 1.5 if entries else 1.0
+    rows = 2 * T * T * (1.1 * e + 2.0 ** -20 * (1 + np.abs(c.want_log())))
+    close(host(a - b), (moved * host(dX)).sum(1), behind + grad + rows, "differences")
+
+
+def test_calls_that_are_refused():
+    c = Case(41, [5], 64, 100)
+    batch, given, ws = c.batch(), c.taught(), torch.empty(sb.symb_loss_workspace_bytes(c.batch()), device="cuda", dtype=torch.uint8)
+    loss, row, dX = torch.full((1,), 7.0, device="cuda"), torch.full((5,), 7.0, device="cuda"), torch.full((5, 64), 7.0, device="cuda", dtype=torch.bfloat16)
+    lib, h, p = sb.lib(), gh.handle(), lambda t: t.data_ptr()
+    good = [h, batch.ref(), p(c.X), p(c.W), p(given[0]), p(loss), p(row), p(dX), p(ws), ws.numel(), None]
+
+    def status(**change):
+        a = list(good)
+        for k, v in change.items():
+            a[int(k[1:])] = v
+        return lib.symb_cross_entropy(*a)
+    for change in ({"_2": None}, {"_3": None}, {"_4": None}, {"_2": p(c.X) + 2}, {"_3": p(c.W) + 8}, {"_4": p(given[0]) + 2}, {"_5": p(loss) + 1}, {"_6": p(row) + 2}, {"_7": p(dX) + 4},
+                   {"_8": p(ws) + 8}, {"_5": None, "_6": None, "_7": None}, {"_1": None}):
+        assert status(**change) == sb.SYMB_ERR_INVALID_ARG, change
+    assert status(_8=None) == status(_9=ws.numel() - 1) == sb.SYMB_ERR_WORKSPACE_TOO_SMALL
+    ids, logits = torch.zeros(5, 2, device="cuda", dtype=torch.int32), torch.zeros(5, 2, device="cuda")
+    for entries, i, l, want in ((0, ids, logits, sb.SYMB_ERR_INVALID_ARG), (-1, ids, logits, sb.SYMB_ERR_INVALID_ARG), (2, None, logits, sb.SYMB_ERR_INVALID_ARG),
+                                (2, ids, None, sb.SYMB_ERR_INVALID_ARG), (sb.SYMB_LOSS_MAX_ENTRIES + 1, ids, logits, sb.SYMB_ERR_UNSUPPORTED)):
+        a = [h, batch.ref(), p(c.X), p(c.W), None if i is None else p(i), None if l is None else p(l), entries, p(loss), p(row), p(dX), p(ws), ws.numel(), None]
+        assert lib.symb_distillation(*a) == want
+    torch.cuda.synchronize()
+    assert (loss == 7).all() and (row == 7).all() and (dX == 7).all()           # nothing ran
+    assert status() == sb.SYMB_OK
