@@ -554,6 +554,172 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_scores_kernel(const LossParams
     }
 }
 
+// The same for batches of up to 32 rows, where W's way from memory is all that counts.  A workgroup of eight wavefronts takes 64 columns: each wavefront every eighth 64 of the inner dimension, both operands
+// from global memory straight into the matrix instruction's registers, the next 64 on their way meanwhile (up to 160 KiB a CU; the tiles of 128 columns have 32); the eight sums meet in LDS.
+// RB: blocks of 16 rows.  One row of 4096 over 32000, W from HBM: 62 us the call, 74 with tiles, where 262 MB take 53 at the rate of a copy.
+constexpr int kFewCols = 64, kFewRows = 32, kFewWaves = 8;
+template <int RB, bool GRAD, bool TEACHER>
+SYMB_KERNEL __launch_bounds__(64 * kFewWaves, RB == 1 ? 4 : 2) void symb_loss_few_kernel(const LossParams p) {
+    constexpr int CB = kFewCols / 16, HALF = kFewWaves / 2;
+    __shared__ floatx4 sums[HALF][RB * CB][64];
+    __shared__ float part[2][16 * RB][CB];                // of 16 columns: sum of weights, largest exponent
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l15 = lane & 15, lg = lane >> 4;
+    const int rows = loss_chunk_rows(p), n0 = blockIdx.x * kFewCols;
+    if (rows <= 0) return;
+    const int32_t* const list = p.rows + p.chunk0;
+    int t[RB];
+    const bf16 *x[RB], *w[CB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        t[r] = list[min(16 * r + l15, rows - 1)];
+        x[r] = p.X + (size_t)t[r] * p.width + 16 * lg;
+    }
+#pragma unroll
+    for (int c = 0; c < CB; ++c) w[c] = p.W + (size_t)min(n0 + 16 * c + l15, p.V - 1) * p.width + 16 * lg;
+    // lane group g holds elements 16 g .. 16 g + 15 of 64, eight for each of two instructions
+    struct Frags {
+        bf16x8 x[RB][2], w[CB][2];
+    };
+    auto load = [&](Frags& f, int k) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) f.w[c][s] = *(const bf16x8*)(w[c] + k + 8 * s);
+#pragma unroll
+        for (int r = 0; r < RB; ++r)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) f.x[r][s] = *(const bf16x8*)(x[r] + k + 8 * s);
+    };
+    floatx4 acc[RB][CB] = {};
+    auto products = [&](const Frags& f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+#pragma unroll
+                for (int c = 0; c < CB; ++c) acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.w[c][s], f.x[r][s], acc[r][c], 0, 0, 0);
+    };
+    const int whole = p.width / 64;
+    Frags f, g;
+    if (wave < whole) load(f, 64 * wave);
+    for (int k = wave; k < whole; k += 2 * kFewWaves) {   // (behind the last 64 the last 64 again, not used)
+        load(g, 64 * min(k + kFewWaves, whole - 1));
+        __builtin_amdgcn_sched_barrier(0);
+        products(f);
+        if (k + kFewWaves >= whole) break;
+        load(f, 64 * min(k + 2 * kFewWaves, whole - 1));
+        __builtin_amdgcn_sched_barrier(0);
+        products(g);
+    }
+    if (p.width % 64 && wave == whole % kFewWaves) {      // what is left of the inner dimension
+        auto at = [&](const bf16* row, int s) __attribute__((always_inline)) {
+            const int k = 64 * whole + 8 * s, last = p.width - 8 - 16 * lg;
+            const bf16x8 v = *(const bf16x8*)(row + min(k, last));
+            return k <= last ? v : bf16x8{};
+        };
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int c = 0; c < CB; ++c) f.w[c][s] = at(w[c], s);
+#pragma unroll
+            for (int r = 0; r < RB; ++r) f.x[r][s] = at(x[r], s);
+        }
+        products(f);
+    }
+    // sums of all wavefronts: the upper ones to the lower ones, and those to whoever takes the block
+    if (wave >= HALF)
+#pragma unroll
+        for (int q = 0; q < RB * CB; ++q) sums[wave - HALF][q][lane] = acc[q / CB][q % CB];
+    __syncthreads();
+    if (wave < HALF)
+#pragma unroll
+        for (int q = 0; q < RB * CB; ++q) {
+            acc[q / CB][q % CB] += sums[wave][q][lane];
+            sums[wave][q][lane] = acc[q / CB][q % CB];
+        }
+    __syncthreads();
+    constexpr int MINE = (RB * CB + kFewWaves - 1) / kFewWaves;
+    float v[MINE][4], slope[MINE][4];
+    // a lane has row 16 r + l15, columns 16 c + 4 lg .. + 3 of its blocks
+    auto block = [&](int k, auto f) __attribute__((always_inline)) {
+        const int q = wave * MINE + k, r = q / CB, c = q % CB;
+        if (q < RB * CB && 16 * r < rows) f(r, c, q, 16 * r + l15, n0 + 16 * c + 4 * lg);
+    };
+    auto row_of = [&](int r) __attribute__((always_inline)) { return list[min(16 * r + l15, rows - 1)]; };
+    auto weights = [&](int k, int q, int row, int col, int label, float shift) __attribute__((always_inline)) {
+        float sum = 0.f, most = -__builtin_inff();
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool in = col + e < p.V;
+            if (in) most = fmaxf(most, v[k][e]);
+            const float u = in ? __builtin_amdgcn_exp2f(v[k][e] - shift) : 0.f;
+            sum += col + e == label ? 0.f : u;
+        }
+        sum = across_rows(sum, Add());
+        most = across_rows(most, Max());
+        if (lg == 0) part[0][row][q % CB] = sum, part[1][row][q % CB] = most;
+    };
+#pragma unroll
+    for (int k = 0; k < MINE; ++k)
+        block(k, [&](int r, int c, int q, int row, int col) __attribute__((always_inline)) {
+            const int t = row_of(r);
+            const LossRow info = p.info[t];
+            floatx4 s = sums[0][q][lane];
+#pragma unroll
+            for (int h = 1; h < HALF; ++h) s += sums[h][q][lane];
+            if constexpr (TEACHER) {
+                const uint16_t* const start = p.starts + (int64_t)t * ((p.V + kFewCols - 1) / kFewCols + 1) + blockIdx.x;
+                const int64_t at = (int64_t)t * p.K;
+                for (int j = start[0], end = row < rows ? start[1] : 0; j < end; ++j) {
+                    const int i = p.sorted[at + j] - col;
+                    if ((unsigned)i < 4u) p.scores[at + j] = i & 2 ? (i & 1 ? s[3] : s[2]) : (i & 1 ? s[1] : s[0]);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                slope[k][e] = 1.f;
+                v[k][e] = fmaf(p.cap > 0.f ? loss_capped(s[e], p.cap, p.to_cap, slope[k][e]) : s[e], info.a, -info.b);
+            }
+            weights(k, q, row, col, TEACHER ? -1 : p.flags[t], 0.f);
+        });
+    __syncthreads();
+    // scores far above a row's own entries (or NaN): smaller units, as in the tiles
+    auto total = [&](int row) __attribute__((always_inline)) {
+        float s = 0.f;
+#pragma unroll
+        for (int c = 0; c < CB; ++c) s += part[0][row][c];
+        return s;
+    };
+    float shift[MINE] = {};
+    bool far = false;
+#pragma unroll
+    for (int k = 0; k < MINE; ++k)
+        block(k, [&](int, int, int, int row, int) __attribute__((always_inline)) {
+            if (total(row) < 0x1p64f) return;
+            far = true;
+            shift[k] = part[1][row][0];
+#pragma unroll
+            for (int c = 1; c < CB; ++c) shift[k] = fmaxf(shift[k], part[1][row][c]);
+        });
+    if (__syncthreads_or(far)) {
+#pragma unroll
+        for (int k = 0; k < MINE; ++k)
+            block(k, [&](int r, int, int q, int row, int col) __attribute__((always_inline)) { weights(k, q, row, col, TEACHER ? -1 : p.flags[row_of(r)], shift[k]); });
+        __syncthreads();
+    }
+#pragma unroll
+    for (int k = 0; k < MINE; ++k)
+        block(k, [&](int, int c, int, int row, int col) __attribute__((always_inline)) {
+            if (row >= rows) return;
+            if (c == 0 && lg == 0) p.stats[(size_t)blockIdx.x * p.chunk + row] = make_float2(shift[k], total(row));
+            if (!GRAD || col >= p.pitch) return;
+            float u[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[e] = col + e < p.V ? __builtin_amdgcn_exp2f(v[k][e] - shift[k]) * slope[k][e] : 0.f;
+            *reinterpret_cast<uint2*>(p.held + (size_t)row * p.pitch + col) = make_uint2(pack2_bf16(u[0], u[1]), pack2_bf16(u[2], u[3]));
+        });
+}
+
 // Parts that the second product's inner dimension (the vocabulary) is cut into: as few rounds of workgroups as possible, weighed against the partial tiles' way through memory.
 template <int BLK>
 struct LossGrad {

@@ -42,7 +42,8 @@ symb_status check_loss(symb_handle h, const symb_loss_batch* b, int32_t entries)
 
 // A call's chunks of rows, tiles, and the places of its workspace.
 struct LossPlan {
-    int chunk = 0, score_blk = 8, grad_blk = 8, pitch = 0, column_parts = 0;
+    int chunk = 0, score_blk = 8, grad_blk = 8, pitch = 0, tile_cols = 0, column_parts = 0;
+    int few = 0;                          // blocks of 16 rows of a batch that the kernel for few rows takes
     int64_t part_tiles = 0;
     bool many_parts = false;              // the second product's tiles come in many parts
     size_t rows = 0, flags = 0, count = 0, gain = 0, info = 0, slopes = 0, sorted = 0, shares = 0, scores = 0, starts = 0, row_loss = 0, stats = 0, row_gain = 0, held = 0, parts = 0, bytes = 0;
@@ -96,7 +97,12 @@ LossPlan plan_loss(const symb_loss_batch* b, int32_t entries, bool gradient) {
         plan.many_parts = (plan.grad_blk == 8 ? n8 : n4) >= 8;
         plan.part_tiles = std::max<int64_t>(tiles_of(first, b->width, edge) * (plan.grad_blk == 8 ? n8 : n4), std::min<int64_t>(512, tiles_of(1, b->width, edge) * std::max(b->vocab / 256, 1)));
     }
-    plan.column_parts = (b->vocab + 32 * plan.score_blk - 1) / (32 * plan.score_blk) * 2;
+    // The kernel for few rows: where rows are long or the tiles of 128 columns few.  Both sides, with W from HBM: 16 rows of 4096 over 32000 65 us with it, 75 with tiles; 32 rows 74, 76; of 6144 over
+    // 49152 134, 142 and 149, 144; of 1024 over 50257 16 rows 45, 36; of 4096 over 12000 37, 65 and, 32 rows, 41, 66; of 768 over 4000 19, 20 and 23, 23.
+    if (T <= kFewRows && (b->width >= 2048 || b->vocab <= 16384)) plan.few = T <= 16 ? 1 : 2;
+    plan.tile_cols = plan.few ? kFewCols : 32 * plan.score_blk;
+    const int column_tiles = (b->vocab + plan.tile_cols - 1) / plan.tile_cols;
+    plan.column_parts = column_tiles * (plan.few ? 1 : 2);
     size_t at = 0;
     auto take = [&](size_t n) {
         const size_t o = at;
@@ -112,7 +118,7 @@ LossPlan plan_loss(const symb_loss_batch* b, int32_t entries, bool gradient) {
     plan.sorted = take(listed * sizeof(int32_t));
     plan.shares = take(listed * sizeof(float));
     plan.scores = take(listed * sizeof(float));
-    plan.starts = take(entries ? T * (plan.column_parts / 2 + 1) * sizeof(uint16_t) : 0);
+    plan.starts = take(entries ? T * (column_tiles + 1) * sizeof(uint16_t) : 0);
     plan.row_loss = take(T * sizeof(float));
     plan.stats = take((size_t)plan.column_parts * plan.chunk * sizeof(float2));
     plan.row_gain = take(gradient ? plan.chunk * sizeof(float) : 0);
@@ -144,6 +150,16 @@ symb_status launch_scores(symb_handle h, const LossParams& p, int rows, hipStrea
     };
     auto by_cap = [&](auto grad) { return p.cap > 0.f ? by_teacher(grad, std::true_type{}) : by_teacher(grad, std::false_type{}); };
     return p.dX ? by_cap(std::true_type{}) : by_cap(std::false_type{});
+}
+template <int RB>
+symb_status launch_few(symb_handle h, const LossParams& p, hipStream_t s) {
+    auto run = [&](auto grad, auto teacher) {
+        hipLaunchKernelGGL((symb_loss_few_kernel<RB, decltype(grad)::value, decltype(teacher)::value>), dim3((p.V + kFewCols - 1) / kFewCols), dim3(64 * kFewWaves), 0, s, p);
+    };
+    if (p.dX) p.ids ? run(std::true_type{}, std::true_type{}) : run(std::true_type{}, std::false_type{});
+    else p.ids ? run(std::false_type{}, std::true_type{}) : run(std::false_type{}, std::false_type{});
+    SYMB_HIP(h, hipGetLastError());
+    return SYMB_OK;
 }
 template <int BLK>
 symb_status launch_grad(symb_handle h, const LossParams& p, int rows, bool many_parts, bool segments, hipStream_t s) {
@@ -213,7 +229,7 @@ symb_status run_loss(symb_handle h, const symb_loss_batch* b, const void* X, con
     p.pitch = plan.pitch;
     p.width = b->width;
     p.K = entries;
-    p.tile_cols = 32 * plan.score_blk;
+    p.tile_cols = plan.tile_cols;
     p.chunk = plan.chunk;
     p.group_m = 8;
     p.grad_blk = plan.grad_blk;
@@ -234,8 +250,10 @@ symb_status run_loss(symb_handle h, const symb_loss_batch* b, const void* X, con
     for (int64_t at = 0; at < T; at += plan.chunk) {
         p.chunk0 = (int32_t)at;
         const int rows = (int)std::min<int64_t>(T - at, plan.chunk);
-        if ((st = plan.score_blk == 8 ? launch_scores<8>(h, p, rows, s) : launch_scores<4>(h, p, rows, s)) != SYMB_OK) return st;
-        hipLaunchKernelGGL(symb_loss_join_kernel, dim3((rows + kJoinRows - 1) / kJoinRows), dim3(kJoinRows * kJoinSets), 0, s, p, plan.column_parts, 16 * plan.score_blk, finish);
+        if (plan.few) st = plan.few == 1 ? launch_few<1>(h, p, s) : launch_few<2>(h, p, s);
+        else st = plan.score_blk == 8 ? launch_scores<8>(h, p, rows, s) : launch_scores<4>(h, p, rows, s);
+        if (st != SYMB_OK) return st;
+        hipLaunchKernelGGL(symb_loss_join_kernel, dim3((rows + kJoinRows - 1) / kJoinRows), dim3(kJoinRows * kJoinSets), 0, s, p, plan.column_parts, plan.few ? kFewCols : plan.tile_cols / 2, finish);
         SYMB_HIP(h, hipGetLastError());
         const bool segments = loss && !finish && at + rows == T;
         if (dX && (st = plan.grad_blk == 8 ? launch_grad<8>(h, p, rows, plan.many_parts, segments, s) : launch_grad<4>(h, p, rows, plan.many_parts, segments, s)) != SYMB_OK) return st;

@@ -12,7 +12,8 @@ from paper_2507_03220_amd import binding as sb
 pytestmark = pytest.mark.gpu
 
 SIZES = [([1], 8, 1), ([1], 8, 2), ([3], 64, 63), ([1, 0, 2], 72, 64), ([5], 56, 65), ([17], 128, 255), ([40, 3], 264, 257), ([128], 192, 1000), ([129, 0, 0, 31], 768, 1025), ([1], 4096, 3001),
-         ([255, 2, 300], 136, 2047), ([700], 512, 513), ([33] * 20, 320, 5003), ([2], 1032, 40001), ([600], 64, 30011)]
+         ([255, 2, 300], 136, 2047), ([700], 512, 513), ([33] * 20, 320, 5003), ([2], 1032, 40001), ([600], 64, 30011), ([16], 2048, 17000), ([9, 8], 2056, 17001), ([0, 32], 4160, 129),
+         ([30], 2104, 16385), ([33], 2048, 300)]
 
 
 @pytest.mark.parametrize("lens,width,vocab", SIZES)
@@ -34,21 +35,23 @@ def test_scores_of_any_size(std):
     Case(5, [70, 200], 256, 3000, std=std, sure=0.0).check(f"scores of {std}")
     Case(6, [70, 200], 256, 3000, std=std, sure=1.0).check(f"scores of {std}, sure rows")
     Case(7, [70, 200], 256, 3000, 9, std=std, sure=0.5).check(f"entries, scores of {std}")
+    for entries in (0, 5):
+        Case(8, [20], 256, 3000, entries, std=std, sure=0.5).check(f"few rows, scores of {std}")
 
 
 def test_weights_in_different_units():
     """Rows whose label lies far below the scores of some columns and not of others: one column alone, one in every part, in the first and the last."""
     width, vocab = 64, 1500
-    for columns in ([1499], [0], [700, 701], list(range(5, 1500, 64)), [3, 300, 1400]):
-        c = Case(11, [300], width, vocab, std=1.0, sure=0.0)
+    for columns, rows in [(c, n) for c in ([1499], [0], [700, 701], list(range(5, 1500, 64)), [3, 300, 1400]) for n in (300, 30, 12)]:
+        c = Case(11, [rows], width, vocab, std=1.0, sure=0.0)
         w = host(c.W)
         w[:, 0] = 0
         for k, v in enumerate(columns):
             w[v, 0] = 20.0 + k                                 # times x[0]: 0 to 400 above the rest
         x = host(c.X)
-        x[:, 0] = np.arange(300) / 15
+        x[:, 0] = np.arange(rows) * 20 / rows
         c.W, c.X = (torch.from_numpy(t.astype(np.float32)).to(torch.bfloat16).cuda() for t in (w, x))
-        c.check(f"columns {columns[:4]}")
+        c.check(f"columns {columns[:4]}, {rows} rows")
 
 
 def test_sure_rows_keep_their_precision():
