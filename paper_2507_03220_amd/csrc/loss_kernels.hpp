@@ -53,7 +53,7 @@ struct LossParams {
     int64_t part_tiles;                   // room for that many
     int32_t T, S, V, pitch, width, K;
     int32_t chunk0, chunk;                // the chunk's first row (of those that take part) and its length at most
-    int32_t tile_cols;                    // columns of a tile of the first product
+    int32_t tile_shift;                   // columns of a tile of the first product: 2^tile_shift
     int32_t group_m, mean, grad_blk;
     float cap, to_cap;                    // 1 / cap
 };
@@ -120,15 +120,23 @@ __device__ __forceinline__ int loss_count(int v, int* lds) {
     __syncthreads();
     return v;
 }
-// Workgroup `b` lists the rows of 256 that take part (and counts those before them itself); behind the lists, one a segment counts its rows.
+// Workgroup `b` lists the rows of 256 that take part (and counts those before them itself); behind the lists, one a segment counts its rows.  IDS: of what the teachers' ids say, not yet of flags.
+template <bool IDS>
 __device__ __forceinline__ void loss_list(const LossParams& p, int b, int* lds) {
     const int lists = (p.T + 255) / 256;
+    auto takes_part = [&](int t) __attribute__((always_inline)) {
+        if constexpr (!IDS) return p.flags[t] >= 0;
+        int most = -1;
+#pragma unroll 8
+        for (int j = 0; j < p.K; ++j) most = max(most, p.ids[(int64_t)t * p.K + j]);
+        return most >= 0;
+    };
     if (b < lists) {
         int before = 0;
-        for (int t = threadIdx.x; t < b * 256; t += 256) before += p.flags[t] >= 0;
+        for (int t = threadIdx.x; t < b * 256; t += 256) before += takes_part(t);
         before = loss_count(before, lds);
         const int t = b * 256 + threadIdx.x;
-        const bool part = t < p.T && p.flags[t] >= 0;
+        const bool part = t < p.T && takes_part(t);
         const unsigned long long mine = __ballot(part);
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         if (lane == 0) lds[wave] = __popcll(mine);
@@ -141,7 +149,7 @@ __device__ __forceinline__ void loss_list(const LossParams& p, int b, int* lds) 
     }
     const int i = b - lists;
     int n = 0;
-    for (int t = p.off[i] + threadIdx.x; t < p.off[i + 1]; t += 256) n += p.flags[t] >= 0;
+    for (int t = p.off[i] + threadIdx.x; t < p.off[i + 1]; t += 256) n += takes_part(t);
     n = loss_count(n, lds);
     if (threadIdx.x == 0) p.gain[i] = p.mean ? p.losses[i].scale / (float)max(n, 1) : p.losses[i].scale;
 }
@@ -150,7 +158,7 @@ __device__ __forceinline__ void loss_list(const LossParams& p, int b, int* lds) 
 SYMB_KERNEL __launch_bounds__(256) void symb_loss_labels_kernel(LossParams p) {
     __shared__ int lds[4];
     const int lists = (p.T + 255) / 256 + p.S;
-    if ((int)blockIdx.x < lists) return loss_list(p, blockIdx.x, lds);
+    if ((int)blockIdx.x < lists) return loss_list<false>(p, blockIdx.x, lds);
     const int t = (blockIdx.x - lists) * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     if (t >= p.T) return;
     const int label = p.flags[t];
@@ -164,40 +172,45 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_labels_kernel(LossParams p) {
 }
 SYMB_KERNEL __launch_bounds__(256) void symb_loss_rows_kernel(LossParams p) {
     __shared__ int lds[4];
-    loss_list(p, blockIdx.x, lds);
+    loss_list<false>(p, blockIdx.x, lds);
 }
 
-// Teachers: a row's entries in the order of their ids, with their shares, the tiles of the vocabulary that they lie in, and the score of the one with the largest share.  A wavefront a row.
-SYMB_KERNEL __launch_bounds__(256) void symb_loss_teacher_kernel(LossParams p) {
+// Teachers: a row's entries in the order of their ids, with their shares, the tiles of the vocabulary that they lie in, and the score of the one with the largest share.  A wavefront a row, behind
+// the `lists` first workgroups, which list the rows.
+SYMB_KERNEL __launch_bounds__(256) void symb_loss_teacher_kernel(LossParams p, int lists) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), t = blockIdx.x * 4 + wave;
+    if ((int)blockIdx.x < lists) return loss_list<true>(p, blockIdx.x, (int*)smem);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), t = (blockIdx.x - lists) * 4 + wave;
     if (t >= p.T) return;
     const int K = p.K, pad = (K + 63) / 64 * 64;
     int* const list = (int*)smem + wave * 2 * pad;        // ids as they come (absent ones behind all others), then in order
     int* const order = list + pad;
     const int32_t* ids = p.ids + (int64_t)t * K;
     const float* l = p.teacher + (int64_t)t * K;
-    float most = -__builtin_inff();
+    const int seg = seg_of_row(p.off, 0, p.S - 1, t);
+    const float T = p.losses[seg].temperature, to_t = 1.f / T;
+    float most = -__builtin_inff(), first = 0.f;          // (first: this lane's first logit, all that it has of up to 64)
     int n = 0;
     bool outside = false;
     for (int j = lane; j < pad; j += 64) {
         const int id = j < K ? ids[j] : -1;
+        const float v = j < K ? l[j] : 0.f;
         list[j] = id < 0 ? 0x7fffffff : min(id, 0x7ffffffe);
-        if (id >= 0) most = fmaxf(most, l[j]);
+        if (j < 64) first = v;
+        if (id >= 0) most = fmaxf(most, v);
         outside |= id >= p.V;
         n += __popcll(__ballot(id >= 0));
     }
     if (lane == 0) p.own_flags[t] = n ? 0 : -1;
     if (!n) return loss_no_row(p, t);
-    const int seg = seg_of_row(p.off, 0, p.S - 1, t);
-    const float T = p.losses[seg].temperature, to_t = 1.f / T;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
     most = across_wave(most, Max());
+    auto raised = [&](int j) __attribute__((always_inline)) { return expf(((j < 64 ? first : l[j]) - most) * to_t); };
     // (a NaN among the logits makes the sum, and with it all shares, NaN)
     float sum = 0.f, best = -1.f;
-    for (int j = lane; j < K; j += 64) sum += ids[j] >= 0 ? expf((l[j] - most) * to_t) : 0.f;
+    for (int j = lane; j < K; j += 64) sum += list[j] != 0x7fffffff ? raised(j) : 0.f;
     const float to_sum = 1.f / across_wave(sum, Add());
     int best_id = 0x7fffffff;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
     for (int j = lane; j < K; j += 64) {
         const int id = list[j];
         if (id == 0x7fffffff) continue;
@@ -207,7 +220,7 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_teacher_kernel(LossParams p) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) at += o[i] < id || (o[i] == id && k + i < j);
         }
-        const float q = expf((l[j] - most) * to_t) * to_sum;
+        const float q = raised(j) * to_sum;
         order[at] = id;
         p.sorted[(int64_t)t * K + at] = id;
         p.shares[(int64_t)t * K + at] = q;
@@ -227,12 +240,23 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_teacher_kernel(LossParams p) {
     const float a = kLog2e * to_t;
     if (lane == 0) p.info[t] = LossRow{a, s * a, seg, n};
     // starts[c]: entries in the tiles before c
-    const int tiles = (p.V + p.tile_cols - 1) / p.tile_cols;
+    const int tiles = ((p.V - 1) >> p.tile_shift) + 1;
     uint16_t* const starts = p.starts + (int64_t)t * (tiles + 1);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
-    for (int k = lane; k <= n; k += 64) {
-        const int from = k ? min(order[k - 1], p.V - 1) / p.tile_cols + 1 : 0, to = k < n ? min(order[k], p.V - 1) / p.tile_cols : tiles;
-        for (int c = from; c <= to; ++c) starts[c] = (uint16_t)k;
+    for (int k0 = 0; k0 <= n; k0 += 64) {
+        const int k = k0 + lane;
+        int from = 0, to = -1;
+        if (k <= n) {
+            from = k ? (min(order[k - 1], p.V - 1) >> p.tile_shift) + 1 : 0;
+            to = k < n ? min(order[k], p.V - 1) >> p.tile_shift : tiles;
+        }
+        const bool wide = to - from >= 16;                // (the whole wavefront on it)
+        if (!wide)
+            for (int c = from; c <= to; ++c) starts[c] = (uint16_t)k;
+        for (unsigned long long left = __ballot(wide); left; left &= left - 1) {
+            const int of = __ffsll(left) - 1, at = __builtin_amdgcn_readlane(from, of), end = __builtin_amdgcn_readlane(to, of);
+            for (int c = at + lane; c <= end; c += 64) starts[c] = (uint16_t)(k0 + of);
+        }
     }
 }
 

@@ -51,6 +51,8 @@ struct LossPlan {
 // What a call may hold: weights of a chunk of rows, and, where the losses alone are wanted, their sums.
 constexpr int64_t kHeldBytes = (int64_t)2 << 30, kStatBytes = (int64_t)256 << 20;
 
+constexpr int kLossListedRows = 512;
+
 int64_t tiles_of(int64_t rows, int64_t columns, int edge) { return ((rows + edge - 1) / edge) * ((columns + edge - 1) / edge); }
 
 // Microseconds of the product with W of so many rows, in tiles of 32 blk.
@@ -229,7 +231,7 @@ symb_status run_loss(symb_handle h, const symb_loss_batch* b, const void* X, con
     p.pitch = plan.pitch;
     p.width = b->width;
     p.K = entries;
-    p.tile_cols = plan.tile_cols;
+    p.tile_shift = plan.tile_cols == 64 ? 6 : plan.tile_cols == 128 ? 7 : 8;
     p.chunk = plan.chunk;
     p.group_m = 8;
     p.grad_blk = plan.grad_blk;
@@ -238,10 +240,14 @@ symb_status run_loss(symb_handle h, const symb_loss_batch* b, const void* X, con
     p.to_cap = b->cap > 0.f ? 1.f / b->cap : 0.f;
     const unsigned lists = (unsigned)((T + 255) / 256 + S), fours = (unsigned)((T + 3) / 4);
     if (entries && T) {
-        hipLaunchKernelGGL(symb_loss_teacher_kernel, dim3(fours), dim3(256), 4 * 2 * align_up(entries, 64) * sizeof(int32_t), s, p);
+        // (few rows: the same launch lists them, of the ids themselves; every list of 256 reads those of all rows before it)
+        const bool one = T <= kLossListedRows;
+        hipLaunchKernelGGL(symb_loss_teacher_kernel, dim3(fours + (one ? lists : 0)), dim3(256), 4 * 2 * align_up(entries, 64) * sizeof(int32_t), s, p, one ? (int)lists : 0);
         SYMB_HIP(h, hipGetLastError());
-        hipLaunchKernelGGL(symb_loss_rows_kernel, dim3(lists), dim3(256), 0, s, p);
-        SYMB_HIP(h, hipGetLastError());
+        if (!one) {
+            hipLaunchKernelGGL(symb_loss_rows_kernel, dim3(lists), dim3(256), 0, s, p);
+            SYMB_HIP(h, hipGetLastError());
+        }
     } else if (T) {
         hipLaunchKernelGGL(symb_loss_labels_kernel, dim3(lists + fours), dim3(256), 0, s, p);
         SYMB_HIP(h, hipGetLastError());
