@@ -13,10 +13,10 @@
  * A row with a negative label, or without any entry of an id >= 0, takes no part: its loss and its gradient are zeros, and what its x holds is not looked at.  (An entry with a negative id is absent.)
  *   loss_i   mean (SYMB_LOSS_SUM: sum) of L over the segment's rows that take part; 0 if none does
  *   dX       scale_i d loss_i / dx
- * A label or id of V or more is never followed: the row's loss and gradient are NaN, and so are those of a row with NaN, or with infinite scores among its entries; no other row's.  A token that a row names
- * twice counts with the sum of its shares.
- * What is rounded: the weights p_v - q_v enter the gradient's product as bf16, off by 2^-8 of each at most; dX is rounded once.  Scores, sums and losses are fp32; a sure row's loss (p_label near one) keeps its
- * relative precision.  Capping is good to 2^-21 of a score.
+ * A label or id of V or more is never followed: the row's loss and gradient are NaN, and so are those of a row with a score of NaN or infinity, or with a logit of NaN or infinity (-infinity beside
+ * others: a share of zero); no other row's.  A token that a row names twice counts with the sum of its shares.
+ * What is rounded: the weights p_v - q_v enter the gradient's product as bf16, off by 2^-8 of each at most (in batches of up to 64 rows as two bf16 terms, 2^-16); dX is rounded once.  Scores, sums and
+ * losses are fp32, a label's own score is formed in 64 bits: a sure row's loss (p_label near one) keeps its relative precision.  Capping is good to 2^-21 of a score.
  * Deterministic: the same arguments give the same bits.  What else is in the batch can change a row's loss and gradient in the last rounding.
  */
 #ifndef SYMB_LOSS_H

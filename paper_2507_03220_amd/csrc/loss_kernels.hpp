@@ -17,6 +17,8 @@ namespace symb {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+constexpr int kTwoRows = 64;
+
 struct LossDesc {
     float scale, temperature;
 };
@@ -40,7 +42,7 @@ struct LossParams {
     int32_t* count;                       // how many they are
     float* gain;                          // [S] scale, over the segment's rows that take part if the loss is a mean
     LossRow* info;                        // [T]
-    float* slopes;                        // [T] z' of the label
+    float2* label;                        // [T] z' of the label, and its own weight: what rounding b makes of one
     int32_t* sorted;                      // [T][K] a row's ids in their order, absent ones left out,
     float* shares;                        // [T][K] their q,
     float* scores;                        // [T][K] and their s, from the first product
@@ -55,6 +57,7 @@ struct LossParams {
     int32_t chunk0, chunk;                // the chunk's first row (of those that take part) and its length at most
     int32_t tile_shift;                   // columns of a tile of the first product: 2^tile_shift
     int32_t group_m, mean, grad_blk;
+    int32_t two;                          // weights are held in two terms, the second kTwoRows rows below the first
     float cap, to_cap;                    // 1 / cap
 };
 
@@ -70,37 +73,42 @@ __device__ __forceinline__ float loss_capped(float s, float cap, float to_cap, f
     return is_near ? near : far;
 }
 
-// tanh(y) for |y| <= kLossNear: y times a polynomial in y^2, 2^-22 of it at most (the coefficients: least largest relative error, from exchanged extrema).
+// tanh(y) for |y| <= kLossNear: y times a polynomial in y^2, 2^-27 of it at most and what fp32 rounds (the coefficients: least largest relative error, from exchanged extrema).
 constexpr float kLossNear = 1.22f;
 __device__ __forceinline__ float loss_tanh(float y) {
     const float u = y * y;
-    float r = -1.9576128e-4f;
-    r = fmaf(r, u, 1.6539543e-3f);
-    r = fmaf(r, u, -6.9249099e-3f);
-    r = fmaf(r, u, 2.0681336e-2f);
-    r = fmaf(r, u, -5.3551411e-2f);
-    r = fmaf(r, u, 1.3325926e-1f);
-    r = fmaf(r, u, -3.3332821e-1f);
-    r = fmaf(r, u, 0.99999994f);
+    float r = 6.16943486e-05f;
+    r = fmaf(r, u, -0.00056751579f);
+    r = fmaf(r, u, 0.00256464523f);
+    r = fmaf(r, u, -0.00808763789f);
+    r = fmaf(r, u, 0.0215047049f);
+    r = fmaf(r, u, -0.0538685345f);
+    r = fmaf(r, u, 0.133319376f);
+    r = fmaf(r, u, -0.333332569f);
+    r = fmaf(r, u, 1.f);
     return y * r;
 }
 
 // ---- which rows take part, and their own scores -------------------------------------------------------------------------------------
-// s = x . W_id over a wavefront; NaN for a number outside the vocabulary, which is never followed.
-__device__ __forceinline__ float loss_score(const LossParams& p, int t, int id) {
-    if (id >= p.V) return __builtin_nanf("");
+// s = x . W_id over a wavefront, in 64 bits: a sure row's loss hangs on how far this one score lies above the others, whose errors even out.  NaN for a number outside the vocabulary, which is never
+// followed.
+__device__ __forceinline__ double loss_score(const LossParams& p, int t, int id) {
+    if (id >= p.V) return __builtin_nan("");
     const bf16 *x = p.X + (int64_t)t * p.width, *w = p.W + (int64_t)id * p.width;
-    float s[2] = {0.f, 0.f};
+    double s[2] = {0.0, 0.0};
 #pragma unroll 4
     for (int c = threadIdx.x & 63; c < p.width >> 3; c += 64) {
         const intx4 u = *(const intx4*)(x + c * 8), v = *(const intx4*)(w + c * 8);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            s[0] = fmaf(bf16_lo((unsigned)u[i]), bf16_lo((unsigned)v[i]), s[0]);
-            s[1] = fmaf(bf16_hi((unsigned)u[i]), bf16_hi((unsigned)v[i]), s[1]);
+        for (int i = 0; i < 4; ++i) {                     // (a product of two bf16 is a float)
+            s[0] += (double)(bf16_lo((unsigned)u[i]) * bf16_lo((unsigned)v[i]));
+            s[1] += (double)(bf16_hi((unsigned)u[i]) * bf16_hi((unsigned)v[i]));
         }
     }
-    return across_wave(s[0] + s[1], Add());
+    double sum = s[0] + s[1];
+#pragma unroll
+    for (int m = 32; m; m >>= 1) sum += __shfl_xor(sum, m);
+    return sum;
 }
 // A row that takes no part: zeros.
 __device__ __forceinline__ void loss_no_row(const LossParams& p, int t) {
@@ -163,11 +171,17 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_labels_kernel(LossParams p) {
     if (t >= p.T) return;
     const int label = p.flags[t];
     if (label < 0) return loss_no_row(p, t);
-    float s = loss_score(p, t, label), slope = 1.f;
-    if (p.cap > 0.f) s = loss_capped(s, p.cap, p.to_cap, slope);
+    double z = loss_score(p, t, label), slope = 1.0;
+    if (p.cap > 0.f) {
+        const double th = tanh(z / p.cap);
+        z = th * p.cap;
+        slope = 1.0 - th * th;
+    }
+    z *= (double)kLog2e;
     if ((threadIdx.x & 63) == 0) {
-        p.info[t] = LossRow{kLog2e, s * kLog2e, seg_of_row(p.off, 0, p.S - 1, t), 1};
-        p.slopes[t] = slope;
+        const float b = (float)z;
+        p.info[t] = LossRow{kLog2e, b, seg_of_row(p.off, 0, p.S - 1, t), 1};
+        p.label[t] = make_float2((float)slope, exp2f((float)(z - (double)b)));
     }
 }
 SYMB_KERNEL __launch_bounds__(256) void symb_loss_rows_kernel(LossParams p) {
@@ -234,7 +248,7 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_teacher_kernel(LossParams p, i
     outside = __any(outside || mine == 0x7fffffff);       // (all shares NaN: none is the largest)
     float s = __builtin_nanf(""), slope;
     if (!outside) {
-        s = loss_score(p, t, mine);
+        s = (float)loss_score(p, t, mine);
         if (p.cap > 0.f) s = loss_capped(s, p.cap, p.to_cap, slope);
     }
     const float a = kLog2e * to_t;
@@ -258,6 +272,11 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_teacher_kernel(LossParams p, i
             for (int c = at + lane; c <= end; c += 64) starts[c] = (uint16_t)(k0 + of);
         }
     }
+}
+
+// What rounding four weights to bf16 leaves of them, as bf16.
+__device__ __forceinline__ uint2 loss_second(const float (&v)[4], uint2 first) {
+    return make_uint2(pack2_bf16(v[0] - bf16_lo(first.x), v[1] - bf16_hi(first.x)), pack2_bf16(v[2] - bf16_lo(first.y), v[3] - bf16_hi(first.y)));
 }
 
 // ---- products -------------------------------------------------------------------------------------------------------------------------
@@ -561,7 +580,14 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_scores_kernel(const LossParams
                 if constexpr (CAP)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) w[j][e] *= slope[j][e];
-                *reinterpret_cast<uint2*>(smem + c_lane + i * 16 * CP + j * 32) = make_uint2(pack2_bf16(w[j][0], w[j][1]), pack2_bf16(w[j][2], w[j][3]));
+                const uint2 first = make_uint2(pack2_bf16(w[j][0], w[j][1]), pack2_bf16(w[j][2], w[j][3]));
+                // (of up to 64 rows the tile's lower half holds their second terms)
+                if (BLK == 4 && p.two) {
+                    if (wm0 == 0) {
+                        *reinterpret_cast<uint2*>(smem + c_lane + i * 16 * CP + j * 32) = first;
+                        *reinterpret_cast<uint2*>(smem + c_lane + (kTwoRows + i * 16) * CP + j * 32) = loss_second(w[j], first);
+                    }
+                } else *reinterpret_cast<uint2*>(smem + c_lane + i * 16 * CP + j * 32) = first;
             }
         }
     });
@@ -569,11 +595,12 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_scores_kernel(const LossParams
         __syncthreads();
         constexpr int LPR = BN / 8, RPP = 256 / LPR;
         const int col = (lane % LPR) * 8, r0 = wave * (64 / LPR) + lane / LPR;
+        const int held_rows = p.two ? kTwoRows + rows : rows;
         if (n0 + col < p.pitch) {
             bf16* const out = p.held + (size_t)m0 * p.pitch + n0 + col;
 #pragma unroll 8
             for (int r = r0; r < BM; r += RPP)
-                if (m0 + r < rows) *reinterpret_cast<uint4*>(out + (size_t)r * p.pitch) = *reinterpret_cast<const uint4*>(smem + r * CP + col * 2);
+                if (m0 + r < held_rows) *reinterpret_cast<uint4*>(out + (size_t)r * p.pitch) = *reinterpret_cast<const uint4*>(smem + r * CP + col * 2);
         }
     }
 }
@@ -740,7 +767,9 @@ SYMB_KERNEL __launch_bounds__(64 * kFewWaves, RB == 1 ? 4 : 2) void symb_loss_fe
             float u[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) u[e] = col + e < p.V ? __builtin_amdgcn_exp2f(v[k][e] - shift[k]) * slope[k][e] : 0.f;
-            *reinterpret_cast<uint2*>(p.held + (size_t)row * p.pitch + col) = make_uint2(pack2_bf16(u[0], u[1]), pack2_bf16(u[2], u[3]));
+            const uint2 first = make_uint2(pack2_bf16(u[0], u[1]), pack2_bf16(u[2], u[3]));
+            *reinterpret_cast<uint2*>(p.held + (size_t)row * p.pitch + col) = first;
+            *reinterpret_cast<uint2*>(p.held + (size_t)(kTwoRows + row) * p.pitch + col) = loss_second(u, first);
         });
 }
 
@@ -841,13 +870,20 @@ SYMB_KERNEL __launch_bounds__(kJoinRows* kJoinSets) void symb_loss_join_kernel(c
         row_info[r] = info;
         if (!(fabsf(info.b) < __builtin_inff())) gain = l = __builtin_nanf("");          // (infinite scores among its entries)
         if (!p.ids) {
-            p.row_loss[t] = unit == 0.f ? log1pf(l) : unit * kLn2 + logf(l + exp2f(-unit));
-            l += exp2f(-unit);
+            const float mine = p.label[t].y * exp2f(-unit);
+            p.row_loss[t] = unit == 0.f ? log1pf(l / mine) : unit * kLn2 + logf(l + mine) - logf(p.label[t].y);
+            l += mine;
         } else gain *= kLog2e / info.a;
         if (p.dX) p.row_gain[m] = gain / l;
         row_gain[r] = l;
     }
     __syncthreads();
+    const size_t second = (size_t)kTwoRows * p.pitch;
+    auto put = [&](bf16* held, float v) __attribute__((always_inline)) {
+        const bf16 first = (bf16)v;
+        held[0] = first;
+        if (p.two) held[second] = (bf16)(v - (float)first);
+    };
     if (p.dX) {
         // columns that were held in other units than the row's
         for (int k = 0; k < kJoinRows && m0 + k < rows; ++k) {
@@ -856,13 +892,13 @@ SYMB_KERNEL __launch_bounds__(kJoinRows* kJoinSets) void symb_loss_join_kernel(c
             bf16* const held = p.held + (size_t)(m0 + k) * p.pitch;
             for (int c = threadIdx.x; c < p.pitch; c += kJoinRows * kJoinSets) {
                 const float shift = c < p.V ? p.stats[(size_t)(c / cols) * p.chunk + m0 + k].x : unit;
-                if (shift != unit) held[c] = (bf16)((float)held[c] * exp2f(shift - unit));
+                if (shift != unit) put(held + c, ((float)held[c] + (p.two ? (float)held[c + second] : 0.f)) * exp2f(shift - unit));
             }
         }
         __syncthreads();
         if (!p.ids && set == 0 && m < rows) {
             const int id = p.flags[t];
-            if (id < p.V) p.held[(size_t)m * p.pitch + id] = (bf16)(-row_sum[r] * p.slopes[t]);
+            if (id < p.V) put(p.held + (size_t)m * p.pitch + id, -row_sum[r] * p.label[t].x);
         }
     }
     if (p.ids)
@@ -881,7 +917,7 @@ SYMB_KERNEL __launch_bounds__(kJoinRows* kJoinSets) void symb_loss_join_kernel(c
                 if (!(q == 0.f)) base += q * (logf(q) - z * kLn2);
                 if (!p.dX || (j && p.sorted[at + j - 1] == id)) continue;
                 for (int o = j + 1; o < row.entries && p.sorted[at + o] == id; ++o) q += p.shares[at + o];     // (a token that the row names twice)
-                held[id] = (bf16)((exp2f(z - unit) - q * l) * slope);
+                put(held + id, (exp2f(z - unit) - q * l) * slope);
             }
             base = across_wave(base, Add());
             if (lane == 0) p.row_loss[row_t[k]] = T * T * (base + unit * kLn2 + logf(l));
@@ -905,8 +941,8 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_grad_kernel(const LossParams p
     using TT = Gemm16Tile<BLK, BLK>;
     constexpr int BM = TT::BM, BN = TT::BN;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    const int rows = loss_chunk_rows(p);
-    if (rows <= 0) return;
+    const int own = loss_chunk_rows(p), rows = p.two ? kTwoRows + own : own;
+    if (own <= 0) return;
     const int m_tiles = (rows + BM - 1) / BM, n_tiles = (p.width + BN - 1) / BN, tiles = m_tiles * n_tiles;
     const int n = *p.part_count, total = tiles * n, per_xcd = (total + 7) >> 3;
     const int lin = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
@@ -968,6 +1004,9 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_reduce_kernel(const LossParams
     floatx4 s = floatx4{0, 0, 0, 0};
 #pragma unroll 8
     for (int k = MANY ? own : 0; k < n; k += MANY ? 4 : 1) s += *(const floatx4*)(src + (size_t)k * tiles * (BM * BM));
+    if (BLK == 4 && p.two)                                // the second terms' product, kTwoRows rows below: of the wavefront two further on
+#pragma unroll 8
+        for (int k = MANY ? own : 0; k < n; k += MANY ? 4 : 1) s += *(const floatx4*)(src + 2 * BLK * BLK * 256 + (size_t)k * tiles * (BM * BM));
     if constexpr (MANY) {
         lds[own][lane] = s;
         __syncthreads();

@@ -45,8 +45,9 @@ struct LossPlan {
     int chunk = 0, score_blk = 8, grad_blk = 8, pitch = 0, tile_cols = 0, column_parts = 0;
     int few = 0;                          // blocks of 16 rows of a batch that the kernel for few rows takes
     int64_t part_tiles = 0;
+    bool two = false;                     // weights held in two terms
     bool many_parts = false;              // the second product's tiles come in many parts
-    size_t rows = 0, flags = 0, count = 0, gain = 0, info = 0, slopes = 0, sorted = 0, shares = 0, scores = 0, starts = 0, row_loss = 0, stats = 0, row_gain = 0, held = 0, parts = 0, bytes = 0;
+    size_t rows = 0, flags = 0, count = 0, gain = 0, info = 0, label = 0, sorted = 0, shares = 0, scores = 0, starts = 0, row_loss = 0, stats = 0, row_gain = 0, held = 0, parts = 0, bytes = 0;
 };
 // What a call may hold: weights of a chunk of rows, and, where the losses alone are wanted, their sums.
 constexpr int64_t kHeldBytes = (int64_t)2 << 30, kStatBytes = (int64_t)256 << 20;
@@ -92,9 +93,13 @@ LossPlan plan_loss(const symb_loss_batch* b, int32_t entries, bool gradient) {
         if (all < least) least = all, plan.chunk = c;
     }
     const int first = (int)std::min<int64_t>(T, plan.chunk);
-    plan.score_blk = score_us(first, b, 8) < score_us(first, b, 4) ? 8 : 4;
+    plan.score_blk = T > kTwoRows && score_us(first, b, 8) < score_us(first, b, 4) ? 8 : 4;
     if (gradient) {
-        plan.grad_blk = grad_us<8>(first, b, n8) < grad_us<4>(first, b, n4) ? 8 : 4;
+        // A row's few largest weights may be most of its gradient, and where rows are few their roundings do not even out: up to 64 rows (half of a tile of 128, whose other half costs nothing) hold
+        // their weights in two bf16 terms.  One row: off by 1.7e-3 of it, what rounding dX costs, up to 3.7e-3 with one term; 256 rows with one term 2.4e-3.
+        plan.two = T <= kTwoRows;
+        const double us8 = grad_us<8>(first, b, n8), us4 = grad_us<4>(first, b, n4);
+        plan.grad_blk = !plan.two && us8 < us4 ? 8 : 4;
         const int edge = 32 * plan.grad_blk;
         plan.many_parts = (plan.grad_blk == 8 ? n8 : n4) >= 8;
         plan.part_tiles = std::max<int64_t>(tiles_of(first, b->width, edge) * (plan.grad_blk == 8 ? n8 : n4), std::min<int64_t>(512, tiles_of(1, b->width, edge) * std::max(b->vocab / 256, 1)));
@@ -116,7 +121,7 @@ LossPlan plan_loss(const symb_loss_batch* b, int32_t entries, bool gradient) {
     plan.count = take(2 * sizeof(int32_t));
     plan.gain = take(b->num_segments * sizeof(float));
     plan.info = take(T * sizeof(LossRow));
-    plan.slopes = take(entries ? 0 : T * sizeof(float));
+    plan.label = take(entries ? 0 : T * sizeof(float2));
     plan.sorted = take(listed * sizeof(int32_t));
     plan.shares = take(listed * sizeof(float));
     plan.scores = take(listed * sizeof(float));
@@ -215,7 +220,7 @@ symb_status run_loss(symb_handle h, const symb_loss_batch* b, const void* X, con
     p.part_count = p.count + 1;
     p.gain = (float*)(w + plan.gain);
     p.info = (LossRow*)(w + plan.info);
-    p.slopes = (float*)(w + plan.slopes);
+    p.label = (float2*)(w + plan.label);
     p.sorted = (int32_t*)(w + plan.sorted);
     p.shares = (float*)(w + plan.shares);
     p.scores = (float*)(w + plan.scores);
@@ -235,6 +240,7 @@ symb_status run_loss(symb_handle h, const symb_loss_batch* b, const void* X, con
     p.chunk = plan.chunk;
     p.group_m = 8;
     p.grad_blk = plan.grad_blk;
+    p.two = plan.two;
     p.mean = b->reduction == SYMB_LOSS_MEAN;
     p.cap = b->cap;
     p.to_cap = b->cap > 0.f ? 1.f / b->cap : 0.f;

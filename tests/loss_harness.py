@@ -89,8 +89,9 @@ class Case:
         n = np.array([max((~self.out[a:b]).sum(), 1) if self.mean else 1 for a, b in zip(self.off[:-1], self.off[1:])])
         total = np.array([bound[a:b].sum() + 2.0 ** -20 * np.abs(want_row[a:b]).sum() for a, b in zip(self.off[:-1], self.off[1:])])
         close(loss, want_loss, total / n + 1e-30, what + ": segments")
-        # half a step of the output, half a step of each weight, the weights' own errors (p's and, in l, once more), sums over the vocabulary in fp32
-        tol = 1.02 * 2.0 ** -8 * np.abs(want) + (1.02 * 2.0 ** -8 + self.vocab * 2.0 ** -24) * mass + 2.2 * e[:, None] * both + 1e-30
+        # half a step of the output, half a step of each weight (of its second term, up to 64 rows), the weights' own errors (p's and, in l, once more), sums over the vocabulary in fp32
+        held = 2.0 ** -16 if self.T <= 64 else 2.0 ** -8
+        tol = 1.02 * 2.0 ** -8 * np.abs(want) + (1.02 * held + self.vocab * 2.0 ** -24) * mass + 2.2 * e[:, None] * both + 1e-30
         close(dX, want, tol, what + ": gradient")
         again = self.run()
         assert all(torch.equal(a, b) for a, b in zip((loss, row, dX), again)), what
