@@ -13,8 +13,8 @@
  * A row with a negative label, or without any entry of an id >= 0, takes no part: its loss and its gradient are zeros, and what its x holds is not looked at.  (An entry with a negative id is absent.)
  *   loss_i   mean (SYMB_LOSS_SUM: sum) of L over the segment's rows that take part; 0 if none does
  *   dX       scale_i d loss_i / dx
- * A label or id of V or more is never followed: the row's loss and gradient are NaN, and so are those of a row with a score of NaN or infinity, or with a logit of NaN or infinity (-infinity beside
- * others: a share of zero); no other row's.  A token that a row names twice counts with the sum of its shares.
+ * A label or id of V or more is never followed: the row's loss and gradient are NaN, and so are those of a row with a score of NaN or +infinity, or of -infinity at its label or its teacher's best entry,
+ * or with a logit of NaN or +infinity (-infinity beside others: a share of zero); no other row's.  A token that a row names twice counts with the sum of its shares.
  * What is rounded: the weights p_v - q_v enter the gradient's product as bf16, off by 2^-8 of each at most (in batches of up to 64 rows as two bf16 terms, 2^-16); dX is rounded once.  Scores, sums and
  * losses are fp32, a label's own score is formed in 64 bits: a sure row's loss (p_label near one) keeps its relative precision.  Capping is good to 2^-21 of a score.
  * Deterministic: the same arguments give the same bits.  What else is in the batch can change a row's loss and gradient in the last rounding.
@@ -39,13 +39,13 @@ typedef struct {
     int32_t width;                 /* d: a multiple of 8, at most SYMB_LOSS_MAX_WIDTH */
     int32_t vocab;                 /* V: any number from 1 to SYMB_LOSS_MAX_VOCAB */
     int32_t num_segments;
-    const int32_t* seg_offsets;    /* HOST, as in symb_batch.  T rows; T times width below 2^31 (SYMB_ERR_UNSUPPORTED otherwise: give more in several calls) */
+    const int32_t* seg_offsets;    /* HOST, as in symb_batch.  T rows: at most SYMB_LOSS_MAX_ROWS, and T times width below 2^31 (SYMB_ERR_UNSUPPORTED otherwise: give more in several calls) */
     const symb_loss* losses;       /* HOST, num_segments entries */
     int32_t reduction;             /* symb_loss_reduction */
     float cap;                     /* >= 0, finite; 0: scores as they are */
 } symb_loss_batch;
 
-enum { SYMB_LOSS_MAX_WIDTH = 32768, SYMB_LOSS_MAX_VOCAB = 1 << 22, SYMB_LOSS_MAX_ENTRIES = 1024 };
+enum { SYMB_LOSS_MAX_WIDTH = 32768, SYMB_LOSS_MAX_VOCAB = 1 << 22, SYMB_LOSS_MAX_ENTRIES = 1024, SYMB_LOSS_MAX_ROWS = 1 << 22 };
 
 /* Bytes of workspace for a call on this batch: entries 0 for symb_cross_entropy, else the entries of symb_distillation; gradient 0 for losses alone (dX NULL).  Host-only. */
 symb_status symb_loss_workspace_bytes(const symb_loss_batch* b, int32_t entries, int32_t gradient, size_t* out);

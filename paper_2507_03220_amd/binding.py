@@ -30,7 +30,7 @@ SYMB_NORM_LAYER, SYMB_NORM_RMS = 0, 1
 SYMB_NORM_MAX_WIDTH = 16384
 SYMB_ROTATE_HALVES, SYMB_ROTATE_ADJACENT = 0, 1
 SYMB_LOSS_MEAN, SYMB_LOSS_SUM = 0, 1
-SYMB_LOSS_MAX_WIDTH, SYMB_LOSS_MAX_VOCAB, SYMB_LOSS_MAX_ENTRIES = 32768, 1 << 22, 1024
+SYMB_LOSS_MAX_WIDTH, SYMB_LOSS_MAX_VOCAB, SYMB_LOSS_MAX_ENTRIES, SYMB_LOSS_MAX_ROWS = 32768, 1 << 22, 1024, 1 << 22
 
 EXPORTS = ("symb_create", "symb_destroy", "symb_validate_batch", "symb_debug_row_segment_map",
            "symb_plan_row_tiles", "symb_workspace_bytes", "symb_base_linear_fwd",

@@ -34,6 +34,7 @@ symb_status check_loss(symb_handle h, const symb_loss_batch* b, int32_t entries)
     if (entries < 0) return fail(h, SYMB_ERR_INVALID_ARG, "entries is negative");
     if (entries > SYMB_LOSS_MAX_ENTRIES) return fail(h, SYMB_ERR_UNSUPPORTED, "%d entries: SYMB_LOSS_MAX_ENTRIES at most", entries);
     const int64_t T = b->seg_offsets[b->num_segments];
+    if (T > SYMB_LOSS_MAX_ROWS) return fail(h, SYMB_ERR_UNSUPPORTED, "%lld rows exceed SYMB_LOSS_MAX_ROWS", (long long)T);
     if (T * b->width >= ((int64_t)1 << 31)) return fail(h, SYMB_ERR_UNSUPPORTED, "%lld rows of %d: fewer than 2^31 elements at once", (long long)T, b->width);
     const size_t need = blob_bytes({{(size_t)b->num_segments + 1, sizeof(int32_t)}, {(size_t)b->num_segments, sizeof(LossDesc)}});
     if (need > kSlotBytes) return fail(h, SYMB_ERR_UNSUPPORTED, "batch descriptors need %zu bytes, capacity is %zu", need, kSlotBytes);

@@ -1,5 +1,6 @@
 // Runs the host-only parts of include/symb_loss.h (argument checks and the plan behind the workspace figures) under -fsanitize=address,undefined: ragged, empty, enormous and invalid batches.
 // No GPU call is made.  Prints one line; exit status 0 = every call returned what it should.
+#include <algorithm>
 #include <climits>
 #include <cstdio>
 #include <vector>
@@ -39,7 +40,7 @@ int main() {
     symb_loss one{1.f, 1.f};
     for (const int64_t width : {8, 4096, 32768})
         for (const int vocab : {1, 300, 1 << 22}) {
-            int32_t off[2] = {0, (int32_t)((((int64_t)1 << 31) - 1) / width)};
+            int32_t off[2] = {0, (int32_t)std::min<int64_t>((((int64_t)1 << 31) - 1) / width, SYMB_LOSS_MAX_ROWS)};
             symb_loss_batch b{(int32_t)width, vocab, 1, off, &one, 0, 0.f};
             for (int gradient = 0; gradient < 2; ++gradient) {
                 fails += symb_loss_workspace_bytes(&b, 0, gradient, &bytes) != SYMB_OK;

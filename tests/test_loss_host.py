@@ -38,6 +38,8 @@ def test_refusals():
     assert _status(_batch(), sb.SYMB_LOSS_MAX_ENTRIES + 1) == _status(_batch(vocab=sb.SYMB_LOSS_MAX_VOCAB + 1)) == _status(_batch(width=sb.SYMB_LOSS_MAX_WIDTH + 8)) == sb.SYMB_ERR_UNSUPPORTED
     assert _status(_batch(width=4096, off=(0, 2 ** 19 - 1))) == sb.SYMB_OK
     assert _status(_batch(width=4096, off=(0, 2 ** 19))) == sb.SYMB_ERR_UNSUPPORTED        # 2^31 elements of X
+    assert _status(_batch(width=8, off=(0, sb.SYMB_LOSS_MAX_ROWS))) == sb.SYMB_OK
+    assert _status(_batch(width=8, off=(0, sb.SYMB_LOSS_MAX_ROWS + 1))) == sb.SYMB_ERR_UNSUPPORTED
     assert _status(_batch(off=tuple(range(180001)))) == sb.SYMB_ERR_UNSUPPORTED            # descriptors: 2 MiB at most
     assert _status(_batch(off=tuple(range(170001)))) == sb.SYMB_OK
     assert sb.lib().symb_loss_workspace_bytes(_batch().ref(), 0, 1, None) == sb.SYMB_ERR_INVALID_ARG
