@@ -56,7 +56,8 @@ struct LossParams {
     int32_t T, S, V, pitch, width, K;
     int32_t chunk0, chunk;                // the chunk's first row (of those that take part) and its length at most
     int32_t tile_shift;                   // columns of a tile of the first product: 2^tile_shift
-    int32_t group_m, mean, grad_blk;
+    int32_t group_m, mean;
+    int32_t grad_tile;                    // LossTileKind of the second product
     int32_t two;                          // weights are held in two terms, the second kTwoRows rows below the first
     float cap, to_cap;                    // 1 / cap
 };
@@ -283,9 +284,9 @@ __device__ __forceinline__ uint2 loss_second(const float (&v)[4], uint2 first) {
 // A tile of Aop [rows][K] times Bop ([columns][K], or [K][columns] if NN) into the accumulation registers, with the loops of gemm16_asm.hpp: stages st0 .. st0 + KF - 1 of 64, and what K leaves
 // behind the last whole stage if `tail`.  a_at(row): where a row of the tile starts, in elements from a_tile; b_tile: its first column at k = 0, `ldb` elements from the next (NN: from the next k);
 // `columns`: how many there are.  The lane layout is that of symb_gemm16_kernel.
-template <int BLK, bool NN, class Row>
+template <int MB, int NB, bool NN, class Row>
 __device__ __forceinline__ void loss_tile(unsigned char* smem, const bf16* a_tile, Row a_at, const bf16* b_tile, int ldb, int columns, int st0, int KF, bool tail, int K) {
-    using TT = Gemm16Tile<BLK, BLK>;
+    using TT = Gemm16Tile<MB, NB>;
     constexpr int BM = TT::BM, BN = TT::BN, NT = TT::NT;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int wm0 = (wave >> 1) * TT::WM, wn0 = (wave & 1) * TT::WN, l15 = lane & 15, lg = lane >> 4;
@@ -297,31 +298,53 @@ __device__ __forceinline__ void loss_tile(unsigned char* smem, const bf16* a_til
         return (unsigned)(lds_off_nmajor16<BN>(k, n >> 3) + ((n & 7) << 1));
     };
     if (KF == 0) {
-        if constexpr (BLK == 8) asm volatile(SYMB_GEMM16_ZERO ::: SYMB_GEMM16_ACLOBBERS);
+        if constexpr (TT::TALL) asm volatile(SYMB_GEMM16T_ZERO ::: SYMB_GEMM16T_ACLOBBERS);
+        else if constexpr (NB == 8) asm volatile(SYMB_GEMM16_ZERO ::: SYMB_GEMM16_ACLOBBERS);
         else asm volatile(SYMB_GEMM16S_ZERO ::: SYMB_GEMM16S_ACLOBBERS);
     } else {
-        constexpr int NVB = BLK > 4 ? BLK : 4;
-        unsigned vA[4], vB[NVB], ab[BLK], bb[BLK];
+        // (the 256x128 loop wants its lane offsets and bases shifted, and starts each XCD at another eighth of the stages: see symb_gemm16_kernel)
+        constexpr unsigned LOWER = TT::TALL ? 4096u : 0u;
+        auto lower = [](int j) { return LOWER ? LOWER - 1024u * (unsigned)(j & 3) : 0u; };
+        constexpr int NVB = NB > 4 ? NB : 4;
+        unsigned vA[4], vB[NVB], ab[MB], bb[NB];
 #pragma unroll
         for (int j = 0; j < 4; ++j) vA[j] = lds0 + frag_a(j >> 1, j & 1);
 #pragma unroll
-        for (int j = 0; j < NVB; ++j) vB[j] = lds0 + (NN ? frag_b_nn(j % BLK) : frag_b_nt((j >> 1) & 1, j & 1));
+        for (int j = 0; j < NVB; ++j) vB[j] = lds0 + (NN ? frag_b_nn(j % NB) : frag_b_nt((j >> 1) & 1, j & 1));
 #pragma unroll
-        for (int j = 0; j < BLK; ++j) {
-            const int row = (wave * BLK + j) * 8 + (lane >> 3), kc = (lane & 7) ^ swz_row(row);
-            ab[j] = (a_at(row) + kc * 8) * 2u;
-            if constexpr (!NN) bb[j] = ((unsigned)min(row, columns - 1) * (unsigned)ldb + kc * 8) * 2u;
-            else {
+        for (int j = 0; j < MB; ++j) {
+            const int row = (wave * MB + j) * 8 + (lane >> 3), kc = (lane & 7) ^ swz_row(row);
+            ab[j] = (a_at(row) + kc * 8) * 2u + lower(j);
+        }
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            if constexpr (!NN) {
+                const int row = (wave * NB + j) * 8 + (lane >> 3), kc = (lane & 7) ^ swz_row(row);
+                bb[j] = ((unsigned)min(row, columns - 1) * (unsigned)ldb + kc * 8) * 2u + lower(j);
+            } else {
                 constexpr int CPR = BN / 8;
-                const int krow = (wave * BLK + j) * (64 / CPR) + lane / CPR, nc = (lane % CPR) ^ swz_nmajor16(krow);
-                bb[j] = ((unsigned)krow * (unsigned)ldb + (unsigned)min(nc * 8, columns - 8)) * 2u;
+                const int krow = (wave * NB + j) * (64 / CPR) + lane / CPR, nc = (lane % CPR) ^ swz_nmajor16(krow);
+                bb[j] = ((unsigned)krow * (unsigned)ldb + (unsigned)min(nc * 8, columns - 8)) * 2u + lower(j);
             }
         }
-        const unsigned long long ga = (unsigned long long)(a_tile + (size_t)st0 * 64);
-        const unsigned long long gb = (unsigned long long)(b_tile + (size_t)st0 * 64 * (NN ? ldb : 1));
+        const int first = TT::TALL ? (int)((blockIdx.x & 7) * (unsigned)KF / 8) : 0;
+        const unsigned long long ga = (unsigned long long)(a_tile + (size_t)(st0 + first) * 64) - LOWER;
+        const unsigned long long gb = (unsigned long long)(b_tile + (size_t)(st0 + first) * 64 * (NN ? ldb : 1)) - LOWER;
         const unsigned stride_b = NN ? 128u * (unsigned)ldb : 128u;
-        const unsigned swa = (unsigned)__builtin_amdgcn_readfirstlane((int)lds0 + wave * (1024 * BLK));
-        if constexpr (BLK == 8) {
+        const unsigned swa = (unsigned)__builtin_amdgcn_readfirstlane((int)lds0 + wave * (1024 * MB));
+        if constexpr (TT::TALL) {
+            const unsigned swb = (unsigned)__builtin_amdgcn_readfirstlane((int)lds0 + wave * (1024 * NB));
+#define SYMB_LOSS_LOOP_OPERANDS                                                                                     \
+    :                                                                                                              \
+    : "v"(vA[0]), "v"(vA[1]), "v"(vA[2]), "v"(vA[3]), "v"(vB[0]), "v"(vB[1]), "v"(vB[2]), "v"(vB[3]),              \
+      "v"(ab[0]), "v"(ab[1]), "v"(ab[2]), "v"(ab[3]), "v"(ab[4]), "v"(ab[5]), "v"(ab[6]), "v"(ab[7]),              \
+      "v"(bb[0]), "v"(bb[1]), "v"(bb[2]), "v"(bb[3]),                                                              \
+      "s"(ga), "s"(gb), "s"(stride_b), "s"(KF), "s"(swa), "s"(swb), "s"(first)                                     \
+    : "memory", "scc", SYMB_GEMM16T_SCLOBBERS, SYMB_GEMM16T_VCLOBBERS, SYMB_GEMM16T_ACLOBBERS
+            if constexpr (NN) asm volatile(SYMB_GEMM16T_LOOP_NN SYMB_LOSS_LOOP_OPERANDS);
+            else asm volatile(SYMB_GEMM16T_LOOP_NT SYMB_LOSS_LOOP_OPERANDS);
+#undef SYMB_LOSS_LOOP_OPERANDS
+        } else if constexpr (NB == 8) {
 #define SYMB_LOSS_LOOP_OPERANDS                                                                                     \
     :                                                                                                              \
     : "v"(vA[0]), "v"(vA[1]), "v"(vA[2]), "v"(vA[3]), "v"(vB[0]), "v"(vB[1]), "v"(vB[2]), "v"(vB[3]), "v"(vB[4]),  \
@@ -348,13 +371,14 @@ __device__ __forceinline__ void loss_tile(unsigned char* smem, const bf16* a_til
     const int k0 = K / 64 * 64;
     if (!tail || k0 == K) return;
     // what is left of K, through registers: chunk i of a thread lies 32 rows (KSTEP k-rows) below chunk 0
-    constexpr int CA = BM * 8 / NT, RSTEP = NT / 8, KSTEP = NT / (BN / 8);
+    constexpr int CA = BM * 8 / NT, CB = BN * 8 / NT, RSTEP = NT / 8, KSTEP = NT / (BN / 8);
     unsigned char *const sA = smem, *const sB = smem + TT::UNIT_A;
     const int lrow = tid >> 3, lkc = (tid & 7) * 8, nn_k = tid / (BN / 8), nn_nc = tid % (BN / 8);
-    uint4 ra[CA], rb[CA];
+    uint4 ra[CA], rb[CB];
 #pragma unroll
-    for (int i = 0; i < CA; ++i) {
-        ra[i] = ld_global_16(a_tile + a_at(lrow + i * RSTEP) + k0 + lkc, k0 + lkc < K);
+    for (int i = 0; i < CA; ++i) ra[i] = ld_global_16(a_tile + a_at(lrow + i * RSTEP) + k0 + lkc, k0 + lkc < K);
+#pragma unroll
+    for (int i = 0; i < CB; ++i) {
         if constexpr (!NN) rb[i] = ld_global_16(b_tile + (size_t)min(lrow + i * RSTEP, columns - 1) * ldb + k0 + lkc, k0 + lkc < K);
         else {
             const int k = k0 + nn_k + i * KSTEP;
@@ -363,25 +387,29 @@ __device__ __forceinline__ void loss_tile(unsigned char* smem, const bf16* a_til
     }
     const int a_lds0 = lds_off_kmajor(lrow, tid & 7), b_lds0 = NN ? lds_off_nmajor16<BN>(nn_k, nn_nc) : a_lds0;
 #pragma unroll
-    for (int i = 0; i < CA; ++i) {
-        *reinterpret_cast<uint4*>(sA + a_lds0 + i * RSTEP * 128) = ra[i];
-        *reinterpret_cast<uint4*>(sB + b_lds0 + i * (NN ? KSTEP * (BN * 2) : RSTEP * 128)) = rb[i];
-    }
+    for (int i = 0; i < CA; ++i) *reinterpret_cast<uint4*>(sA + a_lds0 + i * RSTEP * 128) = ra[i];
+#pragma unroll
+    for (int i = 0; i < CB; ++i) *reinterpret_cast<uint4*>(sB + b_lds0 + i * (NN ? KSTEP * (BN * 2) : RSTEP * 128)) = rb[i];
     __syncthreads();
-    const unsigned all = (1u << BLK) - 1;
+    const unsigned all = (1u << MB) - 1;
     for (int ks = 0; ks < (K - k0 + 31) >> 5; ++ks) {
         const unsigned va0 = lds0 + frag_a(ks, 0), va1 = lds0 + frag_a(ks, 1);
         if constexpr (!NN) {
             const unsigned vb0 = lds0 + TT::UNIT_A + frag_b_nt(ks, 0), vb1 = lds0 + TT::UNIT_A + frag_b_nt(ks, 1);
-            if constexpr (BLK == 8)
+            if constexpr (TT::TALL)
+                asm volatile(SYMB_GEMM16T_KSTEP32_NT : : "v"(va0), "v"(va1), "v"(vb0), "v"(vb1), "s"(all) : "memory", "scc", SYMB_GEMM16T_VCLOBBERS, SYMB_GEMM16T_ACLOBBERS);
+            else if constexpr (NB == 8)
                 asm volatile(SYMB_GEMM16_KSTEP32_NT : : "v"(va0), "v"(va1), "v"(vb0), "v"(vb1), "s"(all) : "memory", "scc", SYMB_GEMM16_VCLOBBERS, SYMB_GEMM16_ACLOBBERS);
             else
                 asm volatile(SYMB_GEMM16S_KSTEP32_NT : : "v"(va0), "v"(va1), "v"(vb0), "v"(vb1), "s"(all) : "memory", "scc", SYMB_GEMM16S_VCLOBBERS, SYMB_GEMM16S_ACLOBBERS);
         } else {
-            unsigned vb[BLK];
+            unsigned vb[NB];
 #pragma unroll
-            for (int j = 0; j < BLK; ++j) vb[j] = lds0 + TT::UNIT_A + frag_b_nn(j) + ks * 32 * (BN * 2);
-            if constexpr (BLK == 8)
+            for (int j = 0; j < NB; ++j) vb[j] = lds0 + TT::UNIT_A + frag_b_nn(j) + ks * 32 * (BN * 2);
+            if constexpr (TT::TALL)
+                asm volatile(SYMB_GEMM16T_KSTEP32_NN : : "v"(va0), "v"(va1), "v"(vb[0]), "v"(vb[1]), "v"(vb[2]), "v"(vb[3]), "s"(all)
+                             : "memory", "scc", SYMB_GEMM16T_VCLOBBERS, SYMB_GEMM16T_ACLOBBERS);
+            else if constexpr (NB == 8)
                 asm volatile(SYMB_GEMM16_KSTEP32_NN : : "v"(va0), "v"(va1), "v"(vb[0]), "v"(vb[1]), "v"(vb[2]), "v"(vb[3]), "v"(vb[4]), "v"(vb[5]), "v"(vb[6]), "v"(vb[7]), "s"(all)
                              : "memory", "scc", SYMB_GEMM16_VCLOBBERS, SYMB_GEMM16_ACLOBBERS);
             else
@@ -404,8 +432,8 @@ __device__ __forceinline__ void loss_place(int lin, int m_tiles, int n_tiles, in
 
 // Element (j, e) of a lane's scores: half of what is left at every step.  (With masks that the compiler cannot see through: it makes selected values loads from a selected address, and the scores
 // an array in scratch memory.)
-template <int BLK>
-__device__ __forceinline__ float loss_pick(const float (&w)[BLK][4], int j, int e) {
+template <int NB>
+__device__ __forceinline__ float loss_pick(const float (&w)[NB][4], int j, int e) {
     auto mask = [](int bit) __attribute__((always_inline)) {
         int m = bit ? -1 : 0;
         asm volatile("" : "+v"(m));
@@ -413,12 +441,12 @@ __device__ __forceinline__ float loss_pick(const float (&w)[BLK][4], int j, int 
     };
     auto pick = [](int m, int yes, int no) __attribute__((always_inline)) { return (yes & m) | (no & ~m); };
     const int e0 = mask(e & 1), e1 = mask(e & 2), j0 = mask(j & 1), j1 = mask(j & 2), j2 = mask(j & 4);
-    int v[BLK];
-    static_for<0, BLK>([&](auto K) __attribute__((always_inline)) {
+    int v[NB];
+    static_for<0, NB>([&](auto K) __attribute__((always_inline)) {
         constexpr int k = decltype(K)::value;
         v[k] = pick(e1, pick(e0, as_int(w[k][3]), as_int(w[k][2])), pick(e0, as_int(w[k][1]), as_int(w[k][0])));
     });
-    if constexpr (BLK == 8) static_for<0, 4>([&](auto K) __attribute__((always_inline)) { v[decltype(K)::value] = pick(j2, v[decltype(K)::value + 4], v[decltype(K)::value]); });
+    if constexpr (NB == 8) static_for<0, 4>([&](auto K) __attribute__((always_inline)) { v[decltype(K)::value] = pick(j2, v[decltype(K)::value + 4], v[decltype(K)::value]); });
     return as_float(pick(j1, pick(j0, v[3], v[2]), pick(j0, v[1], v[0])));
 }
 // A tile row's entries of its teacher, behind the staged tile in LDS.
@@ -430,9 +458,9 @@ struct LossHits {
 };
 
 // X W^T of a chunk, a tile a workgroup: its rows' sums of weights, the scores of their teachers' entries, and the weights themselves where the gradient wants them.
-template <int BLK, bool GRAD, bool CAP, bool TEACHER>
+template <int MB, int NB, bool GRAD, bool CAP, bool TEACHER>
 SYMB_KERNEL __launch_bounds__(256) void symb_loss_scores_kernel(const LossParams p) {
-    using TT = Gemm16Tile<BLK, BLK>;
+    using TT = Gemm16Tile<MB, NB>;
     constexpr int BM = TT::BM, BN = TT::BN, CP = TT::C_PITCH;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int rows = loss_chunk_rows(p);
@@ -448,10 +476,10 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_scores_kernel(const LossParams
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int wm0 = (wave >> 1) * TT::WM, wn0 = (wave & 1) * TT::WN, l15 = lane & 15, lg = lane >> 4;
     // what the epilogue needs of this lane's rows
-    float a[BLK], b[BLK];
-    int label[BLK];
+    float a[MB], b[MB];
+    int label[MB];
 #pragma unroll
-    for (int i = 0; i < BLK; ++i) {
+    for (int i = 0; i < MB; ++i) {
         const int t = list[min(m0 + wm0 + 16 * i + l15, rows - 1)];
         a[i] = p.info[t].a;
         b[i] = p.info[t].b;
@@ -468,7 +496,7 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_scores_kernel(const LossParams
         for (int k = 0; k < 4; ++k) hits.id[k] = p.sorted[(int64_t)t * p.K + min(at + k, p.K - 1)];
     }
     auto a_at = [&](int row) __attribute__((always_inline)) { return (unsigned)(list[min(m0 + row, rows - 1)] - first) * (unsigned)p.width; };
-    loss_tile<BLK, false>(smem, p.X + (size_t)first * p.width, a_at, p.W + (size_t)n0 * p.width, p.width, p.V - n0, 0, p.width / 64, true, p.width);
+    loss_tile<MB, NB, false>(smem, p.X + (size_t)first * p.width, a_at, p.W + (size_t)n0 * p.width, p.width, p.V - n0, 0, p.width / 64, true, p.width);
 
     LossHits* const row_hits = reinterpret_cast<LossHits*>(smem + TT::C_BYTES);
     static_assert(TT::C_BYTES % 16 == 0 && TT::C_BYTES + BM * (int)sizeof(LossHits) <= TT::SMEM, "");
@@ -480,19 +508,19 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_scores_kernel(const LossParams
     const int left = p.V - (n0 + wn0 + 4 * lg);                                // columns of this lane: 16 j + e < left
     const bool edge = n0 + BN > p.V;
     float2* const stats = p.stats + (size_t)(2 * tn + (wave & 1)) * p.chunk + m0 + wm0;
-    static_for<0, BLK>([&](auto I) __attribute__((always_inline)) {
+    static_for<0, MB>([&](auto I) __attribute__((always_inline)) {
         constexpr int i = decltype(I)::value;
-        float w[BLK][4], slope[CAP ? BLK : 1][4];
+        float w[NB][4], slope[CAP ? NB : 1][4];
         auto scores = [&]() __attribute__((always_inline)) {
-            static_for<0, BLK>([&](auto J) __attribute__((always_inline)) {
+            static_for<0, NB>([&](auto J) __attribute__((always_inline)) {
                 constexpr int j = decltype(J)::value;
-                acc16_read4<4 * (BLK * i + j)>(w[j][0], w[j][1], w[j][2], w[j][3]);
+                acc16_read4<4 * (NB * i + j)>(w[j][0], w[j][1], w[j][2], w[j][3]);
             });
         };
         // a z - b, the general way
         auto exponents = [&]() __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < BLK; ++j)
+            for (int j = 0; j < NB; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     if constexpr (CAP) w[j][e] = loss_capped(w[j][e], p.cap, p.to_cap, slope[j][e]);
@@ -503,22 +531,22 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_scores_kernel(const LossParams
         auto weights = [&](float shift) __attribute__((always_inline)) {
             float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < BLK; ++j)
+            for (int j = 0; j < NB; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) w[j][e] = __builtin_amdgcn_exp2f(w[j][e] - shift);
             if (edge)
 #pragma unroll
-                for (int j = 0; j < BLK; ++j)
+                for (int j = 0; j < NB; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) w[j][e] = 16 * j + e < left ? w[j][e] : 0.f;
-            if (!TEACHER && __any((unsigned)label[i] < 16u * BLK)) {
+            if (!TEACHER && __any((unsigned)label[i] < 16u * NB)) {
 #pragma unroll
-                for (int j = 0; j < BLK; ++j)
+                for (int j = 0; j < NB; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[e] += 16 * j + e == label[i] ? 0.f : w[j][e];
             } else {
 #pragma unroll
-                for (int j = 0; j < BLK; ++j)
+                for (int j = 0; j < NB; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[e] += w[j][e];
             }
@@ -534,21 +562,21 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_scores_kernel(const LossParams
                 if (k < n) c = (k < 4 ? hit.id[k] : p.sorted[hit.at + k]) - (n0 + wn0);
                 const bool mine = (unsigned)c < (unsigned)TT::WN && (c >> 2 & 3) == lg;
                 if (!__any(mine)) continue;
-                const float s = loss_pick<BLK>(w, c >> 4, c & 3);
+                const float s = loss_pick<NB>(w, c >> 4, c & 3);
                 if (mine) p.scores[hit.at + k] = s;
             }
         }
         if constexpr (CAP) {
             float top = 0.f;
 #pragma unroll
-            for (int j = 0; j < BLK; ++j)
+            for (int j = 0; j < NB; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(w[j][e]));
             if (__any(!(top <= kLossNear * p.cap))) exponents();
             else {
                 const float to_exp = a[i] * p.cap;
 #pragma unroll
-                for (int j = 0; j < BLK; ++j)
+                for (int j = 0; j < NB; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float y = w[j][e] * p.to_cap, th = loss_tanh(y);
@@ -565,7 +593,7 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_scores_kernel(const LossParams
             exponents();
             float most = -__builtin_inff();
 #pragma unroll
-            for (int j = 0; j < BLK; ++j)
+            for (int j = 0; j < NB; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (!edge || 16 * j + e < left) most = fmaxf(most, w[j][e]);
@@ -576,13 +604,13 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_scores_kernel(const LossParams
         if (lg == 0) stats[16 * i + l15] = make_float2(shift, sum);            // (rows behind the last one have room)
         if constexpr (GRAD) {
 #pragma unroll
-            for (int j = 0; j < BLK; ++j) {
+            for (int j = 0; j < NB; ++j) {
                 if constexpr (CAP)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) w[j][e] *= slope[j][e];
                 const uint2 first = make_uint2(pack2_bf16(w[j][0], w[j][1]), pack2_bf16(w[j][2], w[j][3]));
                 // (of up to 64 rows the tile's lower half holds their second terms)
-                if (BLK == 4 && p.two) {
+                if (MB == 4 && p.two) {
                     if (wm0 == 0) {
                         *reinterpret_cast<uint2*>(smem + c_lane + i * 16 * CP + j * 32) = first;
                         *reinterpret_cast<uint2*>(smem + c_lane + (kTwoRows + i * 16) * CP + j * 32) = loss_second(w[j], first);
@@ -774,22 +802,29 @@ SYMB_KERNEL __launch_bounds__(64 * kFewWaves, RB == 1 ? 4 : 2) void symb_loss_fe
 }
 
 // Parts that the second product's inner dimension (the vocabulary) is cut into: as few rounds of workgroups as possible, weighed against the partial tiles' way through memory.
-template <int BLK>
-struct LossGrad {
-    static constexpr int kSlots = BLK == 8 ? 256 : 512;                        // workgroups at once
-    static constexpr int kPartNs = BLK == 8 ? 116 : 40;                        // a partial tile, written and read
-};
+// Nanoseconds: a stage of a tile of 256x256 and of 256x128, whose workgroup has a CU alone; of 128x128, of two workgroups that share a CU and of one that has it alone; the rest of a workgroup's
+// time; a partial tile, written and read.
 constexpr int kLossParts = 128, kLossRoundNs = 5000;
-// A stage of a tile of 256 x 256; of 128 x 128, of two workgroups that share a CU and of one that has it alone.
-constexpr int kLossStageNs = 1400, kLossStage4Ns = 1100, kLossLoneNs = 720;
-template <int BLK>
-__host__ __device__ constexpr int64_t loss_grad_ns(int64_t tiles, int stages, int n) {
-    using G = LossGrad<BLK>;
-    const int stage = BLK == 8 ? kLossStageNs : tiles * n <= G::kSlots / 2 ? kLossLoneNs : kLossStage4Ns;
-    return (tiles * n + G::kSlots - 1) / G::kSlots * ((int64_t)((stages + n - 1) / n) * stage + kLossRoundNs) + tiles * n * G::kPartNs;
-}
+template <int MB, int NB>
+struct LossTile {
+    static constexpr int kEdgeM = 32 * MB, kEdgeN = 32 * NB, kSlots = MB == 4 ? 512 : 256;
+    static constexpr int kStageNs = NB == 8 ? 1400 : MB == 8 ? 750 : 1100, kLoneNs = MB == 4 ? 720 : kStageNs, kPartNs = NB == 8 ? 116 : 40;
+    __host__ __device__ static constexpr int64_t tiles(int64_t rows, int64_t columns) { return (rows + kEdgeM - 1) / kEdgeM * ((columns + kEdgeN - 1) / kEdgeN); }
+    __host__ __device__ static constexpr int64_t ns(int64_t tiles, int stages, int n) {
+        return (tiles * n + kSlots - 1) / kSlots * ((int64_t)((stages + n - 1) / n) * (tiles * n <= kSlots / 2 ? kLoneNs : kStageNs) + kLossRoundNs) + tiles * n * kPartNs;
+    }
+};
 // room: partial tiles that fit the workspace.
 __host__ __device__ constexpr bool loss_grad_fits(int64_t tiles, int stages, int n, int64_t room) { return n == 1 || (tiles * n <= room && stages / n >= 4); }
+enum LossTileKind : int32_t { kLossBig, kLossTall, kLossSmall };               // 256x256, 256x128, 128x128
+template <class F>
+__host__ __device__ __forceinline__ auto loss_tiled(int kind, F&& f) {
+    return kind == kLossBig ? f(LossTile<8, 8>{}) : kind == kLossTall ? f(LossTile<8, 4>{}) : f(LossTile<4, 4>{});
+}
+template <class F>                        // (the second product)
+__host__ __device__ __forceinline__ auto loss_grad_tiled(int kind, F&& f) {
+    return kind == kLossBig ? f(LossTile<8, 8>{}) : f(LossTile<4, 4>{});
+}
 
 // ---- sums, losses, and the entries of q ---------------------------------------------------------------------------------------------
 constexpr int kJoinRows = 16, kJoinSets = 32;
@@ -797,15 +832,14 @@ constexpr int kJoinRows = 16, kJoinSets = 32;
 __device__ __forceinline__ float loss_in(float2 s, float unit) { return s.x == unit ? s.y : s.y * exp2f(s.x - unit); }
 // 16 rows a workgroup of 512: the column parts' sums in a fixed order, the rows' losses, and their entries of p - q into the held weights.  `parts`: column parts of `cols` columns;
 // finish: the segments' losses as well (one workgroup has all rows).  Beside that, for how many parts the gradient's product comes in.
-template <int BLK>
+template <class Tile>
 __device__ __forceinline__ int loss_grad_parts(const LossParams& p, int rows) {
-    constexpr int BM = 32 * BLK;
-    const int64_t tiles = (int64_t)((rows + BM - 1) / BM) * ((p.width + BM - 1) / BM);
+    const int64_t tiles = Tile::tiles(rows, p.width);
     const int stages = p.V / 64;
     float best = 3e38f;                                   // (nanoseconds)
     int n = 1;
     for (int k = 1 + (int)(threadIdx.x & 63); k <= kLossParts; k += 64) {
-        const float ns = loss_grad_fits(tiles, stages, k, p.part_tiles) ? (float)loss_grad_ns<BLK>(tiles, stages, k) * (1.f + 1e-4f * k) : 3e38f;
+        const float ns = loss_grad_fits(tiles, stages, k, p.part_tiles) ? (float)Tile::ns(tiles, stages, k) * (1.f + 1e-4f * k) : 3e38f;
         if (ns < best) best = ns, n = k;
     }
 #pragma unroll
@@ -825,7 +859,7 @@ SYMB_KERNEL __launch_bounds__(kJoinRows* kJoinSets) void symb_loss_join_kernel(c
     const int rows = loss_chunk_rows(p);
     if (m0 >= rows && !finish) return;
     if (p.dX && blockIdx.x == 0 && wave == kJoinSets / 4 - 1) {
-        const int n = p.grad_blk == 8 ? loss_grad_parts<8>(p, rows) : loss_grad_parts<4>(p, rows);
+        const int n = loss_grad_tiled(p.grad_tile, [&](auto tile) { return loss_grad_parts<decltype(tile)>(p, rows); });
         if (lane == 0) *p.part_count = n;
     }
     int t = 0;
@@ -936,9 +970,9 @@ SYMB_KERNEL __launch_bounds__(kJoinRows* kJoinSets) void symb_loss_join_kernel(c
 }
 
 // ---- the gradient's product -----------------------------------------------------------------------------------------------------------
-template <int BLK>
+template <int MB, int NB>
 SYMB_KERNEL __launch_bounds__(256) void symb_loss_grad_kernel(const LossParams p) {
-    using TT = Gemm16Tile<BLK, BLK>;
+    using TT = Gemm16Tile<MB, NB>;
     constexpr int BM = TT::BM, BN = TT::BN;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int own = loss_chunk_rows(p), rows = p.two ? kTwoRows + own : own;
@@ -953,11 +987,12 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_grad_kernel(const LossParams p
     const int m0 = tm * BM, n0 = tn * BN, stages = p.V / 64;
     const int st0 = (int)((int64_t)stages * part / n), st1 = (int)((int64_t)stages * (part + 1) / n);
     auto a_at = [&](int row) __attribute__((always_inline)) { return (unsigned)(min(m0 + row, rows - 1) - m0) * (unsigned)p.pitch; };
-    loss_tile<BLK, true>(smem, p.held + (size_t)m0 * p.pitch, a_at, p.W + n0, p.width, p.width - n0, st0, st1 - st0, part == n - 1, p.V);
+    loss_tile<MB, NB, true>(smem, p.held + (size_t)m0 * p.pitch, a_at, p.W + n0, p.width, p.width - n0, st0, st1 - st0, part == n - 1, p.V);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const unsigned lane_off = (unsigned)(wave * (BLK * BLK * 1024) + lane * 16);
+    const unsigned lane_off = (unsigned)(wave * (MB * NB * 1024) + lane * 16);
     const unsigned long long mine = (unsigned long long)(p.parts + (size_t)(part * tiles + tm * n_tiles + tn) * (BM * BN));
-    if constexpr (BLK == 8) asm volatile(SYMB_GEMM16_STORE_PARTIAL : : "v"(lane_off), "s"(mine) : "memory", SYMB_GEMM16_VCLOBBERS);
+    static_assert(!TT::TALL, "");
+    if constexpr (NB == 8) asm volatile(SYMB_GEMM16_STORE_PARTIAL : : "v"(lane_off), "s"(mine) : "memory", SYMB_GEMM16_VCLOBBERS);
     else asm volatile(SYMB_GEMM16S_STORE_PARTIAL : : "v"(lane_off), "s"(mine) : "memory", SYMB_GEMM16S_VCLOBBERS);
 }
 
@@ -987,26 +1022,27 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_segments_kernel(LossParams p) 
 
 // The parts of a tile added in a fixed order, times the row's gain, to the rows they belong to.  A workgroup takes blocks of 16 x 16 of one wavefront's rows: four of them, or, of products in many
 // parts, one whose parts its wavefronts share out.  Workgroups from number `blocks` on: the segments' losses.
-template <int BLK, bool MANY>
+template <int MB, int NB, bool MANY>
 SYMB_KERNEL __launch_bounds__(256) void symb_loss_reduce_kernel(const LossParams p, int blocks) {
-    constexpr int BM = 32 * BLK, GROUPS = MANY ? BLK : BLK / 4;
+    constexpr int BM = 32 * MB, BN = 32 * NB, GROUPS = MANY ? NB : NB / 4;
     __shared__ floatx4 lds[4][64];
     if ((int)blockIdx.x >= blocks) return loss_segment(p, blockIdx.x - blocks, lds[0]);
     const int rows = loss_chunk_rows(p);
     if (rows <= 0) return;
-    const int n_tiles = (p.width + BM - 1) / BM, m_tiles = (rows + BM - 1) / BM, tiles = m_tiles * n_tiles;
+    const int n_tiles = (p.width + BN - 1) / BN, m_tiles = (rows + BM - 1) / BM, tiles = m_tiles * n_tiles;
     const int lane = threadIdx.x & 63, own = threadIdx.x >> 6, j = blockIdx.x % GROUPS * (MANY ? 1 : 4) + (MANY ? 0 : own);
-    const int i = blockIdx.x / GROUPS % BLK, wave = blockIdx.x / (GROUPS * BLK) % 4, tile = blockIdx.x / (GROUPS * BLK * 4);
-    if (tile >= tiles) return;
-    const int m = tile / n_tiles * BM + (wave >> 1) * (BM / 2) + 16 * i + (lane & 15), col = tile % n_tiles * BM + (wave & 1) * (BM / 2) + 16 * j + 4 * (lane >> 4);
+    const int i = blockIdx.x / GROUPS % MB, wave = blockIdx.x / (GROUPS * MB) % 4, tile = blockIdx.x / (GROUPS * MB * 4);
+    const int m0 = tile / n_tiles * BM + (wave >> 1) * (BM / 2) + 16 * i;
+    if (tile >= tiles || m0 >= rows) return;              // (of up to kTwoRows rows what is left has its second terms within the tile)
+    const int m = m0 + (lane & 15), col = tile % n_tiles * BN + (wave & 1) * (BN / 2) + 16 * j + 4 * (lane >> 4);
     const int n = *p.part_count;
-    const float* src = p.parts + (size_t)tile * (BM * BM) + (size_t)(wave * BLK * BLK + BLK * i + j) * 256 + lane * 4;
+    const float* src = p.parts + (size_t)tile * (BM * BN) + (size_t)(wave * MB * NB + NB * i + j) * 256 + lane * 4;
     floatx4 s = floatx4{0, 0, 0, 0};
 #pragma unroll 8
-    for (int k = MANY ? own : 0; k < n; k += MANY ? 4 : 1) s += *(const floatx4*)(src + (size_t)k * tiles * (BM * BM));
-    if (BLK == 4 && p.two)                                // the second terms' product, kTwoRows rows below: of the wavefront two further on
+    for (int k = MANY ? own : 0; k < n; k += MANY ? 4 : 1) s += *(const floatx4*)(src + (size_t)k * tiles * (BM * BN));
+    if (MB == 4 && p.two)                                 // the second terms' product, kTwoRows rows below: of the wavefront two further on
 #pragma unroll 8
-        for (int k = MANY ? own : 0; k < n; k += MANY ? 4 : 1) s += *(const floatx4*)(src + 2 * BLK * BLK * 256 + (size_t)k * tiles * (BM * BM));
+        for (int k = MANY ? own : 0; k < n; k += MANY ? 4 : 1) s += *(const floatx4*)(src + 2 * MB * NB * 256 + (size_t)k * tiles * (BM * BN));
     if constexpr (MANY) {
         lds[own][lane] = s;
         __syncthreads();

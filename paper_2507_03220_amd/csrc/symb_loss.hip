@@ -43,9 +43,10 @@ symb_status check_loss(symb_handle h, const symb_loss_batch* b, int32_t entries)
 
 // A call's chunks of rows, tiles, and the places of its workspace.
 struct LossPlan {
-    int chunk = 0, score_blk = 8, grad_blk = 8, pitch = 0, tile_cols = 0, column_parts = 0;
+    int chunk = 0, score_tile = kLossBig, grad_tile = kLossBig, pitch = 0, tile_cols = 0, column_parts = 0;
     int few = 0;                          // blocks of 16 rows of a batch that the kernel for few rows takes
     int64_t part_tiles = 0;
+    size_t part_bytes = 0;
     bool two = false;                     // weights held in two terms
     bool many_parts = false;              // the second product's tiles come in many parts
     size_t rows = 0, flags = 0, count = 0, gain = 0, info = 0, label = 0, sorted = 0, shares = 0, scores = 0, starts = 0, row_loss = 0, stats = 0, row_gain = 0, held = 0, parts = 0, bytes = 0;
@@ -55,23 +56,43 @@ constexpr int64_t kHeldBytes = (int64_t)2 << 30, kStatBytes = (int64_t)256 << 20
 
 constexpr int kLossListedRows = 512;
 
-int64_t tiles_of(int64_t rows, int64_t columns, int edge) { return ((rows + edge - 1) / edge) * ((columns + edge - 1) / edge); }
-
-// Microseconds of the product with W of so many rows, in tiles of 32 blk.
-double score_us(int rows, const symb_loss_batch* b, int blk) {
-    const int64_t tiles = tiles_of(rows, b->vocab, 32 * blk), slots = blk == 8 ? 256 : 512;
-    const int stage = blk == 8 ? kLossStageNs : tiles <= slots / 2 ? kLossLoneNs : kLossStage4Ns;
-    return 1e-3 * (double)((tiles + slots - 1) / slots) * ((b->width + 63) / 64 * stage + (blk == 8 ? 8000 : 6000));
+// Microseconds of the product with W of so many rows, in tiles of one kind; of the gradient's, in the number of parts that suits it best.
+double score_us(int kind, int rows, const symb_loss_batch* b) {
+    return loss_tiled(kind, [&](auto tile) {
+        using L = decltype(tile);
+        const int64_t tiles = L::tiles(rows, b->vocab);
+        return 1e-3 * (double)((tiles + L::kSlots - 1) / L::kSlots) * ((b->width + 63) / 64 * (tiles <= L::kSlots / 2 ? L::kLoneNs : L::kStageNs) + (L::kSlots == 256 ? 8000 : 6000));
+    });
 }
-template <int BLK>
-double grad_us(int rows, const symb_loss_batch* b, int& n) {
-    const int64_t tiles = tiles_of(rows, b->width, 32 * BLK);
-    int64_t least = INT64_MAX;
-    for (int k = 1; k <= kLossParts && loss_grad_fits(tiles, b->vocab / 64, k, INT64_MAX); ++k) {
-        const int64_t ns = loss_grad_ns<BLK>(tiles, b->vocab / 64, k);
-        if (ns + ns / 10000 * k < least) least = ns + ns / 10000 * k, n = k;
-    }
-    return 1e-3 * (double)least;
+double grad_us(int kind, int rows, const symb_loss_batch* b, int& n) {
+    return loss_grad_tiled(kind, [&](auto tile) {
+        using L = decltype(tile);
+        const int64_t tiles = L::tiles(rows, b->width);
+        int64_t least = INT64_MAX;
+        for (int k = 1; k <= kLossParts && loss_grad_fits(tiles, b->vocab / 64, k, INT64_MAX); ++k) {
+            const int64_t ns = L::ns(tiles, b->vocab / 64, k);
+            if (ns + ns / 10000 * k < least) least = ns + ns / 10000 * k, n = k;
+        }
+        return 1e-3 * (double)least;
+    });
+}
+// The kind that takes least, and that time.  (The second product in tiles of 256x128 was no faster anywhere.  The first, of 200 rows of 4096 over 32000: 74.4 us with them, 95.1 with those of
+// 256x256, 90.3 with those of 128x128; 512 rows 126, 109, 160; 128 rows 85, 91, 76.)
+int best_score(int rows, const symb_loss_batch* b, bool two, double& us) {
+    int best = kLossSmall;
+    us = score_us(best, rows, b);
+    for (int kind = kLossBig; kind < kLossSmall && !two; ++kind)
+        if (const double other = score_us(kind, rows, b); other < us) us = other, best = kind;
+    return best;
+}
+int best_grad(int rows, const symb_loss_batch* b, bool two, int& n, double& us) {
+    us = grad_us(kLossSmall, rows, b, n);
+    int parts = 1;
+    const double other = two ? us : grad_us(kLossBig, rows, b, parts);
+    if (other >= us) return kLossSmall;
+    n = parts;
+    us = other;
+    return kLossBig;
 }
 
 LossPlan plan_loss(const symb_loss_batch* b, int32_t entries, bool gradient) {
@@ -82,33 +103,42 @@ LossPlan plan_loss(const symb_loss_batch* b, int32_t entries, bool gradient) {
     // (a row's weights, or, of a small vocabulary, its fp32 product)
     const int64_t row_bytes = gradient ? std::max<int64_t>(plan.pitch * 2, (b->width + 255) / 256 * 1024) : ((int64_t)(b->vocab + 255) / 256) * 4 * (int64_t)sizeof(float2);
     const int most = (int)std::min<int64_t>(rows, std::max<int64_t>((gradient ? kHeldBytes : kStatBytes) / row_bytes / 256 * 256, 256));
+    plan.two = gradient && T <= kTwoRows;
     // of the chunks that fit, the one whose whole chunks take least in all
-    int n8 = 1, n4 = 1;
+    int parts = 1;
     double least = 1e300;
     plan.chunk = most;
     const int step = std::max(256, most / 64 / 256 * 256);
     for (int c = step; c <= most; c += step) {
         const int whole = rows / c, rest = rows % c;
-        auto us = [&](int r) { return r ? std::min(score_us(r, b, 8), score_us(r, b, 4)) + (gradient ? std::min(grad_us<8>(r, b, n8), grad_us<4>(r, b, n4)) : 0.0) + 15.0 : 0.0; };
+        auto us = [&](int r) {
+            double score = 0.0, grad = 0.0;
+            if (r) best_score(r, b, plan.two, score);
+            if (r && gradient) best_grad(r, b, plan.two, parts, grad);
+            return r ? score + grad + 15.0 : 0.0;
+        };
         const double all = whole * us(c) + us(rest);
         if (all < least) least = all, plan.chunk = c;
     }
     const int first = (int)std::min<int64_t>(T, plan.chunk);
-    plan.score_blk = T > kTwoRows && score_us(first, b, 8) < score_us(first, b, 4) ? 8 : 4;
+    double us = 0.0;
+    plan.score_tile = best_score(first, b, plan.two, us);
     if (gradient) {
         // A row's few largest weights may be most of its gradient, and where rows are few their roundings do not even out: up to 64 rows (half of a tile of 128, whose other half costs nothing) hold
         // their weights in two bf16 terms.  One row: off by 1.7e-3 of it, what rounding dX costs, up to 3.7e-3 with one term; 256 rows with one term 2.4e-3.
-        plan.two = T <= kTwoRows;
-        const double us8 = grad_us<8>(first, b, n8), us4 = grad_us<4>(first, b, n4);
-        plan.grad_blk = !plan.two && us8 < us4 ? 8 : 4;
-        const int edge = 32 * plan.grad_blk;
-        plan.many_parts = (plan.grad_blk == 8 ? n8 : n4) >= 8;
-        plan.part_tiles = std::max<int64_t>(tiles_of(first, b->width, edge) * (plan.grad_blk == 8 ? n8 : n4), std::min<int64_t>(512, tiles_of(1, b->width, edge) * std::max(b->vocab / 256, 1)));
+        plan.grad_tile = best_grad(first, b, plan.two, parts, us);
+        plan.many_parts = parts >= 8;
+        loss_grad_tiled(plan.grad_tile, [&](auto tile) {
+            using L = decltype(tile);
+            // (room for more parts of fewer rows, where many of a batch take no part)
+            plan.part_tiles = std::max<int64_t>(L::tiles(first, b->width) * parts, std::min<int64_t>(512, L::tiles(1, b->width) * std::max(b->vocab / 256, 1)));
+            plan.part_bytes = (size_t)plan.part_tiles * L::kEdgeM * L::kEdgeN * sizeof(float);
+        });
     }
     // The kernel for few rows: where rows are long or the tiles of 128 columns few.  Both sides, with W from HBM: 16 rows of 4096 over 32000 65 us with it, 75 with tiles; 32 rows 74, 76; of 6144 over
     // 49152 134, 142 and 149, 144; of 1024 over 50257 16 rows 45, 36; of 4096 over 12000 37, 65 and, 32 rows, 41, 66; of 768 over 4000 19, 20 and 23, 23.
     if (T <= kFewRows && (b->width >= 2048 || b->vocab <= 16384)) plan.few = T <= 16 ? 1 : 2;
-    plan.tile_cols = plan.few ? kFewCols : 32 * plan.score_blk;
+    plan.tile_cols = plan.few ? kFewCols : plan.score_tile == kLossBig ? 256 : 128;
     const int column_tiles = (b->vocab + plan.tile_cols - 1) / plan.tile_cols;
     plan.column_parts = column_tiles * (plan.few ? 1 : 2);
     size_t at = 0;
@@ -131,16 +161,16 @@ LossPlan plan_loss(const symb_loss_batch* b, int32_t entries, bool gradient) {
     plan.stats = take((size_t)plan.column_parts * plan.chunk * sizeof(float2));
     plan.row_gain = take(gradient ? plan.chunk * sizeof(float) : 0);
     plan.held = take(gradient ? (size_t)plan.chunk * plan.pitch * 2 : 0);
-    plan.parts = take((size_t)plan.part_tiles * (32 * plan.grad_blk) * (32 * plan.grad_blk) * sizeof(float));
+    plan.parts = take(plan.part_bytes);
     plan.bytes = T ? at : 0;
     return plan;
 }
 
 // A kernel of the tiles of gemm16_asm.hpp: its LDS once per context (the attribute belongs to the device the kernel is loaded on).
-template <int BLK, class F>
+template <int MB, int NB, class F>
 symb_status launch_tiles(symb_handle h, F kernel, int64_t tiles, const LossParams& p, hipStream_t s) {
     const void* k = reinterpret_cast<const void*>(kernel);
-    constexpr int smem = Gemm16Tile<BLK, BLK>::SMEM;
+    constexpr int smem = Gemm16Tile<MB, NB>::SMEM;
     if (std::find(h->lds_attr_set.begin(), h->lds_attr_set.end(), k) == h->lds_attr_set.end()) {
         SYMB_HIP(h, hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, smem));
         h->lds_attr_set.push_back(k);
@@ -149,12 +179,12 @@ symb_status launch_tiles(symb_handle h, F kernel, int64_t tiles, const LossParam
     SYMB_HIP(h, hipGetLastError());
     return SYMB_OK;
 }
-template <int BLK>
-symb_status launch_scores(symb_handle h, const LossParams& p, int rows, hipStream_t s) {
-    const int64_t tiles = tiles_of(rows, p.V, 32 * BLK);
+template <int MB, int NB>
+symb_status launch_scores(symb_handle h, const LossParams& p, int rows, hipStream_t s, LossTile<MB, NB>) {
+    const int64_t tiles = LossTile<MB, NB>::tiles(rows, p.V);
     auto by_teacher = [&](auto grad, auto cap) {
         constexpr bool G = decltype(grad)::value, C = decltype(cap)::value;
-        return p.ids ? launch_tiles<BLK>(h, symb_loss_scores_kernel<BLK, G, C, true>, tiles, p, s) : launch_tiles<BLK>(h, symb_loss_scores_kernel<BLK, G, C, false>, tiles, p, s);
+        return p.ids ? launch_tiles<MB, NB>(h, symb_loss_scores_kernel<MB, NB, G, C, true>, tiles, p, s) : launch_tiles<MB, NB>(h, symb_loss_scores_kernel<MB, NB, G, C, false>, tiles, p, s);
     };
     auto by_cap = [&](auto grad) { return p.cap > 0.f ? by_teacher(grad, std::true_type{}) : by_teacher(grad, std::false_type{}); };
     return p.dX ? by_cap(std::true_type{}) : by_cap(std::false_type{});
@@ -169,13 +199,13 @@ symb_status launch_few(symb_handle h, const LossParams& p, hipStream_t s) {
     SYMB_HIP(h, hipGetLastError());
     return SYMB_OK;
 }
-template <int BLK>
-symb_status launch_grad(symb_handle h, const LossParams& p, int rows, bool many_parts, bool segments, hipStream_t s) {
-    const symb_status st = launch_tiles<BLK>(h, symb_loss_grad_kernel<BLK>, p.part_tiles, p, s);
+template <int MB, int NB>
+symb_status launch_grad(symb_handle h, const LossParams& p, int rows, bool many_parts, bool segments, hipStream_t s, LossTile<MB, NB>) {
+    const symb_status st = launch_tiles<MB, NB>(h, symb_loss_grad_kernel<MB, NB>, p.part_tiles, p, s);
     if (st != SYMB_OK) return st;
-    const unsigned blocks = (unsigned)(tiles_of(rows, p.width, 32 * BLK) * 4 * BLK * BLK / (many_parts ? 1 : 4)), more = segments ? p.S : 0;
-    if (many_parts) hipLaunchKernelGGL((symb_loss_reduce_kernel<BLK, true>), dim3(blocks + more), dim3(256), 0, s, p, (int)blocks);
-    else hipLaunchKernelGGL((symb_loss_reduce_kernel<BLK, false>), dim3(blocks + more), dim3(256), 0, s, p, (int)blocks);
+    const unsigned blocks = (unsigned)(LossTile<MB, NB>::tiles(rows, p.width) * 4 * MB * NB / (many_parts ? 1 : 4)), more = segments ? p.S : 0;
+    if (many_parts) hipLaunchKernelGGL((symb_loss_reduce_kernel<MB, NB, true>), dim3(blocks + more), dim3(256), 0, s, p, (int)blocks);
+    else hipLaunchKernelGGL((symb_loss_reduce_kernel<MB, NB, false>), dim3(blocks + more), dim3(256), 0, s, p, (int)blocks);
     SYMB_HIP(h, hipGetLastError());
     return SYMB_OK;
 }
@@ -240,7 +270,7 @@ symb_status run_loss(symb_handle h, const symb_loss_batch* b, const void* X, con
     p.tile_shift = plan.tile_cols == 64 ? 6 : plan.tile_cols == 128 ? 7 : 8;
     p.chunk = plan.chunk;
     p.group_m = 8;
-    p.grad_blk = plan.grad_blk;
+    p.grad_tile = plan.grad_tile;
     p.two = plan.two;
     p.mean = b->reduction == SYMB_LOSS_MEAN;
     p.cap = b->cap;
@@ -264,12 +294,12 @@ symb_status run_loss(symb_handle h, const symb_loss_batch* b, const void* X, con
         p.chunk0 = (int32_t)at;
         const int rows = (int)std::min<int64_t>(T - at, plan.chunk);
         if (plan.few) st = plan.few == 1 ? launch_few<1>(h, p, s) : launch_few<2>(h, p, s);
-        else st = plan.score_blk == 8 ? launch_scores<8>(h, p, rows, s) : launch_scores<4>(h, p, rows, s);
+        else st = loss_tiled(plan.score_tile, [&](auto tile) { return launch_scores(h, p, rows, s, tile); });
         if (st != SYMB_OK) return st;
         hipLaunchKernelGGL(symb_loss_join_kernel, dim3((rows + kJoinRows - 1) / kJoinRows), dim3(kJoinRows * kJoinSets), 0, s, p, plan.column_parts, plan.few ? kFewCols : plan.tile_cols / 2, finish);
         SYMB_HIP(h, hipGetLastError());
         const bool segments = loss && !finish && at + rows == T;
-        if (dX && (st = plan.grad_blk == 8 ? launch_grad<8>(h, p, rows, plan.many_parts, segments, s) : launch_grad<4>(h, p, rows, plan.many_parts, segments, s)) != SYMB_OK) return st;
+        if (dX && (st = loss_grad_tiled(plan.grad_tile, [&](auto tile) { return launch_grad(h, p, rows, plan.many_parts, segments, s, tile); })) != SYMB_OK) return st;
     }
     if (loss && !finish && !(dX && T)) {
         hipLaunchKernelGGL(symb_loss_segments_kernel, dim3(S), dim3(256), 0, s, p);

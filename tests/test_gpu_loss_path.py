@@ -179,7 +179,8 @@ def _reference(c):
 # more rows than the weights of one chunk have room for; wide and narrow tiles of both products, whole and ragged, with what is left of either inner dimension behind the last whole stage
 @pytest.mark.parametrize("lens,width,vocab,entries,prompt,cap", [
     ([30000, 9001], 16, 30011, 0, 0.1, 0.0), ([2500, 1, 2595], 64, 256001, 0, 0.0, 5.0), ([5000], 72, 256000, 3, 0.5, 0.0), ([1500, 47], 4104, 9001, 0, 0.0, 5.0), ([2048], 1032, 33000, 5, 0.0, 0.0),
-    ([1100], 2056, 20017, 40, 0.3, 8.0), ([512], 2048, 20011, 0, 0.0, 0.0), ([500, 12], 2048, 20011, 20, 0.0, 5.0), ([4000], 2040, 9000, 0, 0.6, 0.0), ([2000, 1001], 1096, 8129, 9, 0.0, 0.0)])
+    ([1100], 2056, 20017, 40, 0.3, 8.0), ([512], 2048, 20011, 0, 0.0, 0.0), ([500, 12], 2048, 20011, 20, 0.0, 5.0), ([4000], 2040, 9000, 0, 0.6, 0.0), ([2000, 1001], 1096, 8129, 9, 0.0, 0.0),
+    ([200], 2056, 20011, 0, 0.0, 0.0), ([256], 2048, 20017, 11, 0.1, 0.0), ([131], 2048, 29999, 0, 0.0, 6.0), ([100, 99], 2064, 20010, 5, 0.0, 6.0)])
 def test_many_rows(lens, width, vocab, entries, prompt, cap):
     c = Case(35 + vocab, lens, width, vocab, entries, prompt=prompt, cap=cap)
     loss, row, dX = c.run()
@@ -193,6 +194,8 @@ def test_many_rows(lens, width, vocab, entries, prompt, cap):
     n = [max(int((~c.out[a:b]).sum()), 1) for a, b in zip(c.off[:-1], c.off[1:])]
     np.testing.assert_allclose(host(loss), [float(want_row[a:b].sum()) / k for a, b, k in zip(c.off[:-1], c.off[1:], n)], rtol=1e-4)
     assert not dX[torch.from_numpy(c.out).cuda()].any()
+    alone = c.run(gradient=False)
+    assert ((alone[1].double() - want_row).abs() <= 1e-4 * want_row.abs() + 1e-4).all() and alone[2] is None
 
 
 @pytest.mark.parametrize("entries", [0, 6])
