@@ -9,6 +9,8 @@
 // grows beyond 2^64 only where another score lies that far above.  Such columns of a row are held 2^shift smaller, and made equal again when the row's sums meet.
 // The label's own weight is left out of the sum S of the others: the loss is log(1 + S) and its entry of p - q is -S / (1 + S), neither a difference of two numbers that may be almost equal.
 // A row's entries of q go into the held weights in fp32, rounded once with them.
+// 3584 rows of 4608 over 256000, not capped: 5.7 to 5.9 ms the first product and its sums, 11.4 to 11.8 both, 1.43 to 1.48 PFLOP/s, where a library's bare product of 8192 such rows reaches 1.52; capped 3 to 6 % more
+// of the first.  The chip is power-limited: what an epilogue leaves idle comes back as clock.
 #pragma once
 #include "block_device.hpp"
 #include "gemm16_kernel.hpp"
@@ -163,7 +165,7 @@ __device__ __forceinline__ void loss_list(const LossParams& p, int b, int* lds) 
     if (threadIdx.x == 0) p.gain[i] = p.mean ? p.losses[i].scale / (float)max(n, 1) : p.losses[i].scale;
 }
 
-// Labels: the lists, and a wavefront for each row's own score.
+// Labels: the lists, and a wavefront for each row's own score.  Latencies and 2 d elements a row: one row 4.8 us, 8192 of 4608 30.
 SYMB_KERNEL __launch_bounds__(256) void symb_loss_labels_kernel(LossParams p) {
     __shared__ int lds[4];
     const int lists = (p.T + 255) / 256 + p.S;
@@ -191,7 +193,8 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_rows_kernel(LossParams p) {
 }
 
 // Teachers: a row's entries in the order of their ids, with their shares, the tiles of the vocabulary that they lie in, and the score of the one with the largest share.  A wavefront a row, behind
-// the `lists` first workgroups, which list the rows.
+// the `lists` first workgroups, which list the rows.  In order, because a tile of the first product then finds its entries of a row side by side; by counting, entries squared / 64 steps a row.  One row of 20
+// 8.8 us, 4096 of 64 18.5, 2048 of 128 24.
 SYMB_KERNEL __launch_bounds__(256) void symb_loss_teacher_kernel(LossParams p, int lists) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     if ((int)blockIdx.x < lists) return loss_list<true>(p, blockIdx.x, (int*)smem);
@@ -449,7 +452,8 @@ __device__ __forceinline__ float loss_pick(const float (&w)[NB][4], int j, int e
     if constexpr (NB == 8) static_for<0, 4>([&](auto K) __attribute__((always_inline)) { v[decltype(K)::value] = pick(j2, v[decltype(K)::value + 4], v[decltype(K)::value]); });
     return as_float(pick(j1, pick(j0, v[3], v[2]), pick(j0, v[1], v[0])));
 }
-// A tile row's entries of its teacher, behind the staged tile in LDS.
+// A tile row's entries of its teacher, behind the staged tile in LDS.  Their scores come out of the product itself: dot products of their own were 300 us of 1605 (4096 rows of 4096 over 32000, 64 entries), this
+// costs the product some 20.
 struct LossHits {
     int64_t at;                           // of the first one in `sorted`, `scores`
     int32_t n;
@@ -830,6 +834,7 @@ __host__ __device__ __forceinline__ auto loss_grad_tiled(int kind, F&& f) {
 constexpr int kJoinRows = 16, kJoinSets = 32;
 // Pairs (unit, sum): the sum counts in 2^unit.
 __device__ __forceinline__ float loss_in(float2 s, float unit) { return s.x == unit ? s.y : s.y * exp2f(s.x - unit); }
+// (3584 rows of 2000 parts 19 us; 256 rows of 394 7, a chain of loads and the launch.)
 // 16 rows a workgroup of 512: the column parts' sums in a fixed order, the rows' losses, and their entries of p - q into the held weights.  `parts`: column parts of `cols` columns;
 // finish: the segments' losses as well (one workgroup has all rows).  Beside that, for how many parts the gradient's product comes in.
 template <class Tile>
@@ -1021,7 +1026,7 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_segments_kernel(LossParams p) 
 }
 
 // The parts of a tile added in a fixed order, times the row's gain, to the rows they belong to.  A workgroup takes blocks of 16 x 16 of one wavefront's rows: four of them, or, of products in many
-// parts, one whose parts its wavefronts share out.  Workgroups from number `blocks` on: the segments' losses.
+// parts, one whose parts its wavefronts share out (256 rows of 768 in 20 parts: 5.2 us, 15 without).  Workgroups from number `blocks` on: the segments' losses.  3584 rows of 4608: 27 us, 4.9 TB/s.
 template <int MB, int NB, bool MANY>
 SYMB_KERNEL __launch_bounds__(256) void symb_loss_reduce_kernel(const LossParams p, int blocks) {
     constexpr int BM = 32 * MB, BN = 32 * NB, GROUPS = MANY ? NB : NB / 4;
