@@ -807,15 +807,15 @@ SYMB_KERNEL __launch_bounds__(64 * kFewWaves, RB == 1 ? 4 : 2) void symb_loss_fe
 
 // Parts that the second product's inner dimension (the vocabulary) is cut into: as few rounds of workgroups as possible, weighed against the partial tiles' way through memory.
 // Nanoseconds: a stage of a tile of 256x256 and of 256x128, whose workgroup has a CU alone; of 128x128, of two workgroups that share a CU and of one that has it alone; the rest of a workgroup's
-// time; a partial tile, written and read.
-constexpr int kLossParts = 128, kLossRoundNs = 5000;
+// time; a partial tile, written and read (of up to 64 rows kLossTwoNs).
+constexpr int kLossParts = 128, kLossRoundNs = 5000, kLossTwoNs = 15;
 template <int MB, int NB>
 struct LossTile {
     static constexpr int kEdgeM = 32 * MB, kEdgeN = 32 * NB, kSlots = MB == 4 ? 512 : 256;
     static constexpr int kStageNs = NB == 8 ? 1400 : MB == 8 ? 750 : 1100, kLoneNs = MB == 4 ? 720 : kStageNs, kPartNs = NB == 8 ? 116 : 40;
     __host__ __device__ static constexpr int64_t tiles(int64_t rows, int64_t columns) { return (rows + kEdgeM - 1) / kEdgeM * ((columns + kEdgeN - 1) / kEdgeN); }
-    __host__ __device__ static constexpr int64_t ns(int64_t tiles, int stages, int n) {
-        return (tiles * n + kSlots - 1) / kSlots * ((int64_t)((stages + n - 1) / n) * (tiles * n <= kSlots / 2 ? kLoneNs : kStageNs) + kLossRoundNs) + tiles * n * kPartNs;
+    __host__ __device__ static constexpr int64_t ns(int64_t tiles, int stages, int n, bool two) {
+        return (tiles * n + kSlots - 1) / kSlots * ((int64_t)((stages + n - 1) / n) * (tiles * n <= kSlots / 2 ? kLoneNs : kStageNs) + kLossRoundNs) + tiles * n * (two ? kLossTwoNs : kPartNs);
     }
 };
 // room: partial tiles that fit the workspace.
@@ -844,7 +844,7 @@ __device__ __forceinline__ int loss_grad_parts(const LossParams& p, int rows) {
     float best = 3e38f;                                   // (nanoseconds)
     int n = 1;
     for (int k = 1 + (int)(threadIdx.x & 63); k <= kLossParts; k += 64) {
-        const float ns = loss_grad_fits(tiles, stages, k, p.part_tiles) ? (float)Tile::ns(tiles, stages, k) * (1.f + 1e-4f * k) : 3e38f;
+        const float ns = loss_grad_fits(tiles, stages, k, p.part_tiles) ? (float)Tile::ns(tiles, stages, k, p.two) * (1.f + 1e-4f * k) : 3e38f;
         if (ns < best) best = ns, n = k;
     }
 #pragma unroll
@@ -997,6 +997,29 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_grad_kernel(const LossParams p
     const unsigned lane_off = (unsigned)(wave * (MB * NB * 1024) + lane * 16);
     const unsigned long long mine = (unsigned long long)(p.parts + (size_t)(part * tiles + tm * n_tiles + tn) * (BM * BN));
     static_assert(!TT::TALL, "");
+    if constexpr (MB == 4) {
+        if (p.two) {
+            // the second terms' product, of the wavefronts of the tile's lower half, to the first's, and no rows that there are not: 24 KiB of a tile's 64 for 37 rows
+            static_assert(16 * MB == kTwoRows, "");
+            floatx4* const second = reinterpret_cast<floatx4*>(smem) + (wave & 1) * (MB * NB * 64) + lane;
+            auto blocks = [&](auto&& f) __attribute__((always_inline)) {
+                static_for<0, MB>([&](auto I) __attribute__((always_inline)) {
+                    if (16 * decltype(I)::value < own)
+                        static_for<0, NB>([&](auto J) __attribute__((always_inline)) {
+                            constexpr int block = NB * decltype(I)::value + decltype(J)::value;
+                            float v[4];
+                            acc16_read4<4 * block>(v[0], v[1], v[2], v[3]);
+                            f(block, floatx4{v[0], v[1], v[2], v[3]});
+                        });
+                });
+            };
+            if (wave >= 2) blocks([&](int block, floatx4 v) __attribute__((always_inline)) { second[block * 64] = v; });
+            __syncthreads();
+            float* const to = p.parts + (size_t)(part * tiles + tm * n_tiles + tn) * (BM * BN) + (size_t)wave * (MB * NB * 256) + lane * 4;
+            if (wave < 2) blocks([&](int block, floatx4 v) __attribute__((always_inline)) { *(floatx4*)(to + block * 256) = v + second[block * 64]; });
+            return;
+        }
+    }
     if constexpr (NB == 8) asm volatile(SYMB_GEMM16_STORE_PARTIAL : : "v"(lane_off), "s"(mine) : "memory", SYMB_GEMM16_VCLOBBERS);
     else asm volatile(SYMB_GEMM16S_STORE_PARTIAL : : "v"(lane_off), "s"(mine) : "memory", SYMB_GEMM16S_VCLOBBERS);
 }
@@ -1038,16 +1061,13 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_reduce_kernel(const LossParams
     const int lane = threadIdx.x & 63, own = threadIdx.x >> 6, j = blockIdx.x % GROUPS * (MANY ? 1 : 4) + (MANY ? 0 : own);
     const int i = blockIdx.x / GROUPS % MB, wave = blockIdx.x / (GROUPS * MB) % 4, tile = blockIdx.x / (GROUPS * MB * 4);
     const int m0 = tile / n_tiles * BM + (wave >> 1) * (BM / 2) + 16 * i;
-    if (tile >= tiles || m0 >= rows) return;              // (of up to kTwoRows rows what is left has its second terms within the tile)
+    if (tile >= tiles || m0 >= rows) return;
     const int m = m0 + (lane & 15), col = tile % n_tiles * BN + (wave & 1) * (BN / 2) + 16 * j + 4 * (lane >> 4);
     const int n = *p.part_count;
     const float* src = p.parts + (size_t)tile * (BM * BN) + (size_t)(wave * MB * NB + NB * i + j) * 256 + lane * 4;
     floatx4 s = floatx4{0, 0, 0, 0};
 #pragma unroll 8
     for (int k = MANY ? own : 0; k < n; k += MANY ? 4 : 1) s += *(const floatx4*)(src + (size_t)k * tiles * (BM * BN));
-    if (MB == 4 && p.two)                                 // the second terms' product, kTwoRows rows below: of the wavefront two further on
-#pragma unroll 8
-        for (int k = MANY ? own : 0; k < n; k += MANY ? 4 : 1) s += *(const floatx4*)(src + 2 * MB * NB * 256 + (size_t)k * tiles * (BM * BN));
     if constexpr (MANY) {
         lds[own][lane] = s;
         __syncthreads();

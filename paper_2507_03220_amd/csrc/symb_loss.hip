@@ -64,13 +64,13 @@ double score_us(int kind, int rows, const symb_loss_batch* b) {
         return 1e-3 * (double)((tiles + L::kSlots - 1) / L::kSlots) * ((b->width + 63) / 64 * (tiles <= L::kSlots / 2 ? L::kLoneNs : L::kStageNs) + (L::kSlots == 256 ? 8000 : 6000));
     });
 }
-double grad_us(int kind, int rows, const symb_loss_batch* b, int& n) {
+double grad_us(int kind, int rows, const symb_loss_batch* b, bool two, int& n) {
     return loss_grad_tiled(kind, [&](auto tile) {
         using L = decltype(tile);
         const int64_t tiles = L::tiles(rows, b->width);
         int64_t least = INT64_MAX;
         for (int k = 1; k <= kLossParts && loss_grad_fits(tiles, b->vocab / 64, k, INT64_MAX); ++k) {
-            const int64_t ns = L::ns(tiles, b->vocab / 64, k);
+            const int64_t ns = L::ns(tiles, b->vocab / 64, k, two);
             if (ns + ns / 10000 * k < least) least = ns + ns / 10000 * k, n = k;
         }
         return 1e-3 * (double)least;
@@ -86,9 +86,9 @@ int best_score(int rows, const symb_loss_batch* b, bool two, double& us) {
     return best;
 }
 int best_grad(int rows, const symb_loss_batch* b, bool two, int& n, double& us) {
-    us = grad_us(kLossSmall, rows, b, n);
+    us = grad_us(kLossSmall, rows, b, two, n);
     int parts = 1;
-    const double other = two ? us : grad_us(kLossBig, rows, b, parts);
+    const double other = two ? us : grad_us(kLossBig, rows, b, false, parts);
     if (other >= us) return kLossSmall;
     n = parts;
     us = other;
