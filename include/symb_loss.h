@@ -32,7 +32,7 @@ typedef enum { SYMB_LOSS_MEAN = 0, SYMB_LOSS_SUM = 1 } symb_loss_reduction;
 
 typedef struct {
     float scale;                   /* of the gradient: what d (what the client minimises) / d loss_i is.  Finite */
-    float temperature;             /* T_i of symb_distillation: positive, finite; not looked at by symb_cross_entropy */
+    float temperature;             /* T_i of symb_distillation: positive, finite (2^-20 to 2^20; others: SYMB_ERR_UNSUPPORTED); not looked at by symb_cross_entropy */
 } symb_loss;
 
 typedef struct {

@@ -4,7 +4,10 @@ import numpy as np
 
 def _rows(X, W, cap):
     s = X.astype(np.float64) @ W.astype(np.float64).T
-    return (cap * np.tanh(s / cap), 1 - np.tanh(s / cap) ** 2) if cap else (s, np.ones_like(s))
+    if not cap:
+        return s, np.ones_like(s)
+    e = np.exp(-2 * np.minimum(np.abs(s / cap), 350))      # (1 - tanh^2 would cancel)
+    return cap * np.tanh(s / cap), 4 * e / (1 + e) ** 2
 
 
 def _softmax(z):

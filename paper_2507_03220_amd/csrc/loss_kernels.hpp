@@ -176,9 +176,9 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_labels_kernel(LossParams p) {
     if (label < 0) return loss_no_row(p, t);
     double z = loss_score(p, t, label), slope = 1.0;
     if (p.cap > 0.f) {
-        const double th = tanh(z / p.cap);
-        z = th * p.cap;
-        slope = 1.0 - th * th;
+        const double y = z / p.cap, e = exp(-2.0 * fabs(y));
+        slope = 4.0 * e / ((1.0 + e) * (1.0 + e));
+        z = tanh(y) * p.cap;
     }
     z *= (double)kLog2e;
     if ((threadIdx.x & 63) == 0) {
@@ -576,9 +576,9 @@ SYMB_KERNEL __launch_bounds__(256) void symb_loss_scores_kernel(const LossParams
             for (int j = 0; j < NB; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(w[j][e]));
-            if (__any(!(top <= kLossNear * p.cap))) exponents();
+            const float to_exp = a[i] * p.cap;
+            if (__any(!(top <= kLossNear * p.cap) || !(to_exp < __builtin_inff()))) exponents();
             else {
-                const float to_exp = a[i] * p.cap;
 #pragma unroll
                 for (int j = 0; j < NB; ++j)
 #pragma unroll

@@ -30,6 +30,8 @@ symb_status check_loss(symb_handle h, const symb_loss_batch* b, int32_t entries)
         if (!std::isfinite(b->losses[i].scale)) return fail(h, SYMB_ERR_INVALID_ARG, "segment %d: scale must be finite", i);
         if (entries && (!(b->losses[i].temperature > 0.f) || !std::isfinite(b->losses[i].temperature)))
             return fail(h, SYMB_ERR_INVALID_ARG, "segment %d: temperature must be positive and finite", i);
+        if (entries && (b->losses[i].temperature < 0x1p-20f || b->losses[i].temperature > 0x1p20f))        // (its square and its inverse go into fp32 products)
+            return fail(h, SYMB_ERR_UNSUPPORTED, "segment %d: temperature %g, 2^-20 to 2^20 are supported", i, (double)b->losses[i].temperature);
     }
     if (entries < 0) return fail(h, SYMB_ERR_INVALID_ARG, "entries is negative");
     if (entries > SYMB_LOSS_MAX_ENTRIES) return fail(h, SYMB_ERR_UNSUPPORTED, "%d entries: SYMB_LOSS_MAX_ENTRIES at most", entries);

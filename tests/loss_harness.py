@@ -36,6 +36,7 @@ class Case:
             self.ids[self.out] = -1
             self.out |= (self.ids < 0).all(1)
             self.logits = (rng.standard_normal((self.T, entries)) * 3).astype(np.float32)
+            self.logits[self.ids < 0] = NAN                # (absent: not looked at)
         else:
             self.labels = np.where(self.out, -100, token).astype(np.int32)
 
@@ -73,6 +74,14 @@ class Case:
         z = np.minimum(most, self.cap) if self.cap else most
         return (2 * self.width * 2.0 ** -24 * most + (2.0 ** -20 if self.cap else 2.0 ** -22) * z) / T + 2.0 ** -20
 
+    def slope_error(self):
+        """How far 1 - tanh^2(s / cap) may be off, relative: 2 / cap times what the score may be, 2^-21 of |s / cap| (that quotient's and the exponential's roundings), 2^-18 for a polynomial of 2^-22 in it."""
+        if not self.cap:
+            return np.zeros(self.T)
+        x, w = np.abs(np.nan_to_num(host(self.X), nan=0.0)), np.abs(host(self.W))
+        most = (x @ w.T).max(1)
+        return np.expm1(np.minimum(2 * self.width * 2.0 ** -24 * most / self.cap, 50)) + 2.0 ** -18 + 2.0 ** -21 * np.minimum(most / self.cap, 100)
+
     def check(self, what):
         loss, row, dX = self.run()
         want_loss, want_row, want, mass, both = self.want()
@@ -89,9 +98,9 @@ class Case:
         n = np.array([max((~self.out[a:b]).sum(), 1) if self.mean else 1 for a, b in zip(self.off[:-1], self.off[1:])])
         total = np.array([bound[a:b].sum() + 2.0 ** -20 * np.abs(want_row[a:b]).sum() for a, b in zip(self.off[:-1], self.off[1:])])
         close(loss, want_loss, total / n + 1e-30, what + ": segments")
-        # half a step of the output, half a step of each weight (of its second term, up to 64 rows), the weights' own errors (p's and, in l, once more), sums over the vocabulary in fp32
+        # half a step of the output, half a step of each weight (of its second term, up to 64 rows), the weights' own errors (p's and, in l, once more; the slope's), sums over the vocabulary in fp32
         held = 2.0 ** -16 if self.T <= 64 else 2.0 ** -8
-        tol = 1.02 * 2.0 ** -8 * np.abs(want) + (1.02 * held + self.vocab * 2.0 ** -24) * mass + 2.2 * e[:, None] * both + 1e-30
+        tol = 1.02 * 2.0 ** -8 * np.abs(want) + (1.02 * held + self.vocab * 2.0 ** -24) * mass + (2.2 * e + self.slope_error())[:, None] * both + 1e-30
         close(dX, want, tol, what + ": gradient")
         again = self.run()
         assert all(torch.equal(a, b) for a, b in zip((loss, row, dX), again)), what

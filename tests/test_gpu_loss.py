@@ -63,6 +63,23 @@ def test_sure_rows_keep_their_precision():
     assert float(row.min()) < 1e-9
 
 
+@pytest.mark.parametrize("rows", [20, 60, 200])
+@pytest.mark.parametrize("entries", [0, 7])
+def test_caps_and_temperatures_of_any_size(entries, rows):
+    """From caps that flatten every score to caps that change none, and the ends of what a temperature may be."""
+    for cap in (1e-30, 1e-3, 0.5, 4.0, 30.0, 1e6, 1e30, 3e38):
+        Case(21, [rows], 128, 900, entries, cap=cap, std=3.0).check(f"cap {cap}")
+    if entries:
+        for T in (2.0 ** -20, 0.01, 100.0, 2.0 ** 20):
+            for cap in (0.0, 8.0, 3e38):
+                c = Case(22, [rows], 128, 900, entries, cap=cap, std=3.0, temperatures=[T])
+                if T < 1e-3:                               # (the scores themselves to 2^-20 of 1e7: which one is the largest is all that is left to check)
+                    loss, row, dX = c.run()
+                    assert torch.isfinite(row).all() and torch.isfinite(loss).all() and torch.isfinite(dX).all()
+                else:
+                    c.check(f"temperature {T}, cap {cap}")
+
+
 def test_a_token_twice():
     c = Case(13, [9, 30], 64, 300, 12)
     c.ids[:, 5] = c.ids[:, 2]

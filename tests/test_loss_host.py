@@ -31,6 +31,10 @@ def test_refusals():
     for t in (0.0, -1.0, nan, inf):
         assert _status(_batch(losses=[sb.Loss(1.0, t)])) == sb.SYMB_OK                  # (cross entropy does not look at it)
         assert _status(_batch(losses=[sb.Loss(1.0, t)]), 3) == sb.SYMB_ERR_INVALID_ARG
+    for t in (2.0 ** -20, 2.0 ** 20):
+        assert _status(_batch(losses=[sb.Loss(1.0, t)]), 3) == sb.SYMB_OK
+    for t in (2.0 ** -21, 1e-39, 2.0 ** 21):
+        assert _status(_batch(losses=[sb.Loss(1.0, t)]), 3) == sb.SYMB_ERR_UNSUPPORTED
     assert _status(_batch(), -1) == sb.SYMB_ERR_INVALID_ARG
     for off in ((0, 4, 3), (1, 4)):
         assert _status(_batch(off=off)) == sb.SYMB_ERR_BAD_SEGMENTS
