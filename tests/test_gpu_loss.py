@@ -151,6 +151,23 @@ def test_rows_that_take_no_part(entries):
     assert loss[1] == 0 and not dX[4:11].any()
 
 
+@pytest.mark.parametrize("entries", [0, 4])
+def test_holes_and_many_clients(entries):
+    """Rows left out here and there, over several lists of 256; thousands of clients, many of them without a row or without one that takes part."""
+    rng = np.random.default_rng(23)
+    for lens in ([1000, 3, 0, 530], [int(n) for n in rng.integers(0, 4, 2500)]):
+        c = Case(24, lens, 64, 300, entries)
+        hole = rng.random(c.T) < 0.6
+        if entries:
+            c.ids[hole] = -3
+        else:
+            c.labels[hole] = -1
+        c.X[torch.from_numpy(hole).cuda()] = NAN
+        c.out |= hole
+        _, row, dX = c.check("holes")
+        assert not row[torch.from_numpy(c.out).cuda()].any() and not dX[torch.from_numpy(c.out).cuda()].any()
+
+
 def test_in_place():
     for entries in (0, 8):
         c = Case(18, [100, 300], 192, 700, entries, prompt=0.3)
