@@ -818,8 +818,8 @@ struct LossTile {
         return (tiles * n + kSlots - 1) / kSlots * ((int64_t)((stages + n - 1) / n) * (tiles * n <= kSlots / 2 ? kLoneNs : kStageNs) + kLossRoundNs) + tiles * n * (two ? kLossTwoNs : kPartNs);
     }
 };
-// room: partial tiles that fit the workspace.
-__host__ __device__ constexpr bool loss_grad_fits(int64_t tiles, int stages, int n, int64_t room) { return n == 1 || (tiles * n <= room && stages / n >= 4); }
+// room: partial tiles that fit the workspace.  (Four to eight rounds of workgroups even out whatever there is to even out.)
+__host__ __device__ constexpr bool loss_grad_fits(int64_t tiles, int stages, int n, int64_t room) { return n == 1 || (tiles * n <= room && tiles * n <= 2048 && stages / n >= 4); }
 enum LossTileKind : int32_t { kLossBig, kLossTall, kLossSmall };               // 256x256, 256x128, 128x128
 template <class F>
 __host__ __device__ __forceinline__ auto loss_tiled(int kind, F&& f) {
